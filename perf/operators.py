@@ -188,15 +188,20 @@ def _blocks(x):
     return torch.nn.functional.pad(x, (0, -cols % 32)).reshape(rows, -1, 32)
 
 
+def _two_to(e):
+    """2^e in fp32 for whole e from -127 to 127, exactly (a library's power may be a rounding off)."""
+    return torch.where(e > -127, (e + 127) << 23, 1 << 22).to(torch.int32).view(torch.float32)
+
+
 def _through_mx4(x):
     """The mx4 values nearest to x (fp32), ties to the even mantissa."""
     b = _blocks(x)
     _, e = torch.frexp(b.abs().amax(-1, keepdim=True))
     e = (e - 3).clamp(min=-127)  # the largest value of a block gets the exponent of 4, the largest one's
-    a = torch.ldexp(b.abs(), -e)
+    a = b.abs() * _two_to(-e)
     step = torch.where(a < 2, 0.5, torch.where(a < 4, 1.0, 2.0))
     a = (torch.round(a / step) * step).clamp(max=6.0)
-    return torch.ldexp(torch.copysign(a, b), e).reshape(x.shape[0], -1)[:, :x.shape[1]]
+    return (torch.copysign(a, b) * _two_to(e)).reshape(x.shape[0], -1)[:, :x.shape[1]]
 
 
 def _unpack(q, scale, cols):
@@ -204,11 +209,10 @@ def _unpack(q, scale, cols):
     code = torch.stack([q & 15, q >> 4], -1).flatten(-2).to(torch.int32)
     mag = code & 7
     small = 0.5 * mag
-    large = torch.ldexp((2 + (mag & 1)).float(), (mag >> 1) - 2)
+    large = (2 + (mag & 1)) * _two_to((mag >> 1) - 2)
     v = torch.where(mag < 2, small, large) * (1 - 2 * (code >> 3))
     v = v.reshape(*scale.shape, 32)
-    s = torch.ldexp(torch.ones_like(scale, dtype=torch.float32), scale.to(torch.int32) - 127)
-    return (v * s.unsqueeze(-1)).flatten(-2)[..., :cols]
+    return (v * _two_to(scale.to(torch.int32) - 127).unsqueeze(-1)).flatten(-2)[..., :cols]
 
 
 def _plain_grouped(s):
@@ -310,8 +314,9 @@ def _quantized64(x):
     """mx4 values of x by search: the table entry nearest to |x| / scale, of two as near the one with an even code."""
     rows, cols = x.shape
     b = torch.nn.functional.pad(x.double(), (0, -cols % 32)).reshape(rows, -1, 32)
-    top = b.abs().amax(-1, keepdim=True)
-    scale = torch.pow(2.0, torch.floor(torch.log2(top.clamp(min=2.0 ** -149))).double() - 2).clamp(min=2.0 ** -127)
+    top = b.abs().amax(-1, keepdim=True).clamp(min=2.0 ** -149)
+    # a double's bits without its mantissa are the power of two below it
+    scale = ((top.view(torch.int64) >> 52) << 52).view(torch.float64).mul(0.25).clamp(min=2.0 ** -127)
     a = b.abs() / scale
     best, dist = torch.zeros_like(a), a.clone()
     for code, value in enumerate(_E2M1[1:], 1):
@@ -326,7 +331,7 @@ def _values64(q, scale, cols):
     v = torch.empty((*q.shape, 2), dtype=torch.float64, device=q.device)
     v[..., 0] = table[(q % 16).long()]
     v[..., 1] = table[torch.div(q, 16, rounding_mode="floor").long()]
-    v = v.reshape(*q.shape[:-1], -1) * torch.pow(2.0, scale.double() - 127).repeat_interleave(32, dim=-1)
+    v = v.reshape(*q.shape[:-1], -1) * ((scale.long() + 896) << 52).view(torch.float64).repeat_interleave(32, dim=-1)
     return v[..., :cols]
 
 
