@@ -11,6 +11,8 @@
  * Conventions for every entry point:
  *  - Tensors are fp32, NCHW, row-major, contiguous, in DEVICE memory,
  *    allocated and owned by the caller.  The library allocates nothing.
+ *    The operators of the section on mixtures of experts also take bf16,
+ *    fp16 and microscaled 4-bit tensors.
  *  - Calls are asynchronous: argument checks run on the host first and a
  *    negative status means nothing was enqueued; on CNN_OK the kernels are
  *    enqueued on `stream` (a hipStream_t; NULL = the null stream) and the
@@ -183,6 +185,105 @@ int cnn_relu_fwd(const float* x, float* y, int64_t n, cnn_stream_t stream);
  * y == x (in place) is allowed; other overlaps are CNN_ERR_INVALID.  Inputs
  * must be finite (NaN / infinity give unspecified results). */
 int cnn_softmax_fwd(const float* x, int N, int C, int HW, float* y, cnn_stream_t stream);
+
+/* ---------------------------------------------------------------- experts, 4-bit weights
+ * The fully connected layers of a mixture of experts, and layers whose
+ * weights are held in 4 bits: products as cnn_fc_fwd's, for serving.  Beyond
+ * the paper's layers.  A block of it is
+ *   cnn_route_fwd       logits -> choices, and the order of rows by expert
+ *   cnn_fc_grouped_fwd  every expert's rows through its first layer, gathered
+ *   cnn_fc_grouped_fwd  ... and its second
+ *   cnn_combine_fwd     the weighted sum of each token's rows
+ * with weights brought to 4 bits once, by cnn_mx4_quantize.  Nothing here
+ * reads device data on the host, so that all of it can be captured.
+ */
+typedef enum cnn_dtype {
+    CNN_F32 = 0,
+    CNN_BF16 = 1,
+    CNN_F16 = 2,
+    /* Microscaled 4-bit values ("mx4").  A row of C values is
+     * ceil(C / 32) blocks of 32.  A block is 16 bytes, two values a byte,
+     * the earlier one in the low half: a sign bit, then 0..7 for 0, 0.5, 1,
+     * 1.5, 2, 3, 4, 6.  A scale byte s for each block, in a tensor of its
+     * own, multiplies them by 2^(s - 127); s = 255 makes the whole block
+     * NaN.  So R rows are uint8 [R][ceil(C/32)*16], 16-byte aligned, and
+     * uint8 [R][ceil(C/32)].  The values behind column C must be 0. */
+    CNN_MX4 = 3
+} cnn_dtype;
+
+/* x [rows][cols] (fp32, bf16 or fp16) to mx4: s = floor(log2(a)) - 2 + 127
+ * (at least 0) with a the block's largest magnitude, every value over
+ * 2^(s - 127) rounded to the nearest one there is, ties to the even code, 6 at
+ * most.  A NaN or an infinity in a block makes it NaN.  q and scale as in
+ * CNN_MX4, zeros behind the last column. */
+int cnn_mx4_quantize(const void* x, int x_type, int rows, int cols,
+                     uint8_t* q, uint8_t* scale, cnn_stream_t stream);
+
+/* The values of mx4 rows, rounded to y's type (infinity above its range). */
+int cnn_mx4_dequantize(const uint8_t* q, const uint8_t* scale, int rows, int cols,
+                       void* y, int y_type, cnn_stream_t stream);
+
+/* Fully-connected layer with mx4 weights: y[n,o] = b[o] + sum_i x[n,i] * w[o,i].
+ *   x [N][I]; x_type fp32, bf16 or fp16 (then x_scale is NULL and y_type is
+ *     x_type), or mx4 (x_scale, and any wide y_type)
+ *   w, w_scale: O rows of I, mx4       bias fp32 [O] or NULL
+ *   y [N][O]
+ * Wide inputs are not quantised: products are of x as it is with the values
+ * that w stands for (fp32 inputs below 2^-107 in magnitude keep an absolute
+ * precision of 2^-133), sums are fp32 and the result is rounded once.
+ * fuse_relu = 1 applies y = max(y, 0).  The result does not change from call to
+ * call. */
+int cnn_fc_mx4_fwd(const void* x, const uint8_t* x_scale, int x_type, int N, int I,
+                   const uint8_t* w, const uint8_t* w_scale, const float* bias, int O,
+                   int fuse_relu, void* y, int y_type, cnn_stream_t stream);
+
+/* Fully-connected layers of groups of rows, each with weights of its own:
+ *   y[m,o] = b[g,o] + sum_i x[rows[m],i] * w[g,o,i]   for offsets[g] <= m < offsets[g+1]
+ *   x [N][I]       rows int32 [M], or NULL for row m of x (then N must be M)
+ *   offsets int32 [groups + 1], in device memory, not decreasing, from 0; equal
+ *     neighbours are a group without rows.  What lies outside [0, M] is cut off.
+ *   w [groups][O][I] of x's type, or mx4; x may be mx4 where w is
+ *   bias fp32 [groups][O] or NULL
+ *   y [M][O]; rows of y in no group (from offsets[groups] on) are left as they
+ *     were
+ * rows[m] outside [0, N) stands for a row of zeros.  Types, scales and
+ * rounding as cnn_fc_mx4_fwd; every w matrix holds fewer than 2^31 elements,
+ * all of them together may hold more.  At most 2^20 groups. */
+int cnn_fc_grouped_fwd(const void* x, const uint8_t* x_scale, int x_type, int N, int I,
+                       const int32_t* rows, int M, const int32_t* offsets, int groups,
+                       const void* w, const uint8_t* w_scale, int w_type,
+                       const float* bias, int O, int fuse_relu,
+                       void* y, int y_type, cnn_stream_t stream);
+
+/* Device workspace of cnn_route_fwd (0 up to 64 tokens, and on error). */
+size_t cnn_route_workspace_bytes(int T, int E, int k);
+
+/* Routing of T tokens to k of E experts each.
+ *   logits [T][E], fp32, bf16 or fp16
+ *   expert int32 [T][k]: the experts of a token's k largest logits, largest
+ *     first, ties to the lower expert.  Minus infinity and NaN are never
+ *     chosen; choices that are left over are -1.
+ *   weight fp32 [T][k]: exp(logit) over the sum of exp over all the token's
+ *     experts (but for NaN), or, with renormalize = 1, over its choices; 0
+ *     where there is no choice (NaN beside a logit of plus infinity).
+ *   rows int32 [T*k]: the choices' tokens, ordered by expert, then token; -1
+ *     behind the last choice
+ *   offsets int32 [E+1]: rows[offsets[e]] is the first of expert e's; the last
+ *     entry is the number of choices
+ *   slot int32 [T][k]: where in rows a choice stands, -1 for no choice
+ * rows and offsets are cnn_fc_grouped_fwd's, slot and weight cnn_combine_fwd's.
+ * E <= 1024, k <= 64, k <= E, T <= 2^27.  T = 0 clears offsets.  Calls that
+ * overlap need workspaces of their own. */
+int cnn_route_fwd(const void* logits, int type, int T, int E, int k, int renormalize,
+                  int32_t* expert, float* weight, int32_t* rows, int32_t* offsets,
+                  int32_t* slot, void* ws, size_t ws_bytes, cnn_stream_t stream);
+
+/* Weighted sums of rows: y[n,d] = sum_j weight[n,j] * x[slot[n,j],d], j
+ * ascending, in fp32, rounded once.  x [M][D], slot int32 [N][k], weight fp32
+ * [N][k], y [N][D]; x and y of one type, fp32, bf16 or fp16.  A slot outside
+ * [0, M) adds nothing, whatever its weight. */
+int cnn_combine_fwd(const void* x, int type, int M, int D, const int32_t* slot,
+                    const float* weight, int N, int k, void* y, cnn_stream_t stream);
 
 /* ---------------------------------------------------------------- networks
  * A network is an array of layer descriptors executed in order (the paper's

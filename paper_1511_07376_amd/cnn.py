@@ -1,7 +1,8 @@
 """Python binding of libcnn (include/cnn.h): argument marshalling only.
 
 Every function here checks that its tensors are contiguous float32 CUDA
-(ROCm) tensors, passes their device pointers and the current torch stream to
+(ROCm) tensors (those of the section on mixtures of experts: contiguous, on one
+GPU, of the types and shapes they state), passes their device pointers and the current torch stream to
 the C entry point of the same name, and raises ``CnnError`` with
 ``cnn_last_error()`` on a non-OK status.  All computation happens in the HIP
 kernels of libcnn; torch provides device memory and the stream.  Importing
@@ -35,6 +36,7 @@ CNN_OK, CNN_ERR_INVALID, CNN_ERR_UNSUPPORTED, CNN_ERR_HIP, CNN_ERR_WORKSPACE = 0
 CNN_POOL_MAX, CNN_POOL_AVG = 0, 1
 CNN_LAYER_CONV, CNN_LAYER_FC, CNN_LAYER_POOL, CNN_LAYER_LRN, CNN_LAYER_RELU = 0, 1, 2, 3, 4
 CNN_LAYER_SOFTMAX = 5
+CNN_F32, CNN_BF16, CNN_F16, CNN_MX4 = 0, 1, 2, 3
 
 
 class cnn_layer_desc(ctypes.Structure):
@@ -61,6 +63,14 @@ lib.cnn_lrn_fwd.argtypes = [_p, _i, _i, _i, _i, _i, ctypes.c_float, ctypes.c_flo
                             _p, _p]
 lib.cnn_relu_fwd.argtypes = [_p, _p, ctypes.c_int64, _p]
 lib.cnn_softmax_fwd.argtypes = [_p, _i, _i, _i, _p, _p]
+lib.cnn_mx4_quantize.argtypes = [_p, _i, _i, _i, _p, _p, _p]
+lib.cnn_mx4_dequantize.argtypes = [_p, _p, _i, _i, _p, _i, _p]
+lib.cnn_fc_mx4_fwd.argtypes = [_p, _p, _i, _i, _i, _p, _p, _p, _i, _i, _p, _i, _p]
+lib.cnn_fc_grouped_fwd.argtypes = [_p, _p, _i, _i, _i, _p, _i, _p, _i, _p, _p, _i, _p, _i, _i, _p, _i, _p]
+lib.cnn_route_workspace_bytes.argtypes = [_i, _i, _i]
+lib.cnn_route_workspace_bytes.restype = ctypes.c_size_t
+lib.cnn_route_fwd.argtypes = [_p, _i, _i, _i, _i, _i, _p, _p, _p, _p, _p, _p, ctypes.c_size_t, _p]
+lib.cnn_combine_fwd.argtypes = [_p, _i, _i, _i, _p, _p, _i, _i, _p, _p]
 
 
 class cnn_netfile_config(ctypes.Structure):
@@ -105,6 +115,8 @@ lib.cnn_last_error.restype = ctypes.c_char_p
 lib.cnn_version.restype = ctypes.c_char_p
 for _name in ("cnn_conv2d_out_shape", "cnn_pool_out_shape", "cnn_conv2d_fwd", "cnn_fc_fwd",
               "cnn_pool_fwd", "cnn_lrn_fwd", "cnn_relu_fwd", "cnn_softmax_fwd", "cnn_net_out_shape",
+              "cnn_mx4_quantize", "cnn_mx4_dequantize", "cnn_fc_mx4_fwd", "cnn_fc_grouped_fwd",
+              "cnn_route_fwd", "cnn_combine_fwd",
               "cnn_net_fwd",
               "cnn_net_fwd_timed", "cnn_net_fwd_kernel_timed", "cnn_net_fwd_dump", "cnn_net_fwd_noalloc",
               "cnn_conv2d_fwd_config",
@@ -115,6 +127,8 @@ for _name in ("cnn_conv2d_out_shape", "cnn_pool_out_shape", "cnn_conv2d_fwd", "c
 
 EXPORTED = ("cnn_conv2d_out_shape", "cnn_pool_out_shape", "cnn_conv2d_fwd", "cnn_fc_fwd",
             "cnn_pool_fwd", "cnn_lrn_fwd", "cnn_relu_fwd", "cnn_softmax_fwd", "cnn_net_out_shape",
+            "cnn_mx4_quantize", "cnn_mx4_dequantize", "cnn_fc_mx4_fwd", "cnn_fc_grouped_fwd",
+            "cnn_route_workspace_bytes", "cnn_route_fwd", "cnn_combine_fwd",
             "cnn_net_workspace_bytes", "cnn_net_fwd", "cnn_net_fwd_timed", "cnn_net_fwd_kernel_timed",
             "cnn_net_fwd_dump",
             "cnn_net_fwd_noalloc", "cnn_last_error",
@@ -317,6 +331,225 @@ def cnn_softmax_fwd(x, y=None, stream=None):
     for d in x.shape[2:]:
         HW *= d
     _ok(lib.cnn_softmax_fwd(_dev(x, "x"), N, C, HW, _dev(y, "y"), _stream(stream)))
+    return y
+
+
+# ---------------------------------------------------------------- experts, 4-bit weights
+_WIDE = {torch.float32: CNN_F32, torch.bfloat16: CNN_BF16, torch.float16: CNN_F16}
+
+
+def _on(t, name: str, device: torch.device, dtype=None, shape=None):
+    """Device pointer of a contiguous tensor on `device`, of this type and shape where given; None for None."""
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor) or t.device != device:
+        raise TypeError(f"{name} must be a tensor on {device}")
+    if dtype is not None and t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if not t.is_contiguous():
+        raise TypeError(f"{name} must be contiguous")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    return t.data_ptr()
+
+
+def _wide(dtype, name: str) -> int:
+    code = _WIDE.get(dtype)
+    if code is None:
+        raise TypeError(f"{name} must be float32, bfloat16 or float16, got {dtype}")
+    return code
+
+
+def _gpu(t, name: str) -> torch.device:
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a GPU tensor")
+    return t.device
+
+
+class _Launch:
+    """The device and the stream that a call's kernels go to, and its outputs are allocated for: those of its
+    tensors' GPU, current or not, and the stream it was given, else the current one of that GPU."""
+
+    __slots__ = ("handle", "_guards")
+
+    def __init__(self, device, stream):
+        self._guards = ()
+        if stream is None and device.index == torch.cuda.current_device():
+            self.handle = torch.cuda.current_stream().cuda_stream
+            return
+        guards = [torch.cuda.device(device)]
+        if stream is not None:
+            if not isinstance(stream, torch.cuda.Stream):
+                handle = int(stream)
+                stream = (torch.cuda.ExternalStream(handle, device=device) if handle
+                          else torch.cuda.default_stream(device))
+            if stream.device != device:
+                raise ValueError(f"the stream is of {stream.device}, the tensors are on {device}")
+            guards.append(torch.cuda.stream(stream))
+        for g in guards:
+            g.__enter__()
+        self._guards = guards
+        self.handle = torch.cuda.current_stream().cuda_stream
+
+    def __enter__(self):
+        return self.handle
+
+    def __exit__(self, *exc):
+        for g in reversed(self._guards):
+            g.__exit__(*exc)
+
+
+def cnn_mx4_quantize(x, q=None, scale=None, stream=None):
+    """x [rows][cols] -> (q uint8 [rows][ceil(cols/32)*16], scale uint8 [rows][ceil(cols/32)]): mx4 (CNN_MX4).
+
+    Leading dimensions are kept: x [G][O][I] gives q [G][O][...]."""
+    device = _gpu(x, "x")
+    if x.dim() < 2:
+        raise ValueError("mx4_quantize: x must be [rows][cols]")
+    lead, cols = tuple(x.shape[:-1]), x.shape[-1]
+    rows = 1
+    for d in lead:
+        rows *= d
+    blocks = (cols + 31) // 32
+    code = _wide(x.dtype, "x")
+    xp = _on(x, "x", device)
+    with _Launch(device, stream) as st:
+        if q is None:
+            q = torch.empty(lead + (blocks * 16,), dtype=torch.uint8, device=device)
+        if scale is None:
+            scale = torch.empty(lead + (blocks,), dtype=torch.uint8, device=device)
+        _ok(lib.cnn_mx4_quantize(xp, code, rows, cols, _on(q, "q", device, torch.uint8, lead + (blocks * 16,)),
+                                 _on(scale, "scale", device, torch.uint8, lead + (blocks,)), st))
+    return q, scale
+
+
+def cnn_mx4_dequantize(q, scale, cols=None, dtype=torch.float32, y=None, stream=None):
+    """The values of mx4 rows, [...][cols] (cols: 32 a block if not given)."""
+    device = _gpu(q, "q")
+    blocks = scale.shape[-1]
+    cols = 32 * blocks if cols is None else int(cols)
+    if not 32 * (blocks - 1) < cols <= 32 * blocks:
+        raise ValueError(f"mx4_dequantize: {cols} columns in {blocks} blocks")
+    lead = tuple(scale.shape[:-1])
+    rows = 1
+    for d in lead:
+        rows *= d
+    qp = _on(q, "q", device, torch.uint8, lead + (blocks * 16,))
+    sp = _on(scale, "scale", device, torch.uint8)
+    with _Launch(device, stream) as st:
+        if y is None:
+            y = torch.empty(lead + (cols,), dtype=dtype, device=device)
+        _ok(lib.cnn_mx4_dequantize(qp, sp, rows, cols, _on(y, "y", device, None, lead + (cols,)),
+                                   _wide(y.dtype, "y"), st))
+    return y
+
+
+def _operand(x, x_scale, device, name: str):
+    """(pointer, scale pointer, type, rows, columns as far as the tensors say) of rows that may be mx4."""
+    if x_scale is None:
+        return _on(x, name, device), None, _wide(x.dtype, name), x.shape[-1]
+    blocks = x_scale.shape[-1]
+    return (_on(x, name, device, torch.uint8, tuple(x_scale.shape[:-1]) + (blocks * 16,)),
+            _on(x_scale, name + "_scale", device, torch.uint8), CNN_MX4, 32 * blocks)
+
+
+def _columns(x_type: int, x_cols: int, w_type: int, w_cols: int, what: str) -> int:
+    """The length of the reduction: that of x, or whole blocks where both are mx4."""
+    fits = x_cols == w_cols if (x_type == CNN_MX4) == (w_type == CNN_MX4) else w_cols - 32 < x_cols <= w_cols
+    if not fits:
+        raise ValueError(f"{what}: x has {x_cols} columns, w {w_cols}")
+    return x_cols
+
+
+def cnn_fc_mx4_fwd(x, w, w_scale, bias=None, fuse_relu=False, x_scale=None, y_dtype=None, y=None, stream=None):
+    """x [N][I] (or [N][C][H][W], read flattened), w and w_scale mx4 of [O][I] -> y [N][O], of x's type.
+
+    With x_scale x is mx4 too, and y of type y_dtype (float32 if not given)."""
+    device = _gpu(x, "x")
+    if x_scale is None and x.dim() > 2:
+        x = x.reshape(x.shape[0], -1) if x.is_contiguous() else x
+    if x.dim() != 2 or w.dim() != 2 or w_scale.dim() != 2:
+        raise ValueError("fc_mx4: x, w and w_scale must have two dimensions")
+    xp, xs, xt, xc = _operand(x, x_scale, device, "x")
+    wp, ws, wt, wc = _operand(w, w_scale, device, "w")
+    cols = _columns(xt, xc, wt, wc, "fc_mx4")
+    N, O = x.shape[0], w.shape[0]
+    bp = _on(bias, "bias", device, torch.float32, (O,))
+    dtype = x.dtype if xs is None else y_dtype or torch.float32
+    with _Launch(device, stream) as st:
+        if y is None:
+            y = torch.empty((N, O), dtype=dtype, device=device)
+        _ok(lib.cnn_fc_mx4_fwd(xp, xs, xt, N, cols, wp, ws, bp, O, 1 if fuse_relu else 0,
+                               _on(y, "y", device, dtype, (N, O)), _WIDE.get(dtype, -1), st))
+    return y
+
+
+def cnn_fc_grouped_fwd(x, w, offsets, bias=None, fuse_relu=False, rows=None, w_scale=None, x_scale=None,
+                       y_dtype=None, y=None, stream=None):
+    """x [N][I], w [G][O][I], offsets int32 [G+1] -> y [M][O], of x's type: row m of y is row rows[m] (int32 [M];
+    row m if not given) of x through the weights of the group with offsets[g] <= m < offsets[g+1].
+
+    With w_scale [G][O][blocks] w is mx4; with x_scale x is too, and y of type y_dtype (float32 if not given).
+    Rows of y in no group are not written."""
+    device = _gpu(x, "x")
+    if x.dim() != 2 or w.dim() != 3:
+        raise ValueError("fc_grouped: x must be [N][I], w [G][O][I]")
+    xp, xs, xt, xc = _operand(x, x_scale, device, "x")
+    wp, ws, wt, wc = _operand(w, w_scale, device, "w")
+    cols = _columns(xt, xc, wt, wc, "fc_grouped")
+    N, (G, O) = x.shape[0], w.shape[:2]
+    M = N if rows is None else rows.numel()
+    bp = _on(bias, "bias", device, torch.float32, (G, O))
+    op = _on(offsets, "offsets", device, torch.int32, (G + 1,))
+    rp = _on(rows, "rows", device, torch.int32)
+    dtype = x.dtype if xs is None else y_dtype or torch.float32
+    with _Launch(device, stream) as st:
+        if y is None:
+            y = torch.empty((M, O), dtype=dtype, device=device)
+        _ok(lib.cnn_fc_grouped_fwd(xp, xs, xt, N, cols, rp, M, op, G, wp, ws, wt, bp, O, 1 if fuse_relu else 0,
+                                   _on(y, "y", device, dtype, (M, O)), _WIDE.get(dtype, -1), st))
+    return y
+
+
+def cnn_route_fwd(logits, k, renormalize=False, stream=None):
+    """logits [T][E] -> (expert int32 [T][k], weight float32 [T][k], rows int32 [T*k], offsets int32 [E+1],
+    slot int32 [T][k]): each token's k experts and their weights, and the rows for cnn_fc_grouped_fwd."""
+    device = _gpu(logits, "logits")
+    if logits.dim() != 2:
+        raise ValueError("route: logits must be [T][E]")
+    T, E = logits.shape
+    k = int(k)
+    code = _wide(logits.dtype, "logits")
+    lp = _on(logits, "logits", device)
+    need = lib.cnn_route_workspace_bytes(T, E, k)
+    with _Launch(device, stream) as st:
+        n = max(T * k, 0)
+        expert = torch.empty((T, max(k, 0)), dtype=torch.int32, device=device)
+        weight = torch.empty((T, max(k, 0)), dtype=torch.float32, device=device)
+        slot = torch.empty((T, max(k, 0)), dtype=torch.int32, device=device)
+        rows = torch.empty(n, dtype=torch.int32, device=device)
+        offsets = torch.empty(E + 1, dtype=torch.int32, device=device)
+        ws = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+        _ok(lib.cnn_route_fwd(lp, code, T, E, k, 1 if renormalize else 0, expert.data_ptr(), weight.data_ptr(),
+                              rows.data_ptr(), offsets.data_ptr(), slot.data_ptr(),
+                              ws.data_ptr() if need else None, need, st))
+    return expert, weight, rows, offsets, slot
+
+
+def cnn_combine_fwd(x, slot, weight, y=None, stream=None):
+    """x [M][D], slot int32 [N][k], weight float32 [N][k] -> y [N][D] = sum over j of weight[n][j] * x[slot[n][j]]."""
+    device = _gpu(x, "x")
+    if x.dim() != 2 or slot.dim() != 2:
+        raise ValueError("combine: x must be [M][D], slot [N][k]")
+    (M, D), (N, k) = x.shape, slot.shape
+    code = _wide(x.dtype, "x")
+    xp = _on(x, "x", device)
+    sp = _on(slot, "slot", device, torch.int32)
+    wp = _on(weight, "weight", device, torch.float32, (N, k))
+    with _Launch(device, stream) as st:
+        if y is None:
+            y = torch.empty((N, D), dtype=x.dtype, device=device)
+        _ok(lib.cnn_combine_fwd(xp, code, M, D, sp, wp, N, k, _on(y, "y", device, x.dtype, (N, D)), st))
     return y
 
 

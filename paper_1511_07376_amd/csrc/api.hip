@@ -11,6 +11,7 @@
 #include <vector>
 
 #include "common.h"
+#include "wide_types.h"
 
 namespace cnn {
 
@@ -141,6 +142,59 @@ int check_fc(int N, int I, int O) {
     if (N < 0 || I <= 0 || O <= 0) return fail(CNN_ERR_INVALID, "fc: N=%d I=%d O=%d", N, I, O);
     if (too_big(N, I) || too_big(N, O) || too_big(O, I))
         return fail(CNN_ERR_UNSUPPORTED, "fc: tensor exceeds 2^31-1 elements");
+    return CNN_OK;
+}
+
+// ------------------------------------------------------------------ mixture of experts, 4-bit values
+bool wide(int type) { return type == CNN_F32 || type == CNN_BF16 || type == CNN_F16; }
+
+bool aligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
+
+int check_mx4(const char* what, const void* wide_side, int type, int rows, int cols, const uint8_t* q,
+              const uint8_t* scale) {
+    if (!wide(type)) return fail(CNN_ERR_INVALID, "%s: type %d is not fp32, bf16 or fp16", what, type);
+    if (rows < 0 || cols <= 0) return fail(CNN_ERR_INVALID, "%s: %d rows of %d", what, rows, cols);
+    if (rows != 0 && (!wide_side || !q || !scale)) return fail(CNN_ERR_INVALID, "%s: null pointer", what);
+    if (too_big(rows, cols)) return fail(CNN_ERR_UNSUPPORTED, "%s: more than 2^31-1 values", what);
+    if (!aligned(wide_side, type_bytes(type)))
+        return fail(CNN_ERR_INVALID, "%s: values not aligned to their type", what);
+    if (!aligned(q, 16)) return fail(CNN_ERR_UNSUPPORTED, "%s: 4-bit values not 16-byte aligned", what);
+    return CNN_OK;
+}
+
+int check_grouped(const char* what, const GroupedFc& p) {
+    if (p.N < 0 || p.M < 0 || p.I <= 0 || p.O <= 0 || p.G <= 0)
+        return fail(CNN_ERR_INVALID, "%s: N=%d I=%d M=%d groups=%d O=%d", what, p.N, p.I, p.M, p.G, p.O);
+    if (p.x_type != CNN_MX4 && !wide(p.x_type)) return fail(CNN_ERR_INVALID, "%s: input type %d", what, p.x_type);
+    if (p.w_type != CNN_MX4 && p.w_type != p.x_type)
+        return fail(CNN_ERR_INVALID, "%s: weights of type %d for inputs of type %d", what, p.w_type, p.x_type);
+    if (!wide(p.y_type) || (p.x_type != CNN_MX4 && p.y_type != p.x_type))
+        return fail(CNN_ERR_INVALID, "%s: output type %d for inputs of type %d", what, p.y_type, p.x_type);
+    if ((p.x_type == CNN_MX4) != (p.xs != nullptr) || (p.w_type == CNN_MX4) != (p.ws != nullptr))
+        return fail(CNN_ERR_INVALID, "%s: scales go with 4-bit values, and with those only", what);
+    if (!p.w || (p.M != 0 && (!p.x || !p.y))) return fail(CNN_ERR_INVALID, "%s: null x, w or y", what);
+    if (!p.rows && p.N != p.M) return fail(CNN_ERR_INVALID, "%s: %d rows of y from %d of x", what, p.M, p.N);
+    if (p.M != 0 && p.N == 0) return fail(CNN_ERR_INVALID, "%s: %d rows of y from no row of x", what, p.M);
+    if (too_big(p.N, p.I) || too_big(p.M, p.O) || too_big(p.O, p.I))
+        return fail(CNN_ERR_UNSUPPORTED, "%s: x, y or a weight matrix exceeds 2^31-1 elements", what);
+    if (p.G > (1 << 20)) return fail(CNN_ERR_UNSUPPORTED, "%s: %d groups", what, p.G);
+    if (p.x_type == CNN_MX4 ? !aligned(p.x, 16) : !aligned(p.x, type_bytes(p.x_type)))
+        return fail(CNN_ERR_UNSUPPORTED, "%s: x not aligned", what);
+    if (p.w_type == CNN_MX4 ? !aligned(p.w, 16) : !aligned(p.w, type_bytes(p.w_type)))
+        return fail(CNN_ERR_UNSUPPORTED, "%s: w not aligned", what);
+    if (!aligned(p.y, type_bytes(p.y_type)) || !aligned(p.bias, 4) || !aligned(p.rows, 4) || !aligned(p.offsets, 4))
+        return fail(CNN_ERR_UNSUPPORTED, "%s: y, bias, rows or offsets not aligned to their type", what);
+    return CNN_OK;
+}
+
+constexpr int kMaxExperts = 1024, kMaxChoices = 64;
+
+int check_route(int type, int T, int E, int k) {
+    if (!wide(type)) return fail(CNN_ERR_INVALID, "route: type %d is not fp32, bf16 or fp16", type);
+    if (T < 0 || E <= 0 || k <= 0 || k > E) return fail(CNN_ERR_INVALID, "route: T=%d E=%d k=%d", T, E, k);
+    if (E > kMaxExperts || k > kMaxChoices)
+        return fail(CNN_ERR_UNSUPPORTED, "route: %d experts, %d choices: at most %d and %d", E, k, kMaxExperts, kMaxChoices);
+    if (too_big(T, E) || T > (1 << 27)) return fail(CNN_ERR_UNSUPPORTED, "route: %d tokens", T);
     return CNN_OK;
 }
 
@@ -665,6 +719,73 @@ int cnn_softmax_fwd(const float* x, int N, int C, int HW, float* y, cnn_stream_t
             return fail(CNN_ERR_INVALID, "softmax: x and y overlap without being equal");
     }
     return launch_softmax(x, N, C, HW, y, as_stream(stream));
+}
+
+int cnn_mx4_quantize(const void* x, int x_type, int rows, int cols, uint8_t* q, uint8_t* scale, cnn_stream_t stream) {
+    int rc = check_mx4("mx4_quantize", x, x_type, rows, cols, q, scale);
+    if (rc) return rc;
+    return launch_mx4_quantize(x, x_type, rows, cols, q, scale, as_stream(stream));
+}
+
+int cnn_mx4_dequantize(const uint8_t* q, const uint8_t* scale, int rows, int cols, void* y, int y_type,
+                       cnn_stream_t stream) {
+    int rc = check_mx4("mx4_dequantize", y, y_type, rows, cols, q, scale);
+    if (rc) return rc;
+    return launch_mx4_dequantize(q, scale, rows, cols, y, y_type, as_stream(stream));
+}
+
+int cnn_fc_mx4_fwd(const void* x, const uint8_t* x_scale, int x_type, int N, int I, const uint8_t* w,
+                   const uint8_t* w_scale, const float* bias, int O, int fuse_relu, void* y, int y_type,
+                   cnn_stream_t stream) {
+    const GroupedFc p{x, x_scale, nullptr, nullptr, w, w_scale, bias, y, x_type, CNN_MX4, y_type, N, I, N, 1, O,
+                      fuse_relu != 0};
+    int rc = check_grouped("fc_mx4", p);
+    if (rc) return rc;
+    return launch_fc_grouped(p, as_stream(stream));
+}
+
+int cnn_fc_grouped_fwd(const void* x, const uint8_t* x_scale, int x_type, int N, int I, const int32_t* rows, int M,
+                       const int32_t* offsets, int groups, const void* w, const uint8_t* w_scale, int w_type,
+                       const float* bias, int O, int fuse_relu, void* y, int y_type, cnn_stream_t stream) {
+    if (!offsets) return fail(CNN_ERR_INVALID, "fc_grouped: null offsets");
+    const GroupedFc p{x, x_scale, rows, offsets, w, w_scale, bias, y, x_type, w_type, y_type, N, I, M, groups, O,
+                      fuse_relu != 0};
+    int rc = check_grouped("fc_grouped", p);
+    if (rc) return rc;
+    return launch_fc_grouped(p, as_stream(stream));
+}
+
+size_t cnn_route_workspace_bytes(int T, int E, int k) {
+    if (check_route(CNN_F32, T, E, k)) return 0;
+    return route_workspace(T, E);
+}
+
+int cnn_route_fwd(const void* logits, int type, int T, int E, int k, int renormalize, int32_t* expert, float* weight,
+                  int32_t* rows, int32_t* offsets, int32_t* slot, void* ws, size_t ws_bytes, cnn_stream_t stream) {
+    int rc = check_route(type, T, E, k);
+    if (rc) return rc;
+    if (!offsets || (T != 0 && (!logits || !expert || !weight || !rows || !slot)))
+        return fail(CNN_ERR_INVALID, "route: null pointer");
+    if (!aligned(logits, type_bytes(type)) || !aligned(expert, 4) || !aligned(weight, 4) || !aligned(rows, 4) ||
+        !aligned(offsets, 4) || !aligned(slot, 4) || !aligned(ws, 4))
+        return fail(CNN_ERR_UNSUPPORTED, "route: a tensor is not aligned to its type");
+    const size_t need = route_workspace(T, E);
+    if (need > 0 && (!ws || ws_bytes < need))
+        return fail(CNN_ERR_WORKSPACE, "route: workspace of %zu bytes, %zu needed", ws ? ws_bytes : 0, need);
+    return launch_route(logits, type, T, E, k, renormalize != 0, expert, weight, rows, offsets, slot,
+                        reinterpret_cast<int32_t*>(ws), as_stream(stream));
+}
+
+int cnn_combine_fwd(const void* x, int type, int M, int D, const int32_t* slot, const float* weight, int N, int k,
+                    void* y, cnn_stream_t stream) {
+    if (!wide(type)) return fail(CNN_ERR_INVALID, "combine: type %d is not fp32, bf16 or fp16", type);
+    if (M < 0 || N < 0 || D <= 0 || k <= 0) return fail(CNN_ERR_INVALID, "combine: M=%d D=%d N=%d k=%d", M, D, N, k);
+    if (too_big(M, D) || too_big(N, D) || too_big(N, k))
+        return fail(CNN_ERR_UNSUPPORTED, "combine: a tensor exceeds 2^31-1 elements");
+    if (N != 0 && ((M != 0 && !x) || !slot || !weight || !y)) return fail(CNN_ERR_INVALID, "combine: null pointer");
+    if (!aligned(x, type_bytes(type)) || !aligned(y, type_bytes(type)) || !aligned(slot, 4) || !aligned(weight, 4))
+        return fail(CNN_ERR_UNSUPPORTED, "combine: a tensor is not aligned to its type");
+    return launch_combine(x, type, M, D, slot, weight, N, k, y, as_stream(stream));
 }
 
 int cnn_net_out_shape(const cnn_layer_desc* layers, int n_layers, int N, int C, int H, int W,
