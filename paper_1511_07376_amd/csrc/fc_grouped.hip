@@ -4,8 +4,7 @@
 //     y[m][o] = b[g][o] + sum_i x[rows[m]][i] * w[g][o][i],  offsets[g] <= m < offsets[g + 1]
 //
 // Sums are held in fp32 and rounded once, to the type of y.
-#include "common.h"
-#include "wide_types.h"
+#include "fc_operands.h"
 
 #include <algorithm>
 
@@ -13,12 +12,6 @@ namespace cnn {
 namespace {
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
-
-// The rows of a group, clipped to [0, M): offsets are the caller's data.
-__device__ inline void group_rows(const int32_t* offsets, int g, int M, int& lo, int& hi) {
-    lo = min(max(offsets[g], 0), M);
-    hi = min(max(offsets[g + 1], lo), M);
-}
 
 // Tile t of the launch: tiles of TM rows, numbered through the groups.  False
 // behind the last one.  The wave looks at 64 groups at a time; the answer is
@@ -123,6 +116,7 @@ __global__ void __launch_bounds__(kTile * kTile) fc_grouped_plain(GroupedFc p, i
 
 int launch_fc_grouped(const GroupedFc& p, hipStream_t st) {
     if (p.M == 0) return CNN_OK;
+    if (ceil_div64(p.M, p.G) <= 32) return run_fc_rows(p, st);
     const int64_t row_tiles = ceil_div64(p.M, kTile) + (p.offsets ? p.G : 0);
     const int cols = ceil_div(p.O, kTile);
     const int64_t tiles = row_tiles * cols;

@@ -1,0 +1,155 @@
+// Operands of the products on groups of rows, as the matrix cores take them.
+//
+// A lane feeds the matrix cores runs of 32 consecutive values of a row (an mx4
+// block, 64 bytes of a 16-bit type, 128 of fp32).  Which k of the
+// reduction an instruction's slot stands for is free as long as both operands
+// agree, so a run is cut into the instruction's lane parts in order: 4 of 8
+// values for the 16-bit instructions, 32 single ones for the fp32 one, and
+// whole for the scaled 4-bit one.
+//
+// Wide inputs with mx4 weights: the weights' values (2 significant bits and
+// a power of two) are bfloat16 numbers, and so are the parts that a wider
+// input is cut into: its leading 8 bits, the next 8, the rest (one part for
+// bf16, two for fp16, three for fp32).  Every product is then exact in the
+// fp32 sums.
+#pragma once
+
+#include "common.h"
+#include "wide_types.h"
+
+namespace cnn {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+// Bytes of a run of 32 values, and its 16-byte loads.
+template <int T>
+constexpr int kRunBytes = T == CNN_F32 ? 128 : T == CNN_MX4 ? 16 : 64;
+template <int T>
+constexpr int kRunLoads = kRunBytes<T> / 16;
+template <int T>
+constexpr int kElemBytes = T == CNN_F32 ? 4 : 2;  // wide types
+
+// Parts that an input of type XT is cut into beside mx4 weights.
+template <int XT>
+constexpr int kParts = XT == CNN_F32 ? 3 : XT == CNN_F16 ? 2 : 1;
+
+// 32 values of a row that ends after `cols` of them, from k on; past the end
+// they are 0.  FULL: all are inside.
+template <int T, bool FULL>
+__device__ inline void load_run(const char* row, int64_t k, int cols, u32x4* run) {
+    constexpr int ES = kElemBytes<T>, PER = 16 / ES;
+#pragma unroll
+    for (int j = 0; j < kRunLoads<T>; ++j) {
+        const int64_t at = k + j * PER;
+        if (FULL || at + PER <= cols) {
+            run[j] = load16(row + at * ES);
+        } else {
+            u32x4 v = {0, 0, 0, 0};
+            if (at < cols) {
+#pragma unroll
+                for (int c = 0; c < PER; ++c) {
+                    if (at + c < cols) {
+                        if constexpr (ES == 4) {
+                            unsigned e;
+                            __builtin_memcpy(&e, row + (at + c) * 4, 4);
+                            v[c] = e;
+                        } else {
+                            uint16_t e;
+                            __builtin_memcpy(&e, row + (at + c) * 2, 2);
+                            v[c / 2] |= (unsigned)e << (16 * (c % 2));
+                        }
+                    }
+                }
+            }
+            run[j] = v;
+        }
+    }
+}
+
+// The leading bfloat16 of each of two floats, cut and not rounded (so that the
+// largest stay finite), packed; the floats become what it leaves.  Exact: a
+// float has 24 bits, its leading part takes 8 and leaves 16 or fewer.  Infinity leaves
+// 0, NaN leaves NaN.
+__device__ inline unsigned cut_pair(float& a, float& b) {
+    const unsigned ua = __float_as_uint(a), ub = __float_as_uint(b);
+    const unsigned packed = __builtin_amdgcn_perm(ub, ua, 0x07060302u);
+    const float ra = a - __uint_as_float(ua & 0xffff0000u), rb = b - __uint_as_float(ub & 0xffff0000u);
+    a = __builtin_isinf(a) ? 0.0f : ra;
+    b = __builtin_isinf(b) ? 0.0f : rb;
+    return packed;
+}
+
+// 8 values of a run (lane part j) as bfloat16 parts.
+template <int XT>
+__device__ inline void cut_parts(const u32x4* run, int j, bf16x8* part) {
+    if constexpr (XT == CNN_BF16) {
+        part[0] = __builtin_bit_cast(bf16x8, run[j]);
+    } else {
+        float v[8];
+        if constexpr (XT == CNN_F16) {
+            const f16x8 h = __builtin_bit_cast(f16x8, run[j]);
+#pragma unroll
+            for (int c = 0; c < 8; ++c) v[c] = (float)h[c];
+        } else {
+#pragma unroll
+            for (int c = 0; c < 8; ++c) v[c] = __uint_as_float(run[2 * j + c / 4][c % 4]);
+        }
+#pragma unroll
+        for (int q = 0; q < kParts<XT>; ++q) {
+            u32x4 p;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                if (q + 1 < kParts<XT>)
+                    p[c] = cut_pair(v[2 * c], v[2 * c + 1]);
+                else  // what is left has 8 bits at most (below 2^-107: is cut at 2^-133)
+                    p[c] = __builtin_amdgcn_perm(__float_as_uint(v[2 * c + 1]), __float_as_uint(v[2 * c]), 0x07060302u);
+            }
+            part[q] = __builtin_bit_cast(bf16x8, p);
+        }
+    }
+}
+
+// 8 values of an mx4 block (word j) as bfloat16.
+__device__ inline bf16x8 decode8(unsigned word, float scale) {
+    u32x4 out;
+    out[0] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 0));
+    out[1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 1));
+    out[2] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 2));
+    out[3] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 3));
+    return __builtin_bit_cast(bf16x8, out);
+}
+
+__device__ inline i32x8 mx4_operand(u32x4 v) { return i32x8{(int)v[0], (int)v[1], (int)v[2], (int)v[3], 0, 0, 0, 0}; }
+
+// The rows of a group, clipped to [0, M): offsets are the caller's data.
+__device__ inline void group_rows(const int32_t* offsets, int g, int M, int& lo, int& hi) {
+    lo = min(max(offsets[g], 0), M);
+    hi = min(max(offsets[g + 1], lo), M);
+}
+
+// The row of x that row m of y is made of; < 0 where there is none.
+__device__ inline int source_row(const GroupedFc& p, int m) {
+    const int r = p.rows ? p.rows[m] : m;
+    return r < p.N ? r : -1;
+}
+
+template <int YT>
+__device__ inline void store_result(void* y, size_t i, float v) {
+    if constexpr (YT == CNN_F32) ((float*)y)[i] = v;
+    else if constexpr (YT == CNN_BF16) ((bf16_t*)y)[i] = from_f32<bf16_t>(v);
+    else ((f16_t*)y)[i] = from_f32<f16_t>(v);
+}
+__device__ inline void store_result(int type, void* y, size_t i, float v) {
+    if (type == CNN_F32) store_result<CNN_F32>(y, i, v);
+    else if (type == CNN_BF16) store_result<CNN_BF16>(y, i, v);
+    else store_result<CNN_F16>(y, i, v);
+}
+
+int run_fc_rows(const GroupedFc& p, hipStream_t st);
+
+}  // namespace cnn
