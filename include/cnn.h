@@ -235,7 +235,14 @@ int cnn_mx4_dequantize(const uint8_t* q, const uint8_t* scale, int rows, int col
  * call. */
 int cnn_fc_mx4_fwd(const void* x, const uint8_t* x_scale, int x_type, int N, int I,
                    const uint8_t* w, const uint8_t* w_scale, const float* bias, int O,
-                   int fuse_relu, void* y, int y_type, cnn_stream_t stream);
+                   int fuse_relu, void* y, int y_type, void* ws, size_t ws_bytes,
+                   cnn_stream_t stream);
+
+/* Device workspace of cnn_fc_mx4_fwd for these types and sizes: the partial
+ * sums of a reduction that is split over workgroups (some tens of rows);
+ * often 0, and then ws may be NULL.  0 on error.  Calls that overlap need
+ * workspaces of their own. */
+size_t cnn_fc_mx4_workspace_bytes(int x_type, int N, int I, int O);
 
 /* Fully-connected layers of groups of rows, each with weights of its own:
  *   y[m,o] = b[g,o] + sum_i x[rows[m],i] * w[g,o,i]   for offsets[g] <= m < offsets[g+1]
@@ -253,7 +260,11 @@ int cnn_fc_grouped_fwd(const void* x, const uint8_t* x_scale, int x_type, int N,
                        const int32_t* rows, int M, const int32_t* offsets, int groups,
                        const void* w, const uint8_t* w_scale, int w_type,
                        const float* bias, int O, int fuse_relu,
-                       void* y, int y_type, cnn_stream_t stream);
+                       void* y, int y_type, void* ws, size_t ws_bytes,
+                       cnn_stream_t stream);
+
+/* Device workspace of cnn_fc_grouped_fwd, as cnn_fc_mx4_workspace_bytes. */
+size_t cnn_fc_grouped_workspace_bytes(int x_type, int I, int M, int groups, int w_type, int O);
 
 /* Device workspace of cnn_route_fwd (0 up to 64 tokens, and on error). */
 size_t cnn_route_workspace_bytes(int T, int E, int k);

@@ -65,8 +65,13 @@ lib.cnn_relu_fwd.argtypes = [_p, _p, ctypes.c_int64, _p]
 lib.cnn_softmax_fwd.argtypes = [_p, _i, _i, _i, _p, _p]
 lib.cnn_mx4_quantize.argtypes = [_p, _i, _i, _i, _p, _p, _p]
 lib.cnn_mx4_dequantize.argtypes = [_p, _p, _i, _i, _p, _i, _p]
-lib.cnn_fc_mx4_fwd.argtypes = [_p, _p, _i, _i, _i, _p, _p, _p, _i, _i, _p, _i, _p]
-lib.cnn_fc_grouped_fwd.argtypes = [_p, _p, _i, _i, _i, _p, _i, _p, _i, _p, _p, _i, _p, _i, _i, _p, _i, _p]
+lib.cnn_fc_mx4_fwd.argtypes = [_p, _p, _i, _i, _i, _p, _p, _p, _i, _i, _p, _i, _p, ctypes.c_size_t, _p]
+lib.cnn_fc_mx4_workspace_bytes.argtypes = [_i] * 4
+lib.cnn_fc_mx4_workspace_bytes.restype = ctypes.c_size_t
+lib.cnn_fc_grouped_fwd.argtypes = [_p, _p, _i, _i, _i, _p, _i, _p, _i, _p, _p, _i, _p, _i, _i, _p, _i, _p,
+                                   ctypes.c_size_t, _p]
+lib.cnn_fc_grouped_workspace_bytes.argtypes = [_i] * 6
+lib.cnn_fc_grouped_workspace_bytes.restype = ctypes.c_size_t
 lib.cnn_route_workspace_bytes.argtypes = [_i, _i, _i]
 lib.cnn_route_workspace_bytes.restype = ctypes.c_size_t
 lib.cnn_route_fwd.argtypes = [_p, _i, _i, _i, _i, _i, _p, _p, _p, _p, _p, _p, ctypes.c_size_t, _p]
@@ -128,6 +133,7 @@ for _name in ("cnn_conv2d_out_shape", "cnn_pool_out_shape", "cnn_conv2d_fwd", "c
 EXPORTED = ("cnn_conv2d_out_shape", "cnn_pool_out_shape", "cnn_conv2d_fwd", "cnn_fc_fwd",
             "cnn_pool_fwd", "cnn_lrn_fwd", "cnn_relu_fwd", "cnn_softmax_fwd", "cnn_net_out_shape",
             "cnn_mx4_quantize", "cnn_mx4_dequantize", "cnn_fc_mx4_fwd", "cnn_fc_grouped_fwd",
+            "cnn_fc_mx4_workspace_bytes", "cnn_fc_grouped_workspace_bytes",
             "cnn_route_workspace_bytes", "cnn_route_fwd", "cnn_combine_fwd",
             "cnn_net_workspace_bytes", "cnn_net_fwd", "cnn_net_fwd_timed", "cnn_net_fwd_kernel_timed",
             "cnn_net_fwd_dump",
@@ -479,8 +485,11 @@ def cnn_fc_mx4_fwd(x, w, w_scale, bias=None, fuse_relu=False, x_scale=None, y_dt
     with _Launch(device, stream) as st:
         if y is None:
             y = torch.empty((N, O), dtype=dtype, device=device)
+        need = lib.cnn_fc_mx4_workspace_bytes(xt, N, cols, O)
+        work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
         _ok(lib.cnn_fc_mx4_fwd(xp, xs, xt, N, cols, wp, ws, bp, O, 1 if fuse_relu else 0,
-                               _on(y, "y", device, dtype, (N, O)), _WIDE.get(dtype, -1), st))
+                               _on(y, "y", device, dtype, (N, O)), _WIDE.get(dtype, -1),
+                               work.data_ptr() if need else None, need, st))
     return y
 
 
@@ -506,8 +515,11 @@ def cnn_fc_grouped_fwd(x, w, offsets, bias=None, fuse_relu=False, rows=None, w_s
     with _Launch(device, stream) as st:
         if y is None:
             y = torch.empty((M, O), dtype=dtype, device=device)
+        need = lib.cnn_fc_grouped_workspace_bytes(xt, cols, M, G, wt, O)
+        work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
         _ok(lib.cnn_fc_grouped_fwd(xp, xs, xt, N, cols, rp, M, op, G, wp, ws, wt, bp, O, 1 if fuse_relu else 0,
-                                   _on(y, "y", device, dtype, (M, O)), _WIDE.get(dtype, -1), st))
+                                   _on(y, "y", device, dtype, (M, O)), _WIDE.get(dtype, -1),
+                                   work.data_ptr() if need else None, need, st))
     return y
 
 

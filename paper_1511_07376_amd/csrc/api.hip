@@ -734,25 +734,59 @@ int cnn_mx4_dequantize(const uint8_t* q, const uint8_t* scale, int rows, int col
     return launch_mx4_dequantize(q, scale, rows, cols, y, y_type, as_stream(stream));
 }
 
+namespace {
+int run_grouped(const char* what, const GroupedFc& p, void* ws, size_t ws_bytes, cnn_stream_t stream) {
+    int rc = check_grouped(what, p);
+    if (rc) return rc;
+    const size_t need = fc_grouped_workspace(p);
+    if (need > 0 && (!ws || ws_bytes < need))
+        return fail(CNN_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", what, ws ? ws_bytes : 0, need);
+    if (!aligned(ws, 4)) return fail(CNN_ERR_UNSUPPORTED, "%s: workspace not aligned", what);
+    return launch_fc_grouped(p, reinterpret_cast<float*>(ws), as_stream(stream));
+}
+
+// What the workspace depends on: sizes and types.  0 for what the call refuses.
+size_t grouped_workspace(int x_type, int I, int M, bool grouped, int groups, int w_type, int O) {
+    if (M <= 0 || I <= 0 || O <= 0 || groups <= 0 || (x_type != CNN_MX4 && !wide(x_type)) ||
+        (w_type != CNN_MX4 && w_type != x_type) || too_big(M, O) || too_big(O, I))
+        return 0;
+    const int32_t some = 0;
+    GroupedFc p{};
+    p.offsets = grouped ? &some : nullptr;  // not read
+    p.x_type = x_type;
+    p.w_type = w_type;
+    p.N = p.M = M;
+    p.I = I;
+    p.G = groups;
+    p.O = O;
+    return fc_grouped_workspace(p);
+}
+}  // namespace
+
+size_t cnn_fc_mx4_workspace_bytes(int x_type, int N, int I, int O) {
+    return grouped_workspace(x_type, I, N, false, 1, CNN_MX4, O);
+}
+
 int cnn_fc_mx4_fwd(const void* x, const uint8_t* x_scale, int x_type, int N, int I, const uint8_t* w,
-                   const uint8_t* w_scale, const float* bias, int O, int fuse_relu, void* y, int y_type,
-                   cnn_stream_t stream) {
+                   const uint8_t* w_scale, const float* bias, int O, int fuse_relu, void* y, int y_type, void* ws,
+                   size_t ws_bytes, cnn_stream_t stream) {
     const GroupedFc p{x, x_scale, nullptr, nullptr, w, w_scale, bias, y, x_type, CNN_MX4, y_type, N, I, N, 1, O,
                       fuse_relu != 0};
-    int rc = check_grouped("fc_mx4", p);
-    if (rc) return rc;
-    return launch_fc_grouped(p, as_stream(stream));
+    return run_grouped("fc_mx4", p, ws, ws_bytes, stream);
+}
+
+size_t cnn_fc_grouped_workspace_bytes(int x_type, int I, int M, int groups, int w_type, int O) {
+    return grouped_workspace(x_type, I, M, true, groups, w_type, O);
 }
 
 int cnn_fc_grouped_fwd(const void* x, const uint8_t* x_scale, int x_type, int N, int I, const int32_t* rows, int M,
                        const int32_t* offsets, int groups, const void* w, const uint8_t* w_scale, int w_type,
-                       const float* bias, int O, int fuse_relu, void* y, int y_type, cnn_stream_t stream) {
+                       const float* bias, int O, int fuse_relu, void* y, int y_type, void* ws, size_t ws_bytes,
+                       cnn_stream_t stream) {
     if (!offsets) return fail(CNN_ERR_INVALID, "fc_grouped: null offsets");
     const GroupedFc p{x, x_scale, rows, offsets, w, w_scale, bias, y, x_type, w_type, y_type, N, I, M, groups, O,
                       fuse_relu != 0};
-    int rc = check_grouped("fc_grouped", p);
-    if (rc) return rc;
-    return launch_fc_grouped(p, as_stream(stream));
+    return run_grouped("fc_grouped", p, ws, ws_bytes, stream);
 }
 
 size_t cnn_route_workspace_bytes(int T, int E, int k) {

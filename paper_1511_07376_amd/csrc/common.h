@@ -223,7 +223,9 @@ struct GroupedFc {
     int x_type, w_type, y_type;
     int N, I, M, G, O, relu;
 };
-int launch_fc_grouped(const GroupedFc& p, hipStream_t st);
+// Split reductions leave their sums in the workspace.
+size_t fc_grouped_workspace(const GroupedFc& p);
+int launch_fc_grouped(const GroupedFc& p, float* ws, hipStream_t st);
 size_t route_workspace(int T, int E);
 int launch_route(const void* logits, int type, int T, int E, int k, int renorm, int32_t* expert, float* weight,
                  int32_t* rows, int32_t* offsets, int32_t* slot, int32_t* counts, hipStream_t st);

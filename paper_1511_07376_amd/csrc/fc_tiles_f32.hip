@@ -1,0 +1,10 @@
+// Instantiations of fc_tiles (fp32 inputs and weights).
+#include "fc_tiles_kernel.h"
+
+namespace cnn {
+
+void run_tiles_f32(const GroupedFc& p, const TilePlan& plan, bool vec, float* partial, hipStream_t st) {
+    run_tiles<CNN_F32, CNN_F32>(p, plan, vec, partial, st);
+}
+
+}  // namespace cnn

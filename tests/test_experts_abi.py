@@ -38,7 +38,7 @@ def test_mx4_conversions_refuse(args, status):
 
 
 def _fc(**kw):
-    a = dict(x=FAKE, xs=0, xt=BF16, N=4, I=64, w=FAKE, ws=FAKE, bias=0, O=8, relu=0, y=FAKE, yt=BF16, st=0)
+    a = dict(x=FAKE, xs=0, xt=BF16, N=4, I=64, w=FAKE, ws=FAKE, bias=0, O=8, relu=0, y=FAKE, yt=BF16, work=0, n=0, st=0)
     a.update(kw)
     return L.cnn_fc_mx4_fwd(*a.values())
 
@@ -62,7 +62,7 @@ def test_fc_mx4_refuses(kw, status):
 
 def _grouped(**kw):
     a = dict(x=FAKE, xs=0, xt=BF16, N=4, I=64, rows=FAKE, M=6, offsets=FAKE, G=3, w=FAKE, ws=0, wt=BF16, bias=0, O=8,
-             relu=0, y=FAKE, yt=BF16, st=0)
+             relu=0, y=FAKE, yt=BF16, work=0, n=0, st=0)
     a.update(kw)
     return L.cnn_fc_grouped_fwd(*a.values())
 
