@@ -10,6 +10,7 @@ this module fails if libcnn.so has not been built.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from dataclasses import dataclass
@@ -372,37 +373,29 @@ def _gpu(t, name: str) -> torch.device:
     return t.device
 
 
-class _Launch:
-    """The device and the stream that a call's kernels go to, and its outputs are allocated for: those of its
-    tensors' GPU, current or not, and the stream it was given, else the current one of that GPU."""
+_raw_stream = torch._C._cuda_getCurrentRawStream  # a tenth of torch.cuda.current_stream()'s time
 
-    __slots__ = ("handle", "_guards")
 
-    def __init__(self, device, stream):
-        self._guards = ()
-        if stream is None and device.index == torch.cuda.current_device():
-            self.handle = torch.cuda.current_stream().cuda_stream
+def _elsewhere(device, stream) -> bool:
+    """Whether a call's kernels go to another device or stream than the current ones."""
+    return stream is not None or device.index != torch.cuda.current_device()
+
+
+@contextlib.contextmanager
+def _there(device, stream):
+    """Makes the tensors' GPU and the call's stream current, for its kernels and the tensors it allocates."""
+    with torch.cuda.device(device):
+        if stream is None:
+            yield
             return
-        guards = [torch.cuda.device(device)]
-        if stream is not None:
-            if not isinstance(stream, torch.cuda.Stream):
-                handle = int(stream)
-                stream = (torch.cuda.ExternalStream(handle, device=device) if handle
-                          else torch.cuda.default_stream(device))
-            if stream.device != device:
-                raise ValueError(f"the stream is of {stream.device}, the tensors are on {device}")
-            guards.append(torch.cuda.stream(stream))
-        for g in guards:
-            g.__enter__()
-        self._guards = guards
-        self.handle = torch.cuda.current_stream().cuda_stream
-
-    def __enter__(self):
-        return self.handle
-
-    def __exit__(self, *exc):
-        for g in reversed(self._guards):
-            g.__exit__(*exc)
+        if not isinstance(stream, torch.cuda.Stream):
+            handle = int(stream)
+            stream = (torch.cuda.ExternalStream(handle, device=device) if handle
+                      else torch.cuda.default_stream(device))
+        if stream.device != device:
+            raise ValueError(f"the stream is of {stream.device}, the tensors are on {device}")
+        with torch.cuda.stream(stream):
+            yield
 
 
 def cnn_mx4_quantize(x, q=None, scale=None, stream=None):
@@ -410,6 +403,9 @@ def cnn_mx4_quantize(x, q=None, scale=None, stream=None):
 
     Leading dimensions are kept: x [G][O][I] gives q [G][O][...]."""
     device = _gpu(x, "x")
+    if _elsewhere(device, stream):
+        with _there(device, stream):
+            return cnn_mx4_quantize(x, q, scale)
     if x.dim() < 2:
         raise ValueError("mx4_quantize: x must be [rows][cols]")
     lead, cols = tuple(x.shape[:-1]), x.shape[-1]
@@ -419,19 +415,28 @@ def cnn_mx4_quantize(x, q=None, scale=None, stream=None):
     blocks = (cols + 31) // 32
     code = _wide(x.dtype, "x")
     xp = _on(x, "x", device)
-    with _Launch(device, stream) as st:
-        if q is None:
-            q = torch.empty(lead + (blocks * 16,), dtype=torch.uint8, device=device)
-        if scale is None:
-            scale = torch.empty(lead + (blocks,), dtype=torch.uint8, device=device)
-        _ok(lib.cnn_mx4_quantize(xp, code, rows, cols, _on(q, "q", device, torch.uint8, lead + (blocks * 16,)),
-                                 _on(scale, "scale", device, torch.uint8, lead + (blocks,)), st))
+    st = _raw_stream(device.index)
+    if q is None:
+        q = torch.empty(lead + (blocks * 16,), dtype=torch.uint8, device=device)
+        qp = q.data_ptr()
+    else:
+        qp = _on(q, "q", device, torch.uint8, lead + (blocks * 16,))
+    if scale is None:
+        scale = torch.empty(lead + (blocks,), dtype=torch.uint8, device=device)
+        scalep = scale.data_ptr()
+    else:
+        scalep = _on(scale, "scale", device, torch.uint8, lead + (blocks,))
+    _ok(lib.cnn_mx4_quantize(xp, code, rows, cols, qp,
+                             scalep, st))
     return q, scale
 
 
 def cnn_mx4_dequantize(q, scale, cols=None, dtype=torch.float32, y=None, stream=None):
     """The values of mx4 rows, [...][cols] (cols: 32 a block if not given)."""
     device = _gpu(q, "q")
+    if _elsewhere(device, stream):
+        with _there(device, stream):
+            return cnn_mx4_dequantize(q, scale, cols, dtype, y)
     blocks = scale.shape[-1]
     cols = 32 * blocks if cols is None else int(cols)
     if not 32 * (blocks - 1) < cols <= 32 * blocks:
@@ -442,11 +447,14 @@ def cnn_mx4_dequantize(q, scale, cols=None, dtype=torch.float32, y=None, stream=
         rows *= d
     qp = _on(q, "q", device, torch.uint8, lead + (blocks * 16,))
     sp = _on(scale, "scale", device, torch.uint8)
-    with _Launch(device, stream) as st:
-        if y is None:
-            y = torch.empty(lead + (cols,), dtype=dtype, device=device)
-        _ok(lib.cnn_mx4_dequantize(qp, sp, rows, cols, _on(y, "y", device, None, lead + (cols,)),
-                                   _wide(y.dtype, "y"), st))
+    st = _raw_stream(device.index)
+    if y is None:
+        y = torch.empty(lead + (cols,), dtype=dtype, device=device)
+        yp = y.data_ptr()
+    else:
+        yp = _on(y, "y", device, None, lead + (cols,))
+    _ok(lib.cnn_mx4_dequantize(qp, sp, rows, cols, yp,
+                               _wide(y.dtype, "y"), st))
     return y
 
 
@@ -472,6 +480,9 @@ def cnn_fc_mx4_fwd(x, w, w_scale, bias=None, fuse_relu=False, x_scale=None, y_dt
 
     With x_scale x is mx4 too, and y of type y_dtype (float32 if not given)."""
     device = _gpu(x, "x")
+    if _elsewhere(device, stream):
+        with _there(device, stream):
+            return cnn_fc_mx4_fwd(x, w, w_scale, bias, fuse_relu, x_scale, y_dtype, y)
     if x_scale is None and x.dim() > 2:
         x = x.reshape(x.shape[0], -1) if x.is_contiguous() else x
     if x.dim() != 2 or w.dim() != 2 or w_scale.dim() != 2:
@@ -482,14 +493,17 @@ def cnn_fc_mx4_fwd(x, w, w_scale, bias=None, fuse_relu=False, x_scale=None, y_dt
     N, O = x.shape[0], w.shape[0]
     bp = _on(bias, "bias", device, torch.float32, (O,))
     dtype = x.dtype if xs is None else y_dtype or torch.float32
-    with _Launch(device, stream) as st:
-        if y is None:
-            y = torch.empty((N, O), dtype=dtype, device=device)
-        need = lib.cnn_fc_mx4_workspace_bytes(xt, N, cols, O)
-        work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
-        _ok(lib.cnn_fc_mx4_fwd(xp, xs, xt, N, cols, wp, ws, bp, O, 1 if fuse_relu else 0,
-                               _on(y, "y", device, dtype, (N, O)), _WIDE.get(dtype, -1),
-                               work.data_ptr() if need else None, need, st))
+    st = _raw_stream(device.index)
+    if y is None:
+        y = torch.empty((N, O), dtype=dtype, device=device)
+        yp = y.data_ptr()
+    else:
+        yp = _on(y, "y", device, dtype, (N, O))
+    need = lib.cnn_fc_mx4_workspace_bytes(xt, N, cols, O)
+    work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    _ok(lib.cnn_fc_mx4_fwd(xp, xs, xt, N, cols, wp, ws, bp, O, 1 if fuse_relu else 0,
+                           yp, _WIDE.get(dtype, -1),
+                           work.data_ptr() if need else None, need, st))
     return y
 
 
@@ -501,6 +515,9 @@ def cnn_fc_grouped_fwd(x, w, offsets, bias=None, fuse_relu=False, rows=None, w_s
     With w_scale [G][O][blocks] w is mx4; with x_scale x is too, and y of type y_dtype (float32 if not given).
     Rows of y in no group are not written."""
     device = _gpu(x, "x")
+    if _elsewhere(device, stream):
+        with _there(device, stream):
+            return cnn_fc_grouped_fwd(x, w, offsets, bias, fuse_relu, rows, w_scale, x_scale, y_dtype, y)
     if x.dim() != 2 or w.dim() != 3:
         raise ValueError("fc_grouped: x must be [N][I], w [G][O][I]")
     xp, xs, xt, xc = _operand(x, x_scale, device, "x")
@@ -512,14 +529,17 @@ def cnn_fc_grouped_fwd(x, w, offsets, bias=None, fuse_relu=False, rows=None, w_s
     op = _on(offsets, "offsets", device, torch.int32, (G + 1,))
     rp = _on(rows, "rows", device, torch.int32)
     dtype = x.dtype if xs is None else y_dtype or torch.float32
-    with _Launch(device, stream) as st:
-        if y is None:
-            y = torch.empty((M, O), dtype=dtype, device=device)
-        need = lib.cnn_fc_grouped_workspace_bytes(xt, cols, M, G, wt, O)
-        work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
-        _ok(lib.cnn_fc_grouped_fwd(xp, xs, xt, N, cols, rp, M, op, G, wp, ws, wt, bp, O, 1 if fuse_relu else 0,
-                                   _on(y, "y", device, dtype, (M, O)), _WIDE.get(dtype, -1),
-                                   work.data_ptr() if need else None, need, st))
+    st = _raw_stream(device.index)
+    if y is None:
+        y = torch.empty((M, O), dtype=dtype, device=device)
+        yp = y.data_ptr()
+    else:
+        yp = _on(y, "y", device, dtype, (M, O))
+    need = lib.cnn_fc_grouped_workspace_bytes(xt, cols, M, G, wt, O)
+    work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    _ok(lib.cnn_fc_grouped_fwd(xp, xs, xt, N, cols, rp, M, op, G, wp, ws, wt, bp, O, 1 if fuse_relu else 0,
+                               yp, _WIDE.get(dtype, -1),
+                               work.data_ptr() if need else None, need, st))
     return y
 
 
@@ -527,6 +547,9 @@ def cnn_route_fwd(logits, k, renormalize=False, stream=None):
     """logits [T][E] -> (expert int32 [T][k], weight float32 [T][k], rows int32 [T*k], offsets int32 [E+1],
     slot int32 [T][k]): each token's k experts and their weights, and the rows for cnn_fc_grouped_fwd."""
     device = _gpu(logits, "logits")
+    if _elsewhere(device, stream):
+        with _there(device, stream):
+            return cnn_route_fwd(logits, k, renormalize)
     if logits.dim() != 2:
         raise ValueError("route: logits must be [T][E]")
     T, E = logits.shape
@@ -534,23 +557,26 @@ def cnn_route_fwd(logits, k, renormalize=False, stream=None):
     code = _wide(logits.dtype, "logits")
     lp = _on(logits, "logits", device)
     need = lib.cnn_route_workspace_bytes(T, E, k)
-    with _Launch(device, stream) as st:
-        n = max(T * k, 0)
-        expert = torch.empty((T, max(k, 0)), dtype=torch.int32, device=device)
-        weight = torch.empty((T, max(k, 0)), dtype=torch.float32, device=device)
-        slot = torch.empty((T, max(k, 0)), dtype=torch.int32, device=device)
-        rows = torch.empty(n, dtype=torch.int32, device=device)
-        offsets = torch.empty(E + 1, dtype=torch.int32, device=device)
-        ws = torch.empty(need, dtype=torch.uint8, device=device) if need else None
-        _ok(lib.cnn_route_fwd(lp, code, T, E, k, 1 if renormalize else 0, expert.data_ptr(), weight.data_ptr(),
-                              rows.data_ptr(), offsets.data_ptr(), slot.data_ptr(),
-                              ws.data_ptr() if need else None, need, st))
+    st = _raw_stream(device.index)
+    n = max(T * k, 0)
+    expert = torch.empty((T, max(k, 0)), dtype=torch.int32, device=device)
+    weight = torch.empty((T, max(k, 0)), dtype=torch.float32, device=device)
+    slot = torch.empty((T, max(k, 0)), dtype=torch.int32, device=device)
+    rows = torch.empty(n, dtype=torch.int32, device=device)
+    offsets = torch.empty(E + 1, dtype=torch.int32, device=device)
+    ws = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    _ok(lib.cnn_route_fwd(lp, code, T, E, k, 1 if renormalize else 0, expert.data_ptr(), weight.data_ptr(),
+                          rows.data_ptr(), offsets.data_ptr(), slot.data_ptr(),
+                          ws.data_ptr() if need else None, need, st))
     return expert, weight, rows, offsets, slot
 
 
 def cnn_combine_fwd(x, slot, weight, y=None, stream=None):
     """x [M][D], slot int32 [N][k], weight float32 [N][k] -> y [N][D] = sum over j of weight[n][j] * x[slot[n][j]]."""
     device = _gpu(x, "x")
+    if _elsewhere(device, stream):
+        with _there(device, stream):
+            return cnn_combine_fwd(x, slot, weight, y)
     if x.dim() != 2 or slot.dim() != 2:
         raise ValueError("combine: x must be [M][D], slot [N][k]")
     (M, D), (N, k) = x.shape, slot.shape
@@ -558,10 +584,13 @@ def cnn_combine_fwd(x, slot, weight, y=None, stream=None):
     xp = _on(x, "x", device)
     sp = _on(slot, "slot", device, torch.int32)
     wp = _on(weight, "weight", device, torch.float32, (N, k))
-    with _Launch(device, stream) as st:
-        if y is None:
-            y = torch.empty((N, D), dtype=x.dtype, device=device)
-        _ok(lib.cnn_combine_fwd(xp, code, M, D, sp, wp, N, k, _on(y, "y", device, x.dtype, (N, D)), st))
+    st = _raw_stream(device.index)
+    if y is None:
+        y = torch.empty((N, D), dtype=x.dtype, device=device)
+        yp = y.data_ptr()
+    else:
+        yp = _on(y, "y", device, x.dtype, (N, D))
+    _ok(lib.cnn_combine_fwd(xp, code, M, D, sp, wp, N, k, yp, st))
     return y
 
 

@@ -17,6 +17,8 @@
 #include "common.h"
 #include "wide_types.h"
 
+#include <cmath>
+
 namespace cnn {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -38,79 +40,93 @@ constexpr int kElemBytes = T == CNN_F32 ? 4 : 2;  // wide types
 template <int XT>
 constexpr int kParts = XT == CNN_F32 ? 3 : XT == CNN_F16 ? 2 : 1;
 
+// `count` values (0 or fewer: none) from p on in 16-byte vectors, zeros behind them.
+template <int T, int LOADS>
+__device__ inline void load_edge(const char* p, int count, u32x4* v) {
+    constexpr int ES = kElemBytes<T>;
+#pragma unroll
+    for (int h = 0; h < LOADS; ++h) {
+        u32x4 u = {0, 0, 0, 0};
+#pragma unroll
+        for (int c = 0; c < 16 / ES; ++c) {
+            const int at = h * (16 / ES) + c;
+            if (at < count) {
+                if constexpr (ES == 4) {
+                    unsigned e;
+                    __builtin_memcpy(&e, p + at * 4, 4);
+                    u[c] = e;
+                } else {
+                    uint16_t e;
+                    __builtin_memcpy(&e, p + at * 2, 2);
+                    u[c / 2] |= (unsigned)e << (16 * (c % 2));
+                }
+            }
+        }
+        v[h] = u;
+    }
+}
+
 // 32 values of a row that ends after `cols` of them, from k on; past the end
 // they are 0.  FULL: all are inside.
 template <int T, bool FULL>
 __device__ inline void load_run(const char* row, int64_t k, int cols, u32x4* run) {
-    constexpr int ES = kElemBytes<T>, PER = 16 / ES;
+    constexpr int ES = kElemBytes<T>;
+    if (FULL || k + 32 <= cols) {
 #pragma unroll
-    for (int j = 0; j < kRunLoads<T>; ++j) {
-        const int64_t at = k + j * PER;
-        if (FULL || at + PER <= cols) {
-            run[j] = load16(row + at * ES);
-        } else {
-            u32x4 v = {0, 0, 0, 0};
-            if (at < cols) {
-#pragma unroll
-                for (int c = 0; c < PER; ++c) {
-                    if (at + c < cols) {
-                        if constexpr (ES == 4) {
-                            unsigned e;
-                            __builtin_memcpy(&e, row + (at + c) * 4, 4);
-                            v[c] = e;
-                        } else {
-                            uint16_t e;
-                            __builtin_memcpy(&e, row + (at + c) * 2, 2);
-                            v[c / 2] |= (unsigned)e << (16 * (c % 2));
-                        }
-                    }
-                }
-            }
-            run[j] = v;
-        }
+        for (int j = 0; j < kRunLoads<T>; ++j) run[j] = load16(row + k * ES + j * 16);
+    } else {
+        load_edge<T, kRunLoads<T>>(row + k * ES, (int)max((int64_t)cols - k, (int64_t)0), run);
     }
 }
 
 // The leading bfloat16 of each of two floats, cut and not rounded (so that the
 // largest stay finite), packed; the floats become what it leaves.  Exact: a
-// float has 24 bits, its leading part takes 8 and leaves 16 or fewer.  Infinity leaves
-// 0, NaN leaves NaN.
+// float has 24 bits, its leading part takes 8 and leaves 16 or fewer.  NaN
+// leaves NaN.  Infinity leaves NaN too, and 0 with SAFE, which costs four
+// more instructions.
+template <bool SAFE>
 __device__ inline unsigned cut_pair(float& a, float& b) {
     const unsigned ua = __float_as_uint(a), ub = __float_as_uint(b);
     const unsigned packed = __builtin_amdgcn_perm(ub, ua, 0x07060302u);
     const float ra = a - __uint_as_float(ua & 0xffff0000u), rb = b - __uint_as_float(ub & 0xffff0000u);
-    a = __builtin_isinf(a) ? 0.0f : ra;
-    b = __builtin_isinf(b) ? 0.0f : rb;
+    a = SAFE && __builtin_isinf(a) ? 0.0f : ra;
+    b = SAFE && __builtin_isinf(b) ? 0.0f : rb;
     return packed;
 }
 
-// 8 values of a run (lane part j) as bfloat16 parts.
+template <int PARTS, bool SAFE>
+__device__ inline void cut8(float* v, u32x4* part) {
+#pragma unroll
+    for (int q = 0; q < PARTS; ++q)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            if (q + 1 < PARTS)
+                part[q][c] = cut_pair<SAFE>(v[2 * c], v[2 * c + 1]);
+            else  // what is left has 8 bits at most (below 2^-107: is cut at 2^-133)
+                part[q][c] = __builtin_amdgcn_perm(__float_as_uint(v[2 * c + 1]), __float_as_uint(v[2 * c]), 0x07060302u);
+        }
+}
+
+// 8 values of wide type XT (at `run`, 16 or 32 bytes) as bfloat16 parts.
 template <int XT>
-__device__ inline void cut_parts(const u32x4* run, int j, bf16x8* part) {
+__device__ inline void cut_parts(const u32x4* run, u32x4* part) {
     if constexpr (XT == CNN_BF16) {
-        part[0] = __builtin_bit_cast(bf16x8, run[j]);
+        part[0] = run[0];
     } else {
-        float v[8];
+        float v[8], top = 0.0f;
         if constexpr (XT == CNN_F16) {
-            const f16x8 h = __builtin_bit_cast(f16x8, run[j]);
+            const f16x8 h = __builtin_bit_cast(f16x8, run[0]);
 #pragma unroll
             for (int c = 0; c < 8; ++c) v[c] = (float)h[c];
         } else {
 #pragma unroll
-            for (int c = 0; c < 8; ++c) v[c] = __uint_as_float(run[2 * j + c / 4][c % 4]);
+            for (int c = 0; c < 8; ++c) v[c] = __uint_as_float(run[c / 4][c % 4]);
         }
+        // infinities are rare: one test for eight values, and the wave's lanes together
 #pragma unroll
-        for (int q = 0; q < kParts<XT>; ++q) {
-            u32x4 p;
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                if (q + 1 < kParts<XT>)
-                    p[c] = cut_pair(v[2 * c], v[2 * c + 1]);
-                else  // what is left has 8 bits at most (below 2^-107: is cut at 2^-133)
-                    p[c] = __builtin_amdgcn_perm(__float_as_uint(v[2 * c + 1]), __float_as_uint(v[2 * c]), 0x07060302u);
-            }
-            part[q] = __builtin_bit_cast(bf16x8, p);
-        }
+        for (int c = 0; c < 8; ++c) top = fmaxf(top, fabsf(v[c]));
+        if (__any(top == INFINITY)) cut8<kParts<XT>, true>(v, part);
+        else cut8<kParts<XT>, false>(v, part);
     }
 }
 

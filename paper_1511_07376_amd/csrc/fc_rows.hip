@@ -17,34 +17,50 @@
 namespace cnn {
 namespace {
 
-// 128-value steps a wave loads at once: 4 KiB of weights for each 16 outputs
-// (8 for fp32).
-template <int WT>
-constexpr int kSteps = WT == CNN_MX4 ? 4 : WT == CNN_F32 ? 1 : 1;
+// Thin groups (THIN: up to 4 rows a pass) bring their rows of x to LDS first,
+// a wave its own part of the reduction: each value is loaded, and where needed cut
+// into parts, by one lane and not by the 16 that use it.
+constexpr int kThin = 4;
 
-template <int XT, int WT, int OT, int RT, bool FULL>
+template <int XT, int WT, int SS>
+struct ThinRows {
+    static constexpr int ES = kElemBytes<XT>;
+    static constexpr int kPlanes = WT == CNN_MX4 ? kParts<XT> : 1;
+    static constexpr bool kCut = kPlanes > 1;
+    static constexpr int PER = kCut ? 8 : 16 / ES;               // values a vector
+    static constexpr int kLoads = kCut && XT == CNN_F32 ? 2 : 1;  // 16-byte loads of one
+    static constexpr int kInRow = SS * 128 / PER;                // vectors of a row and step
+    static constexpr int kEach = kThin * kInRow / 64;            // of a lane
+    static_assert(kThin * kInRow % 64 == 0 && kEach >= 1, "whole vectors a lane");
+    static constexpr int kRow = kInRow * 16 + 16;  // bytes in LDS: rows on other banks
+    static constexpr int kBytes = kPlanes * kThin * kRow;
+};
+
+template <int XT, int WT, int OT, int RT, int SS, bool THIN, bool FULL>
 __device__ inline void rows_step(const GroupedFc& p, const char* const* wrow, const uint8_t* const* wscale,
-                                 const char* const* xrow, const uint8_t* const* xscale, int64_t s, int nb, int quad,
+                                 const char* const* xrow, const uint8_t* const* xscale, char* thin, int64_t s, int nb,
                                  f32x4 (&acc)[OT][RT]) {
-    constexpr int SS = kSteps<WT>;
+    const int lane = threadIdx.x & 63, l16 = lane & 15, quad = lane >> 4;
+    constexpr int XLOADS = THIN && ThinRows<XT, WT, SS>::kCut ? 1 : kRunLoads<XT>;
     u32x4 w[OT][SS][kRunLoads<WT>];
     unsigned ws[OT][SS], xs[RT][SS];
-    u32x4 x[RT][SS][kRunLoads<XT>];
+    u32x4 x[RT][SS][XLOADS];
     // block (32 values) of step t for this lane
     auto block = [&](int t) { return (s * SS + t) * 4 + quad; };
-    auto load_mx4 = [&](const char* row, const uint8_t* scale, u32x4* run, unsigned* sc, int stride) {
-        if constexpr (FULL && SS == 4) {
-            const u32x4 all = load16(scale + s * 16);
+    auto load_mx4 = [&](const char* row, const uint8_t* scale, u32x4* run, unsigned* sc) {
+        if constexpr (FULL) {
+            unsigned all[SS];
+            __builtin_memcpy(all, scale + s * (4 * SS), 4 * SS);
 #pragma unroll
             for (int t = 0; t < SS; ++t) {
-                run[t * stride] = load16(row + block(t) * 16);
+                run[t] = load16(row + block(t) * 16);
                 sc[t] = (all[t] >> (8 * quad)) & 255;
             }
         } else {
 #pragma unroll
             for (int t = 0; t < SS; ++t) {
-                const bool ok = FULL || block(t) < nb;
-                run[t * stride] = ok ? load16(row + block(t) * 16) : u32x4{0, 0, 0, 0};
+                const bool ok = block(t) < nb;
+                run[t] = ok ? load16(row + block(t) * 16) : u32x4{0, 0, 0, 0};
                 sc[t] = ok ? scale[block(t)] : 127;
             }
         }
@@ -52,19 +68,59 @@ __device__ inline void rows_step(const GroupedFc& p, const char* const* wrow, co
 #pragma unroll
     for (int i = 0; i < OT; ++i) {
         if constexpr (WT == CNN_MX4) {
-            load_mx4(wrow[i], wscale[i], &w[i][0][0], ws[i], 1);
+            load_mx4(wrow[i], wscale[i], &w[i][0][0], ws[i]);
         } else {
 #pragma unroll
             for (int t = 0; t < SS; ++t) load_run<WT, FULL>(wrow[i], block(t) * 32, p.I, w[i][t]);
         }
     }
+    using TR = ThinRows<XT, WT, SS>;
+    if constexpr (THIN) {
+        u32x4 v[TR::kEach][TR::kLoads];
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-        if constexpr (XT == CNN_MX4) {
-            load_mx4(xrow[r], xscale[r], &x[r][0][0], xs[r], 1);
-        } else {
+        for (int e = 0; e < TR::kEach; ++e) {
+            const int64_t k = s * SS * 128 + (e * 64 + lane) % TR::kInRow * TR::PER;
+            const char* src = xrow[e] + k * TR::ES;
+            if (FULL || k + TR::PER <= p.I) {
 #pragma unroll
-            for (int t = 0; t < SS; ++t) load_run<XT, FULL>(xrow[r], block(t) * 32, p.I, x[r][t]);
+                for (int h = 0; h < TR::kLoads; ++h) v[e][h] = load16(src + h * 16);
+            } else {
+                load_edge<XT, TR::kLoads>(src, (int)max(p.I - k, (int64_t)0), v[e]);
+            }
+        }
+        // the reads of the step before are done: a wave's LDS accesses run in order
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int e = 0; e < TR::kEach; ++e) {
+            char* dst = thin + (e * 64 + lane) / TR::kInRow * TR::kRow + (e * 64 + lane) % TR::kInRow * 16;
+            if constexpr (TR::kCut) {
+                u32x4 part[TR::kPlanes];
+                cut_parts<XT>(v[e], part);
+#pragma unroll
+                for (int q = 0; q < TR::kPlanes; ++q) *reinterpret_cast<u32x4*>(dst + q * kThin * TR::kRow) = part[q];
+            } else {
+                *reinterpret_cast<u32x4*>(dst) = v[e][0];
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        if constexpr (!TR::kCut) {
+#pragma unroll
+            for (int t = 0; t < SS; ++t)
+#pragma unroll
+                for (int j = 0; j < kRunLoads<XT>; ++j)
+                    x[0][t][j] = *reinterpret_cast<const u32x4*>(thin + l16 % kThin * TR::kRow + (t * 128 + quad * 32) * TR::ES + j * 16);
+        }
+    } else {
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            if constexpr (XT == CNN_MX4) {
+                load_mx4(xrow[r], xscale[r], &x[r][0][0], xs[r]);
+            } else {
+#pragma unroll
+                for (int t = 0; t < SS; ++t) load_run<XT, FULL>(xrow[r], block(t) * 32, p.I, x[r][t]);
+            }
         }
     }
 #pragma unroll
@@ -89,9 +145,17 @@ __device__ inline void rows_step(const GroupedFc& p, const char* const* wrow, co
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 if constexpr (WT == CNN_MX4) {
-                    bf16x8 part[RT][kParts<XT>];
+                    u32x4 part[RT][kParts<XT>];
 #pragma unroll
-                    for (int r = 0; r < RT; ++r) cut_parts<XT>(x[r][t], j, part[r]);
+                    for (int r = 0; r < RT; ++r) {
+                        if constexpr (THIN && TR::kCut) {
+#pragma unroll
+                            for (int q = 0; q < kParts<XT>; ++q)
+                                part[r][q] = *reinterpret_cast<const u32x4*>(thin + (q * kThin + l16 % kThin) * TR::kRow + (t * 16 + quad * 4 + j) * 16);
+                        } else {
+                            cut_parts<XT>(&x[r][t][XT == CNN_F32 ? 2 * j : j], part[r]);
+                        }
+                    }
 #pragma unroll
                     for (int i = 0; i < OT; ++i) {
                         const bf16x8 wv = decode8(w[i][t][0][j], mx4_scale(ws[i][t]));
@@ -99,7 +163,7 @@ __device__ inline void rows_step(const GroupedFc& p, const char* const* wrow, co
                         for (int r = 0; r < RT; ++r)
 #pragma unroll
                             for (int q = kParts<XT> - 1; q >= 0; --q)
-                                acc[i][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv, part[r][q], acc[i][r], 0, 0, 0);
+                                acc[i][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv, __builtin_bit_cast(bf16x8, part[r][q]), acc[i][r], 0, 0, 0);
                     }
                 } else {
 #pragma unroll
@@ -119,16 +183,20 @@ __device__ inline void rows_step(const GroupedFc& p, const char* const* wrow, co
     }
 }
 
-template <int XT, int WT, int OT, int RT, int NW>
+template <int XT, int WT, int OT, int RT, int SS, int NW, bool THIN>
 __global__ void __launch_bounds__(64 * NW) fc_rows(GroupedFc p, int64_t units, int cols) {
-    constexpr int ROWS = 16 * RT, OUTS = 16 * OT;
+    constexpr int ROWS = THIN ? kThin : 16 * RT, OUTS = 16 * OT;
+    static_assert(!THIN || (RT == 1 && XT != CNN_MX4), "thin rows are wide");
+    using TR = ThinRows<XT, WT, SS>;
+    constexpr int XPTRS = THIN ? TR::kEach : RT;
+    __shared__ __attribute__((aligned(16))) char thin[THIN ? NW * TR::kBytes : 16];
     __shared__ __attribute__((aligned(16))) float part[NW][OT * RT][256];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int l16 = lane & 15, quad = lane >> 4;
+    const int l16 = lane & 15;
     const int nb = (int)(((int64_t)p.I + 31) / 32);
     const int64_t xbytes = XT == CNN_MX4 ? (int64_t)nb * 16 : (int64_t)p.I * kElemBytes<XT>;
     const int64_t wbytes = WT == CNN_MX4 ? (int64_t)nb * 16 : (int64_t)p.I * kElemBytes<WT>;
-    const int64_t span = kSteps<WT> * 128;
+    const int64_t span = SS * 128;
     const int64_t full = p.I / span, steps = (p.I + span - 1) / span;
     for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
         const int g = (int)(u / cols);
@@ -144,11 +212,12 @@ __global__ void __launch_bounds__(64 * NW) fc_rows(GroupedFc p, int64_t units, i
             wscale[i] = p.ws + at * nb;
         }
         for (int64_t row0 = lo; row0 < hi; row0 += ROWS) {
-            const char* xrow[RT];
-            const uint8_t* xscale[RT];
+            const char* xrow[XPTRS];
+            const uint8_t* xscale[XPTRS];
 #pragma unroll
-            for (int r = 0; r < RT; ++r) {
-                const size_t at = (size_t)max(source_row(p, (int)min(row0 + 16 * r + l16, (int64_t)hi - 1)), 0);
+            for (int r = 0; r < XPTRS; ++r) {
+                const int row = THIN ? (r * 64 + lane) / TR::kInRow : 16 * r + l16;
+                const size_t at = (size_t)max(source_row(p, (int)min(row0 + row, (int64_t)hi - 1)), 0);
                 xrow[r] = (const char*)p.x + at * xbytes;
                 xscale[r] = p.xs + at * nb;
             }
@@ -157,25 +226,37 @@ __global__ void __launch_bounds__(64 * NW) fc_rows(GroupedFc p, int64_t units, i
             for (int i = 0; i < OT; ++i)
 #pragma unroll
                 for (int r = 0; r < RT; ++r) acc[i][r] = f32x4{0, 0, 0, 0};
+            // what the epilogue needs of memory is on its way before the weights are
+            constexpr int EACH = (ROWS * OUTS + 64 * NW - 1) / (64 * NW);
+            float bias[EACH];
+            bool none[EACH];
+#pragma unroll
+            for (int c = 0; c < EACH; ++c) {
+                const int e = threadIdx.x + c * 64 * NW;
+                const int64_t m = min(row0 + e / OUTS, (int64_t)hi - 1), o = min((int64_t)o0 + e % OUTS, (int64_t)p.O - 1);
+                bias[c] = p.bias ? p.bias[(size_t)g * p.O + o] : 0.0f;
+                none[c] = p.rows && source_row(p, (int)m) < 0;
+            }
             int64_t s = wave;
-            for (; s < full; s += NW) rows_step<XT, WT, OT, RT, true>(p, wrow, wscale, xrow, xscale, s, nb, quad, acc);
-            if (s < steps) rows_step<XT, WT, OT, RT, false>(p, wrow, wscale, xrow, xscale, s, nb, quad, acc);
+            for (; s < full; s += NW) rows_step<XT, WT, OT, RT, SS, THIN, true>(p, wrow, wscale, xrow, xscale, thin + wave * TR::kBytes * THIN, s, nb, acc);
+            if (s < steps) rows_step<XT, WT, OT, RT, SS, THIN, false>(p, wrow, wscale, xrow, xscale, thin + wave * TR::kBytes * THIN, s, nb, acc);
 #pragma unroll
             for (int i = 0; i < OT; ++i)
 #pragma unroll
                 for (int r = 0; r < RT; ++r) *reinterpret_cast<f32x4*>(&part[wave][i * RT + r][lane * 4]) = acc[i][r];
             __syncthreads();
-            for (int e = threadIdx.x; e < ROWS * OUTS; e += 64 * NW) {
+#pragma unroll
+            for (int c = 0; c < EACH; ++c) {
+                const int e = threadIdx.x + c * 64 * NW;
                 const int row = e / OUTS, o = e % OUTS;
                 const int64_t m = row0 + row;
-                if (m < hi && (int64_t)o0 + o < p.O) {
+                if (e < ROWS * OUTS && m < hi && (int64_t)o0 + o < p.O) {
                     const int tile = (o / 16) * RT + row / 16;
                     const int at = ((o % 16) / 4 * 16 + row % 16) * 4 + o % 4;
                     float v = 0.0f;
 #pragma unroll
                     for (int w = 0; w < NW; ++w) v += part[w][tile][at];
-                    if (source_row(p, (int)m) < 0) v = 0.0f;
-                    if (p.bias) v += p.bias[(size_t)g * p.O + o0 + o];
+                    v = (none[c] ? 0.0f : v) + bias[c];
                     if (p.relu) v = v > 0.0f ? v : 0.0f;
                     if constexpr (XT == CNN_MX4) store_result(p.y_type, p.y, (size_t)m * p.O + o0 + o, v);
                     else store_result<XT>(p.y, (size_t)m * p.O + o0 + o, v);
@@ -186,18 +267,40 @@ __global__ void __launch_bounds__(64 * NW) fc_rows(GroupedFc p, int64_t units, i
     }
 }
 
-template <int XT, int WT, int OT, int RT, int NW>
+template <int XT, int WT, int OT, int RT, int SS, int NW, bool THIN>
 void start(const GroupedFc& p, hipStream_t st) {
     const int cols = ceil_div(p.O, 16 * OT);
     const int64_t units = (int64_t)p.G * cols;
-    enqueue(fc_rows<XT, WT, OT, RT, NW>, dim3((unsigned)std::min<int64_t>(units, 1 << 22)), dim3(64 * NW), 0, st, p, units, cols);
+    enqueue(fc_rows<XT, WT, OT, RT, SS, NW, THIN>, dim3((unsigned)std::min<int64_t>(units, 1 << 22)), dim3(64 * NW), 0, st, p, units, cols);
 }
 
+// The variant of a call.  Wide weights: a workgroup of 8 waves for 16 outputs.
+// 4-bit weights: the same where there are few workgroups, with two steps of loads in
+// flight a wave (one token, 4096 x 4096: 4.5 us; with 32 outputs a workgroup
+// 6.4); from 1024 workgroups on 32 outputs share the rows of x, and a wave
+// takes about four steps, so that fewer waves meet in LDS (16 tokens, 4 of 64
+// experts of 2048 x 4096: 38.7 us; 16 outputs and 8 waves 63).
 template <int XT, int WT>
 void choose(const GroupedFc& p, hipStream_t st) {
-    const int each = (int)ceil_div64(p.M, p.G);
-    if (each <= 16) start<XT, WT, 1, 1, 8>(p, st);
-    else start<XT, WT, 1, 2, 8>(p, st);
+    const bool thin = XT != CNN_MX4 && ceil_div64(p.M, p.G) <= kThin;
+    if constexpr (WT == CNN_MX4) {
+        // groups without rows cost next to nothing
+        const bool many = (int64_t)std::min(p.G, p.M) * ceil_div(p.O, 16) >= 1024;
+        if constexpr (XT != CNN_MX4) {
+            if (thin) {
+                if (!many) start<XT, WT, 1, 1, 2, 8, true>(p, st);
+                else if (p.I <= 2048) start<XT, WT, 2, 1, 2, 2, true>(p, st);
+                else start<XT, WT, 2, 1, 2, 4, true>(p, st);
+                return;
+            }
+        }
+        if (many) start<XT, WT, 2, 1, 2, 4, false>(p, st);
+        else start<XT, WT, 1, 1, 2, 8, false>(p, st);
+    } else {
+        constexpr int SS = WT == CNN_F32 ? 1 : 2;  // 8 loads of a weight row in flight a lane
+        if (thin) start<XT, WT, 1, 1, 1, 8, true>(p, st);
+        else start<XT, WT, 1, 1, SS, 8, false>(p, st);
+    }
 }
 
 }  // namespace

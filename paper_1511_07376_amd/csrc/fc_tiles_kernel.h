@@ -102,32 +102,6 @@ struct TileFinder {
     }
 };
 
-// `count` values (0 or fewer: none) from p on in 16-byte vectors, zeros behind them.
-template <int T, int LOADS>
-__device__ inline void load_edge(const char* p, int count, u32x4* v) {
-    constexpr int ES = kElemBytes<T>;
-#pragma unroll
-    for (int h = 0; h < LOADS; ++h) {
-        u32x4 u = {0, 0, 0, 0};
-#pragma unroll
-        for (int c = 0; c < 16 / ES; ++c) {
-            const int at = h * (16 / ES) + c;
-            if (at < count) {
-                if constexpr (ES == 4) {
-                    unsigned e;
-                    __builtin_memcpy(&e, p + at * 4, 4);
-                    u[c] = e;
-                } else {
-                    uint16_t e;
-                    __builtin_memcpy(&e, p + at * 2, 2);
-                    u[c / 2] |= (unsigned)e << (16 * (c % 2));
-                }
-            }
-        }
-        v[h] = u;
-    }
-}
-
 // One operand's share of a work-item: the vectors of a slab it fetches.
 // DIRECT: copied to LDS by the load.  Otherwise load() brings them to registers and
 // store() writes them, as they are or cut into planes.
@@ -177,11 +151,10 @@ struct Fetch {
                 if constexpr (PLANES == 1) {
                     *reinterpret_cast<u32x4*>(dst) = reg[i];
                 } else {
-                    bf16x8 part[PLANES];
-                    cut_parts<T>(reg + i * kLoads, 0, part);
+                    u32x4 part[PLANES];
+                    cut_parts<T>(reg + i * kLoads, part);
 #pragma unroll
-                    for (int q = 0; q < PLANES; ++q)
-                        *reinterpret_cast<bf16x8*>(dst + q * ROWS * C * 16) = part[q];
+                    for (int q = 0; q < PLANES; ++q) *reinterpret_cast<u32x4*>(dst + q * ROWS * C * 16) = part[q];
                 }
             }
         }
