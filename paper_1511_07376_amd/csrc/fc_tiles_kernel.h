@@ -17,16 +17,47 @@
 #include "fc_operands.h"
 
 #include <algorithm>
+#include <type_traits>
+#include <utility>
 
 namespace cnn {
 
 struct TileParams {
     GroupedFc fc;
-    int cols;          // tiles across the outputs
-    int splits;        // parts of the reduction: above 1, sums go to `partial`
-    int pairs;         // pairs of slabs a split
-    float* partial;    // [splits][M][O]
+    int cols;        // tiles across the outputs
+    int slabs;       // slabs of the reduction
+    int unroll;      // slabs the kernel takes at a time
+    int slots;       // workgroups that run at once
+    float* partial;  // sums of the tail's parts, a tile each; NULL: no tile is split
 };
+
+// The tiles of a call, of which only the last few (fewer than run at once) may
+// be split along the reduction: into `parts` runs of `run` slabs, so that the
+// tail keeps all compute units busy for part of a tile's time instead of some of
+// them for all of it.  (With few tiles the tail is all there is.)
+struct Tail {
+    int64_t full;  // tiles before it
+    int tiles, parts, run;
+};
+constexpr int kMaxParts = 16;
+__host__ __device__ inline Tail make_tail(const TileParams& tp, int64_t tiles) {
+    Tail t;
+    t.full = tiles / tp.slots * tp.slots;
+    t.tiles = (int)(tiles - t.full);
+    t.parts = 1;
+    t.run = tp.slabs;
+    if (tp.partial && t.tiles > 0) {
+        const int fours = (tp.slabs + tp.unroll - 1) / tp.unroll;
+        const int want = tp.slots / t.tiles;
+        const int most = tp.slabs / 4;  // no part is shorter than 4 slabs
+        const int parts = want < most ? (want < kMaxParts ? want : kMaxParts) : (most < kMaxParts ? most : kMaxParts);
+        if (parts > 1) {
+            t.run = (fours + parts - 1) / parts * tp.unroll;
+            t.parts = (tp.slabs + t.run - 1) / t.run;
+        }
+    }
+    return t;
+}
 
 static __device__ const u32x4 kZeroVector = {0, 0, 0, 0};
 
@@ -36,14 +67,30 @@ __device__ constexpr int vector_swap(int row) {
     return C == 16 ? row & 15 : C == 8 ? (row >> 1) & 7 : C == 4 ? (row >> 1) & 3 : (row >> 2) & 1;
 }
 
-template <int XT, int WT>
+// The slabs of a kernel.  VEC: rows of wide operands are whole 16-byte vectors.
+// Operands that are copied to LDS by the loads have ST buffers there, so that
+// ST - 1 slabs are on their way while one is at work; those that go through
+// registers have two, and R slabs on their way in registers.
+template <int XT, int WT, int WM, int WN, int FM, int FN, bool VEC>
 struct Slab {
     static constexpr bool kCut = WT == CNN_MX4 && (XT == CNN_F32 || XT == CNN_F16);
-    static constexpr int BK = XT == CNN_MX4 ? 256 : WT == CNN_MX4 ? 64 : XT == CNN_F32 ? 32 : 64;
+    static constexpr bool kDecode = WT == CNN_MX4 && XT != CNN_MX4;
+    static constexpr bool ADIRECT = XT == CNN_MX4 || (VEC && !kCut), BDIRECT = WT == CNN_MX4 || VEC;
+    static constexpr int TM = WM * FM * 32, TN = WN * FN * 32, NT = 64 * WM * WN;
+    // steps of a plane's products in a slab (16 values of the 16-bit types, 8 of fp32, 64 of mx4)
+    static constexpr int T = 4;
+    static constexpr int BK = T * (XT == CNN_MX4 ? 64 : WT == CNN_F32 ? 8 : 16);
     static constexpr int kPlanes = kCut ? kParts<XT> : 1;
     static constexpr int AROW = XT == CNN_MX4 ? BK / 2 : kCut ? BK * 2 : BK * kElemBytes<XT>;  // bytes in LDS
     static constexpr int BROW = WT == CNN_MX4 ? BK / 2 : BK * kElemBytes<WT>;
     static constexpr int AC = AROW / 16, BC = BROW / 16;
+    static constexpr int APLANE = TM * AROW;
+    // 4 buffers where they fit with another workgroup's beside them (4 waves) or alone (8)
+    static constexpr int kRoom = WM * WN > 4 ? 160 * 1024 - 2048 : 80 * 1024 - 1024;
+    static constexpr int ST = ((ADIRECT ? 4 : 2) * APLANE * kPlanes + (BDIRECT ? 4 : 2) * TN * BROW) <= kRoom ? 4 : 2;
+    static constexpr int AST = ADIRECT ? ST : 2, BST = BDIRECT ? ST : 2;
+    static constexpr int R = WM * FM * WN * FN > 8 ? 1 : 2;
+    static_assert(R <= ST, "what is awaited is older than what may be on its way");
 };
 
 // Number of tiles of TM rows in all groups, and tile t among them.
@@ -102,17 +149,29 @@ struct TileFinder {
     }
 };
 
+// Where tile t is: tiles are numbered in bands of 4 rows of tiles, walked column by
+// column, so that neighbours share operands in an XCD's L2.
+template <int TM, int TN>
+__device__ inline void locate_tile(const TileFinder<TM>& finder, int64_t t, int64_t row_tiles, int cols, int& g, int& row0, int& hi, int& o0) {
+    constexpr int BAND = 4;
+    const int64_t band = t / (BAND * (int64_t)cols), in_band = t % (BAND * (int64_t)cols);
+    const int band_rows = (int)min((int64_t)BAND, row_tiles - band * BAND);
+    o0 = (int)(in_band / band_rows) * TN;
+    finder.find(band * BAND + in_band % band_rows, g, row0, hi);
+}
+
 // One operand's share of a work-item: the vectors of a slab it fetches.
 // DIRECT: copied to LDS by the load.  Otherwise load() brings them to registers and
 // store() writes them, as they are or cut into planes.
-template <int T, int ROWS, int C, int BK, int NT, bool DIRECT, int PLANES>
+template <int T, int ROWS, int C, int BK, int NT, bool DIRECT, int PLANES, int R>
 struct Fetch {
     static constexpr int kVectors = ROWS * C / NT;  // LDS vectors (of one plane) a work-item
     static_assert(ROWS * C % NT == 0, "whole vectors a work-item");
     static constexpr int PER = T == CNN_MX4 ? 32 : PLANES > 1 ? 8 : 16 / kElemBytes<T>;  // values a vector
     static constexpr int kLoads = PLANES > 1 && T == CNN_F32 ? 2 : 1;                    // 16-byte loads a vector
-    const char* ptr[kVectors];  // this work-item's vector of slab 0
-    u32x4 reg[DIRECT ? 1 : kVectors * kLoads];
+    const char* ptr[kVectors];  // this work-item's vectors of the next slab
+    static constexpr int kInstructions = kVectors * kLoads;  // memory instructions a slab
+    u32x4 reg[DIRECT ? 1 : R][DIRECT ? 1 : kVectors * kLoads];
 
     static __device__ int row_of(int i) { return (i * NT + (int)threadIdx.x) / C; }
     static __device__ int vector_of(int i) {
@@ -120,39 +179,45 @@ struct Fetch {
     }
     static __device__ constexpr int bytes(int values) { return T == CNN_MX4 ? values / 2 : values * kElemBytes<T>; }
 
-    // Slab s; `cols`: values of a row (mx4: of its whole blocks).
-    __device__ void load(int64_t s, int cols, char* lds) {
-        const bool full = (s + 1) * BK <= cols;
-        const int64_t ahead = s * bytes(BK);
-        if constexpr (DIRECT) {
+    // The next slab, of which `left` values (mx4: of whole blocks) remain, to LDS
+    // or to registers r.
+    __device__ void load(int64_t left, char* lds, int r) {
+        if (left >= BK) {
 #pragma unroll
             for (int i = 0; i < kVectors; ++i) {
-                const char* src = ptr[i] + ahead;
-                if (!full && s * BK + vector_of(i) * PER >= cols) src = (const char*)&kZeroVector;
-                // 64 lanes write 64 consecutive vectors from here on
-                char* dst = lds + (i * NT + (int)(threadIdx.x & ~63u)) * 16;
-                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
-                                                 (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
-            }
-        } else if (full) {
+                if constexpr (DIRECT) {
+                    copy(i, ptr[i], lds);
+                } else {
 #pragma unroll
-            for (int i = 0; i < kVectors * kLoads; ++i) reg[i] = load16(ptr[i / kLoads] + ahead + i % kLoads * 16);
+                    for (int h = 0; h < kLoads; ++h) reg[r][i * kLoads + h] = load16(ptr[i] + h * 16);
+                }
+                ptr[i] += bytes(BK);
+            }
         } else {
 #pragma unroll
-            for (int i = 0; i < kVectors; ++i)
-                load_edge<T, kLoads>(ptr[i] + ahead, (int)min(cols - s * BK - vector_of(i) * PER, (int64_t)PER), reg + i * kLoads);
+            for (int i = 0; i < kVectors; ++i) {
+                const int k = vector_of(i) * PER;
+                if constexpr (DIRECT) copy(i, k < left ? ptr[i] : (const char*)&kZeroVector, lds);
+                else load_edge<T, kLoads>(ptr[i], (int)min(left - k, (int64_t)PER), reg[r] + i * kLoads);
+            }
         }
     }
-    __device__ void store(char* lds) {
+    // 64 lanes write 64 consecutive vectors
+    static __device__ void copy(int i, const char* src, char* lds) {
+        char* dst = lds + (i * NT + (int)(threadIdx.x & ~63u)) * 16;
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
+                                         (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
+    }
+    __device__ void store(char* lds, int r) {
         if constexpr (!DIRECT) {
 #pragma unroll
             for (int i = 0; i < kVectors; ++i) {
                 char* dst = lds + (i * NT + (int)threadIdx.x) * 16;
                 if constexpr (PLANES == 1) {
-                    *reinterpret_cast<u32x4*>(dst) = reg[i];
+                    *reinterpret_cast<u32x4*>(dst) = reg[r][i];
                 } else {
                     u32x4 part[PLANES];
-                    cut_parts<T>(reg + i * kLoads, part);
+                    cut_parts<T>(reg[r] + i * kLoads, part);
 #pragma unroll
                     for (int q = 0; q < PLANES; ++q) *reinterpret_cast<u32x4*>(dst + q * ROWS * C * 16) = part[q];
                 }
@@ -166,33 +231,40 @@ template <int N>
 struct Scales {
     static constexpr int W = N / 4;
     unsigned word[W];
-    // blocks [at, at + N) of a row of nb
-    __device__ void load(const uint8_t* row, int64_t at, int nb) {
+    // blocks [at, at + N) of the row of nb that begins at base + row
+    __device__ void load(const uint8_t* base, int row, int at, int nb) {
+        const uint8_t* src = base + (unsigned)(row + at);
         if (at + N <= nb) {
-            if constexpr (N == 16) {
-                const u32x4 v = load16(row + at);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) word[i] = v[i];
-            } else {
-                __builtin_memcpy(word, row + at, N);
-            }
+            __builtin_memcpy(word, src, N);
         } else {
 #pragma unroll
             for (int i = 0; i < W; ++i) {
-                unsigned v = 0;
-#pragma unroll
-                for (int b = 0; b < 4; ++b) v |= (unsigned)(at + 4 * i + b < nb ? row[at + 4 * i + b] : 127) << (8 * b);
+                unsigned v = 0x7f7f7f7fu;  // beside zeros: anything but NaN
+#pragma unroll 1
+                for (int b = 0; b < 4 && at + 4 * i + b < nb; ++b) v = (v & ~(255u << (8 * b))) | (unsigned)src[4 * i + b] << (8 * b);
                 word[i] = v;
             }
         }
     }
 };
 
-// All loads of this wave have landed, and all its LDS reads are done; then
-// all waves'.
+template <int N>
+using Step = std::integral_constant<int, N>;
+template <typename F, int... U>
+__device__ inline void unroll_steps(F&& f, std::integer_sequence<int, U...>) {
+    (f(Step<U>{}), ...);
+}
+template <int N, typename F>
+__device__ inline void unroll_steps(F&& f) {
+    unroll_steps(f, std::make_integer_sequence<int, N>{});
+}
+
+// All but the wave's last N loads have landed, and all its LDS accesses are
+// done; then all waves'.
+template <int N>
 __device__ inline void slab_barrier() {
     asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
+    __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 0x70);  // vmcnt(N) lgkmcnt(0)
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 }
@@ -221,36 +293,53 @@ __device__ inline void store_row8(T* dst, const float* v, int count) {
 // Two waves a SIMD: 256 registers each.
 template <int XT, int WT, int WM, int WN, int FM, int FN, bool VEC>
 __global__ void __launch_bounds__(64 * WM * WN, 2) fc_tiles(TileParams tp) {
-    using S = Slab<XT, WT>;
-    constexpr int TM = WM * FM * 32, TN = WN * FN * 32, NT = 64 * WM * WN, BK = S::BK;
-    constexpr bool ADIRECT = XT == CNN_MX4 || (VEC && !S::kCut), BDIRECT = WT == CNN_MX4 || VEC;
-    constexpr int APLANE = TM * S::AROW;
-    constexpr int NS = 2 * BK / 32;  // scales a row and pair of slabs
-    __shared__ __attribute__((aligned(16))) char sA0[APLANE * S::kPlanes], sA1[APLANE * S::kPlanes];
-    __shared__ __attribute__((aligned(16))) char sB0[TN * S::BROW], sB1[TN * S::BROW];
+    using S = Slab<XT, WT, WM, WN, FM, FN, VEC>;
+    constexpr int TM = S::TM, TN = S::TN, NT = S::NT, BK = S::BK, APLANE = S::APLANE, ST = S::ST, R = S::R;
+    constexpr int kUnroll = ST;             // slabs: every buffer at a fixed place in the code
+    constexpr int NS = kUnroll * BK / 32;   // scales of a row in them
+    constexpr int ABYTES = APLANE * S::kPlanes, BBYTES = TN * S::BROW;
+    // arrays of their own: the compiler sees that a copy into one does not concern reads of another
+    __shared__ __attribute__((aligned(16))) char sA0[ABYTES], sA1[ABYTES], sA2[S::AST > 2 ? ABYTES : 16], sA3[S::AST > 2 ? ABYTES : 16];
+    __shared__ __attribute__((aligned(16))) char sB0[BBYTES], sB1[BBYTES], sB2[S::BST > 2 ? BBYTES : 16], sB3[S::BST > 2 ? BBYTES : 16];
     __shared__ int sRow[TM];
+    auto abuf = [&](auto slab) -> char* {
+        constexpr int i = decltype(slab)::value % S::AST;
+        if constexpr (i == 0) return sA0;
+        else if constexpr (i == 1) return sA1;
+        else if constexpr (i == 2) return sA2;
+        else return sA3;
+    };
+    auto bbuf = [&](auto slab) -> char* {
+        constexpr int i = decltype(slab)::value % S::BST;
+        if constexpr (i == 0) return sB0;
+        else if constexpr (i == 1) return sB1;
+        else if constexpr (i == 2) return sB2;
+        else return sB3;
+    };
 
     const GroupedFc& p = tp.fc;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int wm = wave / WN, wn = wave % WN, half = lane >> 5, l32 = lane & 31;
 
-    // Workgroups go to the eight XCDs in turn; each XCD gets a contiguous run
-    // of tiles, in bands of 4 rows of tiles walked column by column, so that
-    // neighbours share operands in its L2.
+    // Workgroups go to the eight XCDs in turn; each XCD gets a contiguous run of
+    // the tiles.
     const TileFinder<TM> finder{p};
     const int64_t row_tiles = finder.total();
-    const int64_t tiles = row_tiles * tp.cols, jobs = tiles * tp.splits;
-    for (int64_t b = blockIdx.x; b < jobs; b += gridDim.x) {
-        const int64_t xcd = b % 8, each = jobs / 8, more = jobs % 8;
-        const int64_t job = xcd * each + min(xcd, more) + b / 8;
-        const int split = (int)(job / tiles);
-        const int64_t tile = job % tiles;
-        constexpr int BAND = 4;
-        const int64_t band = tile / (BAND * tp.cols), in_band = tile % (BAND * tp.cols);
-        const int band_rows = (int)min((int64_t)BAND, row_tiles - band * BAND);
-        const int o0 = (int)(in_band / band_rows) * TN;
-        int g, row0, hi;
-        finder.find(band * BAND + in_band % band_rows, g, row0, hi);
+    const Tail tail = make_tail(tp, row_tiles * tp.cols);
+    const int64_t jobs = tail.full + (int64_t)tail.tiles * tail.parts;
+    for (int64_t turn = blockIdx.x; turn < jobs; turn += gridDim.x) {
+        int64_t tile;
+        int part = 0;
+        if (turn < tail.full) {
+            const int64_t xcd = turn % 8, each = tail.full / 8, more = tail.full % 8;
+            tile = xcd * each + min(xcd, more) + turn / 8;
+        } else {
+            tile = tail.full + (turn - tail.full) % tail.tiles;
+            part = (int)((turn - tail.full) / tail.tiles);
+        }
+        const bool split = turn >= tail.full && tail.parts > 1;
+        int g, row0, hi, o0;
+        locate_tile<TM, TN>(finder, tile, row_tiles, tp.cols, g, row0, hi, o0);
 
         for (int r = tid; r < TM; r += NT) sRow[r] = (int64_t)row0 + r < hi ? source_row(p, row0 + r) : -1;
         __syncthreads();
@@ -259,37 +348,40 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) fc_tiles(TileParams tp) {
         const int acols = XT == CNN_MX4 ? nb * 32 : p.I, bcols = WT == CNN_MX4 ? nb * 32 : p.I;
         const int64_t abytes = XT == CNN_MX4 ? (int64_t)nb * 16 : (int64_t)p.I * kElemBytes<XT>;
         const int64_t bbytes = WT == CNN_MX4 ? (int64_t)nb * 16 : (int64_t)p.I * kElemBytes<WT>;
-        using FetchA = Fetch<XT, TM, S::AC, BK, NT, ADIRECT, S::kPlanes>;
-        using FetchB = Fetch<WT, TN, S::BC, BK, NT, BDIRECT, 1>;
+        const int64_t first = split ? (int64_t)part * tail.run : 0, last = split ? min(first + tail.run, (int64_t)tp.slabs) : tp.slabs;
+        using FetchA = Fetch<XT, TM, S::AC, BK, NT, S::ADIRECT, S::kPlanes, R>;
+        using FetchB = Fetch<WT, TN, S::BC, BK, NT, S::BDIRECT, 1, R>;
         FetchA fa;
         FetchB fb;
 #pragma unroll
         for (int i = 0; i < FetchA::kVectors; ++i)
-            fa.ptr[i] = (const char*)p.x + (int64_t)max(sRow[FetchA::row_of(i)], 0) * abytes + FetchA::bytes(FetchA::vector_of(i) * FetchA::PER);
+            fa.ptr[i] = (const char*)p.x + (int64_t)max(sRow[FetchA::row_of(i)], 0) * abytes + FetchA::bytes(FetchA::vector_of(i) * FetchA::PER) + first * FetchA::bytes(BK);
 #pragma unroll
         for (int i = 0; i < FetchB::kVectors; ++i)
             fb.ptr[i] = (const char*)p.w + ((int64_t)g * p.O + min((int64_t)o0 + FetchB::row_of(i), (int64_t)p.O - 1)) * bbytes +
-                        FetchB::bytes(FetchB::vector_of(i) * FetchB::PER);
-        const uint8_t* as[XT == CNN_MX4 ? FM : 1];
-        const uint8_t* bs[WT == CNN_MX4 ? FN : 1];
+                        FetchB::bytes(FetchB::vector_of(i) * FetchB::PER) + first * FetchB::bytes(BK);
+        // scale rows: offsets from the group's (fewer than 2^31 values, so fewer scales)
+        const uint8_t* wscale = p.ws + (int64_t)g * p.O * nb;
+        int as[XT == CNN_MX4 ? FM : 1], bs[WT == CNN_MX4 ? FN : 1];
         if constexpr (XT == CNN_MX4) {
 #pragma unroll
-            for (int i = 0; i < FM; ++i) as[i] = p.xs + (int64_t)max(sRow[wm * FM * 32 + i * 32 + l32], 0) * nb;
+            for (int i = 0; i < FM; ++i) as[i] = max(sRow[wm * FM * 32 + i * 32 + l32], 0) * nb;
         }
         if constexpr (WT == CNN_MX4) {
 #pragma unroll
-            for (int j = 0; j < FN; ++j)
-                bs[j] = p.ws + ((int64_t)g * p.O + min((int64_t)o0 + wn * FN * 32 + j * 32 + l32, (int64_t)p.O - 1)) * nb;
+            for (int j = 0; j < FN; ++j) bs[j] = (int)min((int64_t)o0 + wn * FN * 32 + j * 32 + l32, (int64_t)p.O - 1) * nb;
         }
-        Scales<NS> asc[XT == CNN_MX4 ? FM : 1], bsc[WT == CNN_MX4 ? FN : 1];
-        auto load_scales = [&](int64_t pair) {
+        // scales of kUnroll slabs: those at work, and those that follow
+        Scales<NS> acur[XT == CNN_MX4 ? FM : 1], anext[XT == CNN_MX4 ? FM : 1], bcur[WT == CNN_MX4 ? FN : 1], bnext[WT == CNN_MX4 ? FN : 1];
+        auto load_scales = [&](int64_t slab) {
+            const int at = (int)(slab * (BK / 32));
             if constexpr (XT == CNN_MX4) {
 #pragma unroll
-                for (int i = 0; i < FM; ++i) asc[i].load(as[i], pair * NS, nb);
+                for (int i = 0; i < FM; ++i) anext[i].load(p.xs, as[i], at, nb);
             }
             if constexpr (WT == CNN_MX4) {
 #pragma unroll
-                for (int j = 0; j < FN; ++j) bsc[j].load(bs[j], pair * NS, nb);
+                for (int j = 0; j < FN; ++j) bnext[j].load(wscale, bs[j], at, nb);
             }
         };
 
@@ -301,147 +393,139 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) fc_tiles(TileParams tp) {
 #pragma unroll
                 for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
 
-        // this lane's first vector of a fragment; those of later steps are an XOR away
-        const int arow = (wm * FM * 32 + l32) * S::AROW, brow = (wn * FN * 32 + l32) * S::BROW;
-        const int aswap = vector_swap<S::AC>(l32), bswap = vector_swap<S::BC>(l32);
-        // scales cur, next: of the pair of slabs at work and of the one after
-        auto compute = [&](const char* A, const char* B, int in_pair, const Scales<NS>* xa, const Scales<NS>* wb) {
-            auto avec = [&](int plane, int i, int v, int hv) {
-                return *reinterpret_cast<const u32x4*>(A + plane * APLANE + i * 32 * S::AROW + arow + (((half * hv) ^ aswap ^ v) * 16));
-            };
-            auto bvec = [&](int j, int v, int hv) {
-                return *reinterpret_cast<const u32x4*>(B + j * 32 * S::BROW + brow + (((half * hv) ^ bswap ^ v) * 16));
-            };
-            if constexpr (XT == CNN_MX4) {
-                // blocks 2 t + half: bytes 0, 2, 4, 6 or 1, 3, 5, 7 of a slab's eight
-                const unsigned pick = half ? 0x07050301u : 0x06040200u;
-                unsigned sa[FM], sb[FN];
+        // A slab is U steps: T parts of its reduction, and for cut inputs each of
+        // their planes, least first.  A step's fragments are read while the one before
+        // is at work.
+        constexpr int U = S::T * S::kPlanes;
+        // this lane's first vector of a fragment; those of other steps are an XOR away
+        const int afirst = (wm * FM * 32 + l32) * S::AROW + ((half * (S::kDecode ? 4 : 1)) ^ vector_swap<S::AC>(l32)) * 16;
+        const int bfirst = (wn * FN * 32 + l32) * S::BROW + (half ^ vector_swap<S::BC>(l32)) * 16;
+        u32x4 a[2][FM], b[2][FN];  // b: of a step, or of a slab (4-bit weights to be decoded)
+        bf16x8 wide[S::kDecode ? FN : 1];
+        auto read = [&](auto slab, auto step) {
+            constexpr int u = decltype(step)::value, t = u / S::kPlanes, q = S::kPlanes - 1 - u % S::kPlanes;
+            constexpr int av = (S::kDecode ? t : 2 * t) * 16, bv = S::kDecode ? 0 : 2 * t * 16;
+            const char *A = abuf(slab), *B = bbuf(slab);
+            int af = afirst, bf = bfirst;
+            asm volatile("" : "+v"(af), "+v"(bf));  // one XOR here, not an address for every step in a register
 #pragma unroll
-                for (int i = 0; i < FM; ++i) sa[i] = __builtin_amdgcn_perm(xa[i].word[2 * in_pair + 1], xa[i].word[2 * in_pair], pick);
+            for (int i = 0; i < FM; ++i) a[u % 2][i] = *reinterpret_cast<const u32x4*>(A + q * APLANE + i * 32 * S::AROW + (af ^ av));
+            if constexpr (!S::kDecode || u == 0) {
 #pragma unroll
-                for (int j = 0; j < FN; ++j) sb[j] = __builtin_amdgcn_perm(wb[j].word[2 * in_pair + 1], wb[j].word[2 * in_pair], pick);
-#define CNN_STEP(t)                                                                                                      \
-    {                                                                                                                    \
-        u32x4 a[FM], b[FN];                                                                                              \
-        _Pragma("unroll") for (int i = 0; i < FM; ++i) a[i] = avec(0, i, 2 * t, 1);                                      \
-        _Pragma("unroll") for (int j = 0; j < FN; ++j) b[j] = bvec(j, 2 * t, 1);                                         \
-        _Pragma("unroll") for (int i = 0; i < FM; ++i) _Pragma("unroll") for (int j = 0; j < FN; ++j) acc[i][j] =        \
-            __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(mx4_operand(a[i]), mx4_operand(b[j]), acc[i][j], 4, 4, t,    \
-                                                            (int)sa[i], t, (int)sb[j]);                                  \
-    }
-                CNN_STEP(0) CNN_STEP(1) CNN_STEP(2) CNN_STEP(3)
-#undef CNN_STEP
-            } else if constexpr (WT == CNN_MX4) {
-                // two blocks a slab, one for each half of the lanes
-                u32x4 raw[FN];
-                float sc[FN];
-#pragma unroll
-                for (int j = 0; j < FN; ++j) {
-                    raw[j] = bvec(j, 0, 1);
-                    sc[j] = mx4_scale((wb[j].word[0] >> (16 * in_pair + 8 * half)) & 255);
-                }
-#pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    bf16x8 b[FN];
-#pragma unroll
-                    for (int j = 0; j < FN; ++j) b[j] = decode8(raw[j][t], sc[j]);
-#pragma unroll
-                    for (int q = S::kPlanes - 1; q >= 0; --q) {
-                        u32x4 a[FM];
-#pragma unroll
-                        for (int i = 0; i < FM; ++i) a[i] = avec(q, i, t, 4);
-#pragma unroll
-                        for (int i = 0; i < FM; ++i)
-#pragma unroll
-                            for (int j = 0; j < FN; ++j)
-                                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a[i]), b[j], acc[i][j], 0, 0, 0);
-                    }
-                }
-            } else {
-#pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    u32x4 a[FM], b[FN];
-#pragma unroll
-                    for (int i = 0; i < FM; ++i) a[i] = avec(0, i, 2 * t, 1);
-#pragma unroll
-                    for (int j = 0; j < FN; ++j) b[j] = bvec(j, 2 * t, 1);
-                    if constexpr (XT == CNN_F32) {
-#pragma unroll
-                        for (int c = 0; c < 4; ++c)
-#pragma unroll
-                            for (int i = 0; i < FM; ++i)
-#pragma unroll
-                                for (int j = 0; j < FN; ++j)
-                                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[i][c]), __uint_as_float(b[j][c]), acc[i][j], 0, 0, 0);
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < FM; ++i)
-#pragma unroll
-                            for (int j = 0; j < FN; ++j) {
-                                if constexpr (XT == CNN_BF16)
-                                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a[i]), __builtin_bit_cast(bf16x8, b[j]), acc[i][j], 0, 0, 0);
-                                else
-                                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a[i]), __builtin_bit_cast(f16x8, b[j]), acc[i][j], 0, 0, 0);
-                            }
-                    }
-                }
+                for (int j = 0; j < FN; ++j)
+                    b[S::kDecode ? decltype(slab)::value % 2 : u % 2][j] = *reinterpret_cast<const u32x4*>(B + j * 32 * S::BROW + (bf ^ bv));
             }
         };
-
-        const int64_t slabs = ((int64_t)max(acols, bcols) + BK - 1) / BK;
-        const int64_t first = (int64_t)split * tp.pairs * 2, last = min(first + (int64_t)tp.pairs * 2, slabs);
+        auto multiply = [&](auto slab, auto step) {
+            constexpr int h = decltype(slab)::value, u = decltype(step)::value, t = u / S::kPlanes, set = u % 2;
+            if constexpr (S::kDecode && u % S::kPlanes == 0) {
+                // a slab is two blocks, one for each half of the lanes
+#pragma unroll
+                for (int j = 0; j < FN; ++j)
+                    wide[j] = decode8(b[h % 2][j][t], mx4_scale((bcur[j].word[h / 2] >> (16 * (h % 2) + 8 * half)) & 255));
+            }
+            // mx4: a lane's blocks are 2 t + half: bytes 0 and 2 of two words, shifted by the half
+            auto scale = [&](const Scales<NS>& sc) { return (int)(sc.word[(2 * h + t / 2) % Scales<NS>::W] >> (8 * half)); };
+            constexpr int REPEAT = XT == CNN_F32 && WT == CNN_F32 ? 4 : 1;
+#pragma unroll
+            for (int c = 0; c < REPEAT; ++c)
+#pragma unroll
+                for (int i = 0; i < FM; ++i)
+#pragma unroll
+                    for (int j = 0; j < FN; ++j) {
+                        if constexpr (XT == CNN_MX4)
+                            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(mx4_operand(a[set][i]), mx4_operand(b[set][j]), acc[i][j], 4, 4,
+                                                                                        t % 2 * 2, scale(acur[i]), t % 2 * 2, scale(bcur[j]));
+                        else if constexpr (S::kDecode)
+                            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a[set][i]), wide[j], acc[i][j], 0, 0, 0);
+                        else if constexpr (XT == CNN_F32)
+                            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[set][i][c]), __uint_as_float(b[set][j][c]), acc[i][j], 0, 0, 0);
+                        else if constexpr (XT == CNN_BF16)
+                            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a[set][i]), __builtin_bit_cast(bf16x8, b[set][j]), acc[i][j], 0, 0, 0);
+                        else
+                            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a[set][i]), __builtin_bit_cast(f16x8, b[set][j]), acc[i][j], 0, 0, 0);
+                    }
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        // Asks for slab s (place `slab` in the unrolled code) of the operands that
+        // are copied, or of those that go through registers.
+        auto ask_direct = [&](int64_t s, auto slab) {
+            if (s >= last) return;
+            if constexpr (S::ADIRECT) fa.load(acols - s * BK, abuf(slab), 0);
+            if constexpr (S::BDIRECT) fb.load(bcols - s * BK, bbuf(slab), 0);
+        };
+        auto ask_staged = [&](int64_t s, auto slab) {
+            if (s >= last) return;
+            if constexpr (!S::ADIRECT) fa.load(acols - s * BK, nullptr, decltype(slab)::value % R);
+            if constexpr (!S::BDIRECT) fb.load(bcols - s * BK, nullptr, decltype(slab)::value % R);
+        };
+        auto put_staged = [&](auto slab) {
+            fa.store(abuf(slab), decltype(slab)::value % R);
+            fb.store(bbuf(slab), decltype(slab)::value % R);
+        };
+        // loads that may be on their way when a slab is taken: of ST - 2 later slabs and of R - 1
+        constexpr int kDirect = S::ADIRECT * FetchA::kInstructions + S::BDIRECT * FetchB::kInstructions;
+        constexpr int kStaged = !S::ADIRECT * FetchA::kInstructions + !S::BDIRECT * FetchB::kInstructions;
+        constexpr int kAhead = (ST - 2) * kDirect + (R - 1) * kStaged;
+        static_assert(kAhead < 64, "what a wait can count");
+        // Slab s, its step 0 already read.  Before its last step the next slab is made
+        // ready, later ones are asked for (this one's buffer is free: all waves have read what
+        // they need), and the next one's step 0 is read: the last step's products cover that.
+        auto work = [&](int64_t s, auto slab) {
+            constexpr int h = decltype(slab)::value;
+            unroll_steps<U - 1>([&](auto step) {
+                constexpr int u = decltype(step)::value;
+                read(slab, Step<u + 1>{});
+                multiply(slab, step);
+            });
+            if (s + 1 < last) {
+                put_staged(Step<h + 1>{});
+                // near the end loads may be fewer than counted on
+                if (kAhead > 0 && s + ST + 1 < last) slab_barrier<kAhead>();
+                else slab_barrier<0>();
+                ask_direct(s + ST, Step<h + ST>{});
+                ask_staged(s + 1 + R, Step<h + 1 + R>{});
+                if (h == kUnroll - 2 && s + 2 < last) load_scales(s + 2);
+                read(Step<(h + 1) % kUnroll>{}, Step<0>{});
+            }
+            multiply(slab, Step<U - 1>{});
+        };
         if (first < last) {
-            fa.load(first, acols, sA0);
-            fb.load(first, bcols, sB0);
-            load_scales(first / 2);
-            fa.store(sA0);
-            fb.store(sB0);
+            unroll_steps<ST>([&](auto slab) { ask_direct(first + decltype(slab)::value, slab); });
+            unroll_steps<R>([&](auto slab) { ask_staged(first + decltype(slab)::value, slab); });
+            load_scales(first);
+            put_staged(Step<0>{});
+            slab_barrier<0>();
+            ask_staged(first + R, Step<R>{});
+            read(Step<0>{}, Step<0>{});
         }
-        for (int64_t s = first; s < last; s += 2) {
-            Scales<NS> xa[XT == CNN_MX4 ? FM : 1], wb[WT == CNN_MX4 ? FN : 1];
-            slab_barrier();
+        for (int64_t s = first; s < last; s += kUnroll) {
             if constexpr (XT == CNN_MX4) {
 #pragma unroll
-                for (int i = 0; i < FM; ++i) xa[i] = asc[i];
+                for (int i = 0; i < FM; ++i) acur[i] = anext[i];
             }
             if constexpr (WT == CNN_MX4) {
 #pragma unroll
-                for (int j = 0; j < FN; ++j) wb[j] = bsc[j];
+                for (int j = 0; j < FN; ++j) bcur[j] = bnext[j];
             }
-            if (s + 1 < last) {
-                fa.load(s + 1, acols, sA1);
-                fb.load(s + 1, bcols, sB1);
-            }
-            if (s + 2 < last) load_scales(s / 2 + 1);
-            compute(sA0, sB0, 0, xa, wb);
-            if (s + 1 < last) {
-                fa.store(sA1);
-                fb.store(sB1);
-            }
-            slab_barrier();
-            if (s + 2 < last) {
-                fa.load(s + 2, acols, sA0);
-                fb.load(s + 2, bcols, sB0);
-            }
-            if (s + 1 < last) compute(sA1, sB1, 1, xa, wb);
-            if (s + 2 < last) {
-                fa.store(sA0);
-                fb.store(sB0);
-            }
+            unroll_steps<kUnroll>([&](auto slab) {
+                if (s + decltype(slab)::value < last) work(s + decltype(slab)::value, slab);
+            });
         }
 
         // A lane holds rows 8 (v / 4) + 4 half + v % 4 of column l32 of every 32 x
         // 32 block.  Through LDS, 16 rows of the wave's outputs at a time, it gets
         // 8 neighbours of a row: 128-byte lines leave whole.
         constexpr int SW = FN * 32, VROW = SW / 8, RPI = 64 / VROW;  // strip width, its vectors of 8, rows a round
-        static_assert(APLANE * S::kPlanes >= WM * WN * 16 * SW * 4, "the strips fit the first buffer");
-        __syncthreads();  // all waves are done with it
-        float* strip = reinterpret_cast<float*>(sA0) + wave * 16 * SW;
+        constexpr int STRIP = 16 * SW * 4, PER = ABYTES / STRIP;  // strips a buffer
+        static_assert(PER > 0 && 2 * PER >= WM * WN, "the strips fit two buffers");
+        __syncthreads();  // all waves are done with them
+        float* strip = reinterpret_cast<float*>((wave < PER ? sA0 : sA1) + wave % PER * STRIP);
         const int64_t oc = (int64_t)o0 + wn * SW + lane % VROW * 8;  // this lane's first output
         const int count = (int)min((int64_t)8, p.O - oc);
         float bias[8];
 #pragma unroll
-        for (int c = 0; c < 8; ++c) bias[c] = tp.splits == 1 && p.bias && c < count ? p.bias[(size_t)g * p.O + oc + c] : 0.0f;
+        for (int c = 0; c < 8; ++c) bias[c] = !split && p.bias && c < count ? p.bias[(size_t)g * p.O + oc + c] : 0.0f;
         auto finish = [&](auto put) {
 #pragma unroll
             for (int i = 0; i < FM; ++i)
@@ -465,7 +549,7 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) fc_tiles(TileParams tp) {
                         const bool none = sRow[r] < 0;
 #pragma unroll
                         for (int c = 0; c < 8; ++c) v[c] = none ? 0.0f : v[c];
-                        if ((int64_t)row0 + r < hi && count > 0) put((size_t)(row0 + r) * p.O + oc, v);
+                        if ((int64_t)row0 + r < hi && count > 0) put((size_t)(row0 + r) * p.O + oc, r, v);
                     }
                     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
                     __builtin_amdgcn_wave_barrier();
@@ -479,17 +563,17 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) fc_tiles(TileParams tp) {
                 if (p.relu) v[c] = v[c] > 0.0f ? v[c] : 0.0f;
             }
         };
-        if (tp.splits > 1) {
-            float* dst = tp.partial + (size_t)split * p.M * p.O;
-            finish([&](size_t at, float* v) { store_row8(dst + at, v, count); });
+        if (split) {
+            float* dst = tp.partial + (turn - tail.full) * (TM * TN) - o0;
+            finish([&](size_t, int r, float* v) { store_row8(dst + r * TN + oc, v, 8); });
         } else if constexpr (XT == CNN_F32) {
-            finish([&](size_t at, float* v) { result(v); store_row8((float*)p.y + at, v, count); });
+            finish([&](size_t at, int, float* v) { result(v); store_row8((float*)p.y + at, v, count); });
         } else if constexpr (XT == CNN_BF16) {
-            finish([&](size_t at, float* v) { result(v); store_row8((bf16_t*)p.y + at, v, count); });
+            finish([&](size_t at, int, float* v) { result(v); store_row8((bf16_t*)p.y + at, v, count); });
         } else if constexpr (XT == CNN_F16) {
-            finish([&](size_t at, float* v) { result(v); store_row8((f16_t*)p.y + at, v, count); });
+            finish([&](size_t at, int, float* v) { result(v); store_row8((f16_t*)p.y + at, v, count); });
         } else {
-            finish([&](size_t at, float* v) {
+            finish([&](size_t at, int, float* v) {
                 result(v);
                 if (p.y_type == CNN_F32) store_row8((float*)p.y + at, v, count);
                 else if (p.y_type == CNN_BF16) store_row8((bf16_t*)p.y + at, v, count);
@@ -500,45 +584,89 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) fc_tiles(TileParams tp) {
     }
 }
 
-// Rows and outputs of a tile.
-struct TileSize {
-    int rows, outs;
-};
-// The tile, the splits of the reduction and the slab pairs of each for a call; the same whenever the call's
-// sizes and types are, so that the workspace is known before.
-struct TilePlan {
-    int size;    // index into the tile sizes
-    int splits, pairs;
-};
-
-template <int XT, int WT, int WM, int WN, int FM, int FN>
-void start_tiles(const GroupedFc& p, const TilePlan& plan, bool vec, float* partial, hipStream_t st) {
-    constexpr int TM = WM * FM * 32, TN = WN * FN * 32;
-    const TileParams tp{p, ceil_div(p.O, TN), plan.splits, plan.pairs, partial};
-    // groups end inside a tile: at most one more tile each
-    const int64_t jobs = (ceil_div64(p.M, TM) + (p.offsets ? p.G : 0)) * tp.cols * plan.splits;
-    const dim3 grid((unsigned)std::min<int64_t>(jobs, 1 << 22)), block(64 * WM * WN);
-    if constexpr (XT == CNN_MX4) {
-        enqueue(fc_tiles<XT, WT, WM, WN, FM, FN, true>, grid, block, 0, st, tp);
-    } else {
-        if (vec) enqueue(fc_tiles<XT, WT, WM, WN, FM, FN, true>, grid, block, 0, st, tp);
-        else enqueue(fc_tiles<XT, WT, WM, WN, FM, FN, false>, grid, block, 0, st, tp);
+// Adds the parts of the tail's tiles, in their order, then bias and ReLU.  A
+// workgroup takes 8 rows of 64 (or 4 of 128, 2 of 256) work-items' outputs.
+template <int TM, int TN, int YT>
+__global__ void __launch_bounds__(256) fc_join(TileParams tp) {
+    constexpr int ROWS = 256 * 8 / TN, CHUNKS = TM / ROWS;
+    const GroupedFc& p = tp.fc;
+    const TileFinder<TM> finder{p};
+    const int64_t row_tiles = finder.total();
+    const Tail tail = make_tail(tp, row_tiles * tp.cols);
+    if (tail.parts < 2) return;
+    for (int u = blockIdx.x; u < tail.tiles * CHUNKS; u += gridDim.x) {
+        const int t = u / CHUNKS, r = u % CHUNKS * ROWS + (int)threadIdx.x * 8 / TN, c = (int)threadIdx.x * 8 % TN;
+        int g, row0, hi, o0;
+        locate_tile<TM, TN>(finder, tail.full + t, row_tiles, tp.cols, g, row0, hi, o0);
+        const int count = (int)min((int64_t)8, (int64_t)p.O - o0 - c);
+        if ((int64_t)row0 + r >= hi || count <= 0) continue;
+        const float* src = tp.partial + (int64_t)t * (TM * TN) + r * TN + c;
+        float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        for (int q = 0; q < tail.parts; ++q, src += (int64_t)tail.tiles * (TM * TN)) {
+            const f32x4 lo = *reinterpret_cast<const f32x4*>(src), up = *reinterpret_cast<const f32x4*>(src + 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                v[e] += lo[e];
+                v[4 + e] += up[e];
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if (p.bias && e < count) v[e] += p.bias[(size_t)g * p.O + o0 + c + e];
+            if (p.relu) v[e] = v[e] > 0.0f ? v[e] : 0.0f;
+        }
+        const size_t at = (size_t)(row0 + r) * p.O + o0 + c;
+        if constexpr (YT == CNN_F32) store_row8((float*)p.y + at, v, count);
+        else if constexpr (YT == CNN_BF16) store_row8((bf16_t*)p.y + at, v, count);
+        else store_row8((f16_t*)p.y + at, v, count);
     }
 }
 
-// By tile size: 0: 64 x 128, 1: 128 x 128, 2: 256 x 256 (128 x 256 for inputs cut into parts, whose planes fill LDS).
-template <int XT, int WT>
-void run_tiles(const GroupedFc& p, const TilePlan& plan, bool vec, float* partial, hipStream_t st) {
-    if (plan.size == 0) start_tiles<XT, WT, 1, 4, 2, 1>(p, plan, vec, partial, st);
-    else if (plan.size == 1) start_tiles<XT, WT, 2, 2, 2, 2>(p, plan, vec, partial, st);
-    else if constexpr (Slab<XT, WT>::kCut) start_tiles<XT, WT, 2, 4, 2, 2>(p, plan, vec, partial, st);
-    else start_tiles<XT, WT, 2, 4, 4, 2>(p, plan, vec, partial, st);
+// A call's tile size (0: 64 x 128, 1: 128 x 128, 2: 256 x 256, or 128 x 256 for
+// inputs cut into parts).
+struct TileSize {
+    int rows, outs, slots;  // slots: workgroups that run at once on 256 compute units
+};
+
+template <int TM, int TN>
+void start_join(const TileParams& tp, int64_t tiles, hipStream_t st) {
+    const dim3 grid((unsigned)(std::min<int64_t>(tiles, tp.slots) * (TM * TN / 2048))), block(256);
+    if (tp.fc.y_type == CNN_F32) enqueue(fc_join<TM, TN, CNN_F32>, grid, block, 0, st, tp);
+    else if (tp.fc.y_type == CNN_BF16) enqueue(fc_join<TM, TN, CNN_BF16>, grid, block, 0, st, tp);
+    else enqueue(fc_join<TM, TN, CNN_F16>, grid, block, 0, st, tp);
 }
 
-void run_tiles_f32(const GroupedFc&, const TilePlan&, bool vec, float* partial, hipStream_t);
-void run_tiles_16(const GroupedFc&, const TilePlan&, bool vec, float* partial, hipStream_t);
-void run_tiles_mx4(const GroupedFc&, const TilePlan&, bool vec, float* partial, hipStream_t);
-void run_tiles_wide_mx4(const GroupedFc&, const TilePlan&, bool vec, float* partial, hipStream_t);
-void run_tiles_cut(const GroupedFc&, const TilePlan&, bool vec, float* partial, hipStream_t);
+template <int XT, int WT, int WM, int WN, int FM, int FN, bool VEC>
+void start_tiles(const GroupedFc& p, int slots, float* partial, hipStream_t st) {
+    using S = Slab<XT, WT, WM, WN, FM, FN, VEC>;
+    const int64_t values = XT == CNN_MX4 ? ((int64_t)p.I + 31) / 32 * 32 : p.I;
+    const TileParams tp{p, ceil_div(p.O, S::TN), (int)ceil_div64(values, S::BK), S::ST, slots, partial};
+    // groups end inside a tile: at most one more tile each
+    const int64_t tiles = (ceil_div64(p.M, S::TM) + (p.offsets ? p.G : 0)) * tp.cols;
+    enqueue(fc_tiles<XT, WT, WM, WN, FM, FN, VEC>, dim3((unsigned)std::min<int64_t>(tiles + slots, 1 << 22)), dim3(S::NT), 0, st, tp);
+    // without groups the tail is known here
+    if (partial && (p.offsets || make_tail(tp, tiles).parts > 1)) start_join<S::TM, S::TN>(tp, tiles, st);
+}
+
+template <int XT, int WT, bool VEC>
+void run_tiles(const GroupedFc& p, int size, int slots, float* partial, hipStream_t st) {
+    if (size == 0) start_tiles<XT, WT, 1, 4, 2, 1, VEC>(p, slots, partial, st);
+    else if (size == 1) start_tiles<XT, WT, 2, 2, 2, 2, VEC>(p, slots, partial, st);
+    else if constexpr (Slab<XT, WT, 2, 4, 4, 2, VEC>::kCut) start_tiles<XT, WT, 2, 4, 2, 2, VEC>(p, slots, partial, st);
+    else if constexpr (XT != CNN_MX4 && VEC) start_tiles<XT, WT, 2, 4, 4, 2, VEC>(p, slots, partial, st);
+}
+
+// vec: rows of wide operands are whole 16-byte vectors.
+template <int XT, int WT>
+void run_tiles(const GroupedFc& p, int size, int slots, bool vec, float* partial, hipStream_t st) {
+    if (XT == CNN_MX4 || vec || Slab<XT, WT, 1, 4, 2, 1, true>::kCut) run_tiles<XT, WT, true>(p, size, slots, partial, st);
+    else if constexpr (XT != CNN_MX4 && !Slab<XT, WT, 1, 4, 2, 1, true>::kCut) run_tiles<XT, WT, false>(p, size, slots, partial, st);
+}
+
+void run_tiles_f32(const GroupedFc&, int size, int slots, bool vec, float* partial, hipStream_t);
+void run_tiles_16(const GroupedFc&, int size, int slots, bool vec, float* partial, hipStream_t);
+void run_tiles_mx4(const GroupedFc&, int size, int slots, bool vec, float* partial, hipStream_t);
+void run_tiles_wide_mx4(const GroupedFc&, int size, int slots, bool vec, float* partial, hipStream_t);
+void run_tiles_cut(const GroupedFc&, int size, int slots, bool vec, float* partial, hipStream_t);
 
 }  // namespace cnn
