@@ -30,7 +30,7 @@ bool cut_inputs(const GroupedFc& p) { return p.w_type == CNN_MX4 && (p.x_type ==
 
 TileSize tile_size(const GroupedFc& p, int size) {
     const bool cut = cut_inputs(p);
-    if (size == 0) return {64, 128, 512};
+    if (size == 0) return {64, 256, 256};
     if (size == 1) return {128, 128, cut && p.x_type == CNN_F32 ? 256 : 512};
     return {cut ? 128 : 256, 256, 256};
 }
