@@ -9,10 +9,10 @@
 // and a choice's place among them is the number of bits below its own: the
 // order does not depend on when an atomic lands.
 //
-// Tokens are taken 64 to a workgroup (a wave takes four).  Up to 64 tokens,
-// one workgroup does it all.  Above, one kernel chooses and counts the
-// choices of every expert per 64 tokens, and a second one adds up what stands
-// before each of its own 64 tokens and places them.  Where that sum is
+// Up to 64 tokens, one workgroup does it all.  Above, one kernel chooses, 32
+// tokens a workgroup (a wave takes two), and counts the choices of every expert
+// in them, and a second one adds up what stands before each 64 tokens and
+// places them.  Where that sum is
 // long (kMaxCounts) a kernel between the two turns the counts into sums.
 #include "common.h"
 #include "wide_types.h"
@@ -23,20 +23,38 @@
 namespace cnn {
 namespace {
 
-constexpr int kTokens = 64;      // tokens a workgroup
+constexpr int kTokens = 32;      // tokens a workgroup, where there are several
+constexpr int kOne = 64;         // tokens up to which one does it all
 constexpr int kThreads = 1024;
 constexpr int kWaves = kThreads / 64;
 
-// Largest of the wave's values, in every lane.
-__device__ inline unsigned wave_umax(unsigned v) {
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) v = max(v, (unsigned)__shfl_xor((int)v, off));
-    return v;
+// Reductions over the wave by data-parallel moves: rows of 16 lanes first, then
+// across rows, the result in lane 63 and from there everywhere.  Lanes that a
+// move reads nothing for give 0, which changes neither a maximum of
+// unsigned values nor a sum.  (Through lane exchanges, which go by LDS, a
+// token's eight maxima took four times as long.)
+template <int CTRL, int ROWS>
+__device__ inline unsigned moved(unsigned v) {
+    return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, true);
 }
-__device__ inline float wave_sum(float v) {
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off);
-    return v;
+__device__ inline unsigned wave_umax(unsigned v) {
+    v = max(v, moved<0x111, 0xf>(v));  // one lane up
+    v = max(v, moved<0x112, 0xf>(v));
+    v = max(v, moved<0x114, 0xf>(v));
+    v = max(v, moved<0x118, 0xf>(v));
+    v = max(v, moved<0x142, 0xa>(v));  // lane 15 of a row to the next row, 1 and 3
+    v = max(v, moved<0x143, 0xc>(v));  // lane 31 to rows 2 and 3
+    return (unsigned)__builtin_amdgcn_readlane((int)v, 63);
+}
+__device__ inline float wave_sum(float f) {
+    auto add = [](float a, unsigned b) { return a + __uint_as_float(b); };
+    f = add(f, moved<0x111, 0xf>(__float_as_uint(f)));
+    f = add(f, moved<0x112, 0xf>(__float_as_uint(f)));
+    f = add(f, moved<0x114, 0xf>(__float_as_uint(f)));
+    f = add(f, moved<0x118, 0xf>(__float_as_uint(f)));
+    f = add(f, moved<0x142, 0xa>(__float_as_uint(f)));
+    f = add(f, moved<0x143, 0xc>(__float_as_uint(f)));
+    return __uint_as_float((unsigned)__builtin_amdgcn_readlane((int)__float_as_uint(f), 63));
 }
 
 // A number that orders as the logit does, -0 as 0; 0 for what is never chosen (minus
@@ -50,53 +68,49 @@ __device__ inline float key_logit(unsigned key) {
     return __uint_as_float((key >> 31) ? key & 0x7fffffffu : ~key);
 }
 
-// One wave, one token: lane l holds experts l, l + 64, ... (J of them).
-template <typename T, int J>
-__device__ inline void choose(const T* row, int E, int k, bool renorm, int32_t* expert, float* weight,
+// One wave, one token: lane l holds experts l, l + 64, ... (J of them, as
+// order keys).  Lane c ends up with choice c.
+template <int J>
+__device__ inline void choose(unsigned (&key)[J], int k, bool renorm, int32_t* expert, float* weight,
                               unsigned long long* mask, int bit) {
     const int lane = threadIdx.x & 63;
-    unsigned key[J];
-#pragma unroll
-    for (int j = 0; j < J; ++j) key[j] = lane + 64 * j < E ? order_key(to_f32(row[lane + 64 * j])) : 0;
-    float top = 0.0f, all = 0.0f, chosen = 0.0f, mine = 0.0f;
+    unsigned best[J], mine = 0;  // best: of key[0..j], kept up as keys go
     int my_expert = -1;
+    float sum = 0.0f, top = 0.0f;
     for (int c = 0; c < k; ++c) {
-        unsigned best = 0;
+        best[0] = key[0];
 #pragma unroll
-        for (int j = 0; j < J; ++j) best = max(best, key[j]);
-        best = wave_umax(best);
-        if (best == 0) break;  // nothing left that may be chosen
-        int e = -1;
+        for (int j = 1; j < J; ++j) best[j] = max(best[j - 1], key[j]);
+        const unsigned most = wave_umax(best[J - 1]);
+        if (most == 0) break;  // nothing left that may be chosen
+        int e = 0;
 #pragma unroll
         for (int j = J - 1; j >= 0; --j) {
-            const unsigned long long at = __ballot(key[j] == best);
+            const unsigned long long at = __ballot(key[j] == most);
             if (at) e = 64 * j + __builtin_ctzll(at);
         }
-        const float logit = key_logit(best);
         if (c == 0) {
-            top = logit;
+            top = key_logit(most);
             if (!renorm) {
-                float s = 0.0f;
 #pragma unroll
                 for (int j = 0; j < J; ++j)
-                    if (key[j]) s += expf(key_logit(key[j]) - top);
-                all = wave_sum(s);
+                    if (key[j]) sum += expf(key_logit(key[j]) - top);
             }
         }
-        const float p = expf(logit - top);
-        chosen += p;
         if (lane == c) {
-            mine = p;
+            mine = most;
             my_expert = e;
         }
 #pragma unroll
         for (int j = 0; j < J; ++j)
             if (e == lane + 64 * j) key[j] = 0;
     }
+    const float p = mine ? expf(key_logit(mine) - top) : 0.0f;
+    sum = wave_sum(renorm ? p : sum);
     if (lane < k) {
         expert[lane] = my_expert;
-        weight[lane] = my_expert < 0 ? 0.0f : mine / (renorm ? chosen : all);
-        if (my_expert >= 0) atomicOr(&mask[my_expert], 1ull << bit);
+        weight[lane] = mine ? p / sum : 0.0f;
+        if (mine) atomicOr(&mask[my_expert], 1ull << bit);
     }
 }
 
@@ -108,24 +122,45 @@ struct RouteParams {
     int32_t* rows;
     int32_t* offsets;
     int32_t* slot;
-    int32_t* counts;  // [ceil(T / 64)][E]
+    int32_t* counts;  // [ceil(T / 32)][E], and the totals
 };
 
-// Places the choices of tokens [t0, t0 + n): first[e] is the slot of the first
-// of these tokens' choices of expert e.
-__device__ inline void place(const RouteParams& p, int t0, int n, const int* first, const unsigned long long* mask) {
-    for (int i = threadIdx.x; i < n * p.k; i += kThreads) {
-        const int t = i / p.k;
-        const size_t at = (size_t)t0 * p.k + i;
-        const int e = p.expert[at];
-        int s = -1;
-        if (e >= 0) {
-            s = first[e] + __builtin_popcountll(mask[e] & ((1ull << t) - 1));
-            p.rows[s] = t0 + t;
+// The experts of the choices of n <= kOne tokens from t0 on, of this work-item:
+// choices threadIdx.x, + kThreads, ...
+constexpr int kMostChoices = 64;
+struct Choices {
+    static constexpr int kEach = kOne * kMostChoices / kThreads;
+    int expert[kEach];
+
+    __device__ void load(const RouteParams& p, int t0, int n) {
+#pragma unroll
+        for (int c = 0; c < kEach; ++c) {
+            const int i = threadIdx.x + c * kThreads;
+            expert[c] = i < n * p.k ? p.expert[(size_t)t0 * p.k + i] : -1;
         }
-        p.slot[at] = s;
     }
-}
+    // Marks the tokens in their experts' masks.
+    __device__ void mark(const RouteParams& p, unsigned long long* mask) const {
+#pragma unroll
+        for (int c = 0; c < kEach; ++c)
+            if (expert[c] >= 0) atomicOr(&mask[expert[c]], 1ull << ((threadIdx.x + c * kThreads) / (unsigned)p.k));
+    }
+    // first[e]: the slot of the first of these tokens' choices of expert e.
+    __device__ void place(const RouteParams& p, int t0, int n, const int* first, const unsigned long long* mask) const {
+#pragma unroll
+        for (int c = 0; c < kEach; ++c) {
+            const int i = threadIdx.x + c * kThreads;
+            if (i >= n * p.k) break;
+            const int t = (int)((unsigned)i / (unsigned)p.k), e = expert[c];
+            int s = -1;
+            if (e >= 0) {
+                s = first[e] + __builtin_popcountll(mask[e] & ((1ull << t) - 1));
+                p.rows[s] = t0 + t;
+            }
+            p.slot[(size_t)t0 * p.k + i] = s;
+        }
+    }
+};
 
 // before[e] = sum of total[e'] over e' < e, in LDS, and the sum of all in
 // *sum; the first wave does it.
@@ -151,16 +186,27 @@ __device__ inline void scan_experts(const int* total, int* before, int E, int* s
 // ONE: all tokens are this workgroup's, which places them too.
 template <typename T, int J, bool ONE>
 __global__ void __launch_bounds__(kThreads) route_choose(RouteParams p) {
+    constexpr int MOST = ONE ? kOne : kTokens, EACH = MOST / kWaves;  // tokens a wave
     __shared__ unsigned long long mask[64 * J];
     __shared__ int total[64 * J], before[64 * J], sum;
-    const int t0 = blockIdx.x * kTokens;
-    const int n = min(kTokens, p.T - t0);
+    const int t0 = blockIdx.x * MOST, lane = threadIdx.x & 63;
+    const int n = min(MOST, p.T - t0);
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    // all of the wave's logits are on their way before the first token's choices
+    unsigned key[EACH][J];
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const T* row = (const T*)p.logits + (size_t)(t0 + min(wave + i * kWaves, n - 1)) * p.E;
+#pragma unroll
+        for (int j = 0; j < J; ++j) key[i][j] = lane + 64 * j < p.E ? order_key(to_f32(row[lane + 64 * j])) : 0;
+    }
     for (int e = threadIdx.x; e < p.E; e += kThreads) mask[e] = 0;
     __syncthreads();
-    for (int t = (int)(threadIdx.x >> 6); t < n; t += kWaves) {
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const int t = wave + i * kWaves;
         const size_t row = (size_t)(t0 + t);
-        choose<T, J>((const T*)p.logits + row * p.E, p.E, p.k, p.renorm != 0, p.expert + row * p.k,
-                     p.weight + row * p.k, mask, t);
+        if (t < n) choose<J>(key[i], p.k, p.renorm != 0, p.expert + row * p.k, p.weight + row * p.k, mask, t);
     }
     __syncthreads();
     if constexpr (ONE) {
@@ -170,7 +216,9 @@ __global__ void __launch_bounds__(kThreads) route_choose(RouteParams p) {
         __syncthreads();
         for (int e = threadIdx.x; e < p.E; e += kThreads) p.offsets[e] = before[e];
         if (threadIdx.x == 0) p.offsets[p.E] = sum;
-        place(p, 0, n, before, mask);
+        Choices mine;
+        mine.load(p, 0, n);
+        mine.place(p, 0, n, before, mask);
         for (int i = sum + (int)threadIdx.x; i < n * p.k; i += kThreads) p.rows[i] = -1;
     } else {
         for (int e = threadIdx.x; e < p.E; e += kThreads)
@@ -203,17 +251,20 @@ __global__ void __launch_bounds__(kThreads) route_scan(int32_t* counts, int grou
     if (wave == kWaves - 1) counts[(int64_t)groups * E + e] = at;
 }
 
-// SCANNED: counts hold the sums of route_scan.
+// SCANNED: counts hold the sums of route_scan.  A workgroup places the choices
+// of kOne tokens, those of kOne / kTokens rows of counts.
 template <bool SCANNED>
 __global__ void __launch_bounds__(kThreads) route_place(RouteParams p, int groups) {
     __shared__ unsigned long long mask[1024];
     __shared__ int total[1024], mine[1024], before[1024], sum;
-    const int t0 = blockIdx.x * kTokens;
-    const int n = min(kTokens, p.T - t0);
+    const int t0 = blockIdx.x * kOne, g0 = blockIdx.x * (kOne / kTokens);
+    const int n = min(kOne, p.T - t0);
+    Choices choices;
+    choices.load(p, t0, n);
     for (int e = threadIdx.x; e < p.E; e += kThreads) {
         mask[e] = 0;
         if constexpr (SCANNED) {
-            mine[e] = p.counts[(size_t)blockIdx.x * p.E + e];
+            mine[e] = p.counts[(size_t)g0 * p.E + e];
             total[e] = p.counts[(size_t)groups * p.E + e];
         } else {
             mine[e] = total[e] = 0;
@@ -226,19 +277,17 @@ __global__ void __launch_bounds__(kThreads) route_place(RouteParams p, int group
         const int e = (int)threadIdx.x % p.E, r = (int)threadIdx.x / p.E;
         if (r < lanes) {
             int all = 0, earlier = 0;
+#pragma unroll 8
             for (int g = r; g < groups; g += lanes) {
                 const int v = p.counts[(size_t)g * p.E + e];
                 all += v;
-                earlier += g < (int)blockIdx.x ? v : 0;
+                earlier += g < g0 ? v : 0;
             }
             atomicAdd(&total[e], all);
             atomicAdd(&mine[e], earlier);
         }
     }
-    for (int i = threadIdx.x; i < n * p.k; i += kThreads) {
-        const int e = p.expert[(size_t)t0 * p.k + i];
-        if (e >= 0) atomicOr(&mask[e], 1ull << (i / p.k));
-    }
+    choices.mark(p, mask);
     __syncthreads();
     scan_experts(total, before, p.E, &sum);
     __syncthreads();
@@ -248,7 +297,7 @@ __global__ void __launch_bounds__(kThreads) route_place(RouteParams p, int group
     }
     for (int e = threadIdx.x; e < p.E; e += kThreads) mine[e] += before[e];
     __syncthreads();
-    place(p, t0, n, mine, mask);
+    choices.place(p, t0, n, mine, mask);
     // this workgroup's share of the slots that no choice has
     const int64_t lo = std::max<int64_t>((int64_t)t0 * p.k, sum), hi = (int64_t)(t0 + n) * p.k;
     for (int64_t i = lo + threadIdx.x; i < hi; i += kThreads) p.rows[i] = -1;
@@ -265,16 +314,16 @@ constexpr int64_t kMaxCounts = 32768;
 template <typename T, int J>
 void run_route(const RouteParams& p, hipStream_t st) {
     const int groups = ceil_div(p.T, kTokens);
-    if (groups == 1) {
+    if (p.T <= kOne) {
         enqueue(route_choose<T, J, true>, dim3(1), dim3(kThreads), 0, st, p);
         return;
     }
     enqueue(route_choose<T, J, false>, dim3(groups), dim3(kThreads), 0, st, p);
     if ((int64_t)groups * p.E <= kMaxCounts) {
-        enqueue(route_place<false>, dim3(groups), dim3(kThreads), 0, st, p, groups);
+        enqueue(route_place<false>, dim3(ceil_div(p.T, kOne)), dim3(kThreads), 0, st, p, groups);
     } else {
         enqueue(route_scan, dim3(ceil_div(p.E, 64)), dim3(kThreads), 0, st, p.counts, groups, p.E);
-        enqueue(route_place<true>, dim3(groups), dim3(kThreads), 0, st, p, groups);
+        enqueue(route_place<true>, dim3(ceil_div(p.T, kOne)), dim3(kThreads), 0, st, p, groups);
     }
 }
 
@@ -346,7 +395,7 @@ void run_combine(const T* x, int M, int D, const int32_t* slot, const float* wei
 
 size_t route_workspace(int T, int E) {
     const int64_t groups = ceil_div(T, kTokens);
-    return groups <= 1 ? 0 : (size_t)(groups + 1) * E * sizeof(int32_t);
+    return T <= kOne ? 0 : (size_t)(groups + 1) * E * sizeof(int32_t);
 }
 
 int launch_route(const void* logits, int type, int T, int E, int k, int renorm, int32_t* expert, float* weight,

@@ -95,7 +95,7 @@ def _route(**kw):
     (dict(E=1025), UNS), (dict(E=100, k=65), UNS), (dict(T=(1 << 27) + 1, E=1, k=1), UNS), (dict(T=1 << 25, E=1000), UNS),
     (dict(logits=0), INV), (dict(expert=0), INV), (dict(weight=0), INV), (dict(rows=0), INV), (dict(offsets=0), INV),
     (dict(slot=0), INV), (dict(logits=FAKE + 2), UNS), (dict(ws=FAKE + 2), UNS),
-    (dict(ws=0), WS), (dict(n=3 * 8 * 4 - 1), WS),       # two workgroups of 64 tokens and the totals
+    (dict(ws=0), WS), (dict(n=5 * 8 * 4 - 1), WS),       # four workgroups of 32 tokens and the totals
 ])
 def test_route_refuses(kw, status):
     assert _route(**kw) == status
@@ -104,7 +104,7 @@ def test_route_refuses(kw, status):
 
 def test_route_workspace():
     assert cnn.lib.cnn_route_workspace_bytes(64, 8, 2) == 0
-    assert cnn.lib.cnn_route_workspace_bytes(65, 8, 2) == 3 * 8 * 4
+    assert cnn.lib.cnn_route_workspace_bytes(65, 8, 2) == 4 * 8 * 4
     assert cnn.lib.cnn_route_workspace_bytes(65, 8, 9) == 0
 
 
