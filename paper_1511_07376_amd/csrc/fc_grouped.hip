@@ -13,9 +13,14 @@
 namespace cnn {
 namespace {
 
-constexpr int kRowsMost = 16;  // average rows a group up to which the weights are streamed
-
-bool few_rows(const GroupedFc& p) { return ceil_div64(p.M, p.G) <= kRowsMost; }
+// Up to 16 rows a group (on average: offsets are on the device) the weights
+// are streamed.  A plain layer on 4-bit weights, whose rows are known, up to 32 (24 rows,
+// 4096 x 4096, bf16: 9.6 us against 18.8 on tiles), but for inputs in fp32, whose parts
+// are then cut once for every 16 outputs (32 rows, 9216 x 4096: 42 us against 31).
+bool few_rows(const GroupedFc& p) {
+    const bool wide_pass = !p.offsets && p.w_type == CNN_MX4 && p.x_type != CNN_F32;
+    return ceil_div64(p.M, p.G) <= (wide_pass ? 32 : 16);
+}
 
 // Whole 16-byte vectors: rows of wide operands that begin and end at one.
 bool whole_vectors(const GroupedFc& p) {
@@ -30,19 +35,27 @@ bool cut_inputs(const GroupedFc& p) { return p.w_type == CNN_MX4 && (p.x_type ==
 
 TileSize tile_size(const GroupedFc& p, int size) {
     const bool cut = cut_inputs(p);
-    if (size == 0) return {64, 256, 256};
+    if (size == 0) return {64, 128, 512};
     if (size == 1) return {128, 128, cut && p.x_type == CNN_F32 ? 256 : 512};
     return {cut ? 128 : 256, 256, 256};
 }
 
 // By sizes and types alone (the workspace is sized before the call's pointers
-// are known).
+// are known).  The larger tile where there are enough of them for all compute
+// units: 2048 x 4096 x 4096 in bf16 on 4-bit weights 94, 77 and 106 us by size
+// (512 of 128 x 128), 4096 x 8192 x 8192 644, 555 and 482 (512 of 256 x 256), 512
+// tokens, 2 of 8 experts of 2048 x 2048 34, 38 and 56.  Cut inputs: each value is
+// cut once a workgroup, so the one with the most outputs (256 x 9216 x 4096 76, 86 and 72).
 int choose_size(const GroupedFc& p) {
     const int64_t each = ceil_div64(p.M, p.G);
+    auto tiles = [&](int size) {
+        const TileSize t = tile_size(p, size);
+        return ceil_div64(each, t.rows) * p.G * ceil_div(p.O, t.outs);
+    };
     if (each <= 64) return 0;
-    const bool large = cut_inputs(p) || (p.x_type != CNN_MX4 && (int64_t)p.I * type_bytes(p.x_type) % 16 == 0);
-    const TileSize t = tile_size(p, 2);
-    return large && ceil_div64(each, t.rows) * p.G * ceil_div(p.O, t.outs) >= 128 ? 2 : 1;
+    if (cut_inputs(p)) return 2;
+    if (p.x_type != CNN_MX4 && (int64_t)p.I * type_bytes(p.x_type) % 16 == 0 && tiles(2) >= 256) return 2;
+    return tiles(1) >= 384 ? 1 : 0;
 }
 
 }  // namespace

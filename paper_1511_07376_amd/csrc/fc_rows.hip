@@ -294,6 +294,13 @@ void choose(const GroupedFc& p, hipStream_t st) {
                 return;
             }
         }
+        if constexpr (XT != CNN_F32) {
+            if (ceil_div64(p.M, p.G) > 16) {
+                if (many) start<XT, WT, 2, 2, 2, 4, false>(p, st);
+                else start<XT, WT, 1, 2, 2, 8, false>(p, st);
+                return;
+            }
+        }
         if (many) start<XT, WT, 2, 1, 2, 4, false>(p, st);
         else start<XT, WT, 1, 1, 2, 8, false>(p, st);
     } else {

@@ -90,8 +90,6 @@ struct Slab {
     static constexpr int ST = ((ADIRECT ? 4 : 2) * APLANE * kPlanes + (BDIRECT ? 4 : 2) * TN * BROW) <= kRoom ? 4 : 2;
     static constexpr int AST = ADIRECT ? ST : 2, BST = BDIRECT ? ST : 2;
     static constexpr int R = WM * FM * WN * FN > 16 ? 1 : 2;
-    // steps whose fragments are read ahead: more where a step's products are few
-    static constexpr int kReadAhead = FM * FN > 2 ? 1 : 3, kSets = kReadAhead + 1;
     static_assert(R <= ST, "what is awaited is older than what may be on its way");
 };
 
@@ -403,9 +401,8 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) fc_tiles(TileParams tp) {
         // this lane's first vector of a fragment; those of other steps are an XOR away
         const int afirst = (wm * FM * 32 + l32) * S::AROW + ((half * (S::kDecode ? 4 : 1)) ^ vector_swap<S::AC>(l32)) * 16;
         const int bfirst = (wn * FN * 32 + l32) * S::BROW + (half ^ vector_swap<S::BC>(l32)) * 16;
-        constexpr int PD = S::kReadAhead, SETS = S::kSets;
-        static_assert(U % SETS == 0, "a step's set is the same in every slab");
-        u32x4 a[SETS][FM], b[S::kDecode ? 2 : SETS][FN];  // b: of a step, or of a slab (4-bit weights to be decoded)
+        static_assert(U % 2 == 0, "a step's set is the same in every slab");
+        u32x4 a[2][FM], b[2][FN];  // b: of a step, or of a slab (4-bit weights to be decoded)
         bf16x8 wide[S::kDecode ? FN : 1];
         auto read = [&](auto slab, auto step) {
             constexpr int u = decltype(step)::value, t = u / S::kPlanes, q = S::kPlanes - 1 - u % S::kPlanes;
@@ -414,15 +411,15 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) fc_tiles(TileParams tp) {
             int af = afirst, bf = bfirst;
             asm volatile("" : "+v"(af), "+v"(bf));  // one XOR here, not an address for every step in a register
 #pragma unroll
-            for (int i = 0; i < FM; ++i) a[u % SETS][i] = *reinterpret_cast<const u32x4*>(A + q * APLANE + i * 32 * S::AROW + (af ^ av));
+            for (int i = 0; i < FM; ++i) a[u % 2][i] = *reinterpret_cast<const u32x4*>(A + q * APLANE + i * 32 * S::AROW + (af ^ av));
             if constexpr (!S::kDecode || u == 0) {
 #pragma unroll
                 for (int j = 0; j < FN; ++j)
-                    b[S::kDecode ? decltype(slab)::value % 2 : u % SETS][j] = *reinterpret_cast<const u32x4*>(B + j * 32 * S::BROW + (bf ^ bv));
+                    b[S::kDecode ? decltype(slab)::value % 2 : u % 2][j] = *reinterpret_cast<const u32x4*>(B + j * 32 * S::BROW + (bf ^ bv));
             }
         };
         auto multiply = [&](auto slab, auto step) {
-            constexpr int h = decltype(slab)::value, u = decltype(step)::value, t = u / S::kPlanes, set = u % SETS;
+            constexpr int h = decltype(slab)::value, u = decltype(step)::value, t = u / S::kPlanes, set = u % 2;
             if constexpr (S::kDecode && u % S::kPlanes == 0) {
                 // a slab is two blocks, one for each half of the lanes
 #pragma unroll
@@ -473,29 +470,27 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) fc_tiles(TileParams tp) {
         constexpr int kStaged = !S::ADIRECT * FetchA::kInstructions + !S::BDIRECT * FetchB::kInstructions;
         constexpr int kAhead = (ST - 2) * kDirect + (R - 1) * kStaged;
         static_assert(kAhead < 64, "what a wait can count");
-        // Slab s, its first PD steps already read.  Before the first of its last PD steps
-        // the next slab is made ready and later ones are asked for (this one's buffer is
-        // free: all waves have read what they need); reads go on in the next slab.
+        // Slab s, its first step already read.  Before its last step the next slab is made
+        // ready, later ones are asked for (this one's buffer is free: all waves have
+        // read what they need), and the next one's first step is read: the last step's
+        // products cover that.  (Three steps ahead instead of one: no faster.)
         auto work = [&](int64_t s, auto slab) {
             constexpr int h = decltype(slab)::value;
-            unroll_steps<U>([&](auto step) {
-                constexpr int u = decltype(step)::value;
-                if constexpr (u < U - PD) {
-                    read(slab, Step<u + PD>{});
-                } else if (s + 1 < last) {
-                    if constexpr (u == U - PD) {
-                        put_staged(Step<h + 1>{});
-                        // near the end loads may be fewer than counted on
-                        if (kAhead > 0 && s + ST + 1 < last) slab_barrier<kAhead>();
-                        else slab_barrier<0>();
-                        ask_direct(s + ST, Step<h + ST>{});
-                        ask_staged(s + 1 + R, Step<h + 1 + R>{});
-                        if (h == kUnroll - 2 && s + 2 < last) load_scales(s + 2);
-                    }
-                    read(Step<(h + 1) % kUnroll>{}, Step<u + PD - U>{});
-                }
+            unroll_steps<U - 1>([&](auto step) {
+                read(slab, Step<decltype(step)::value + 1>{});
                 multiply(slab, step);
             });
+            if (s + 1 < last) {
+                put_staged(Step<h + 1>{});
+                // near the end loads may be fewer than counted on
+                if (kAhead > 0 && s + ST + 1 < last) slab_barrier<kAhead>();
+                else slab_barrier<0>();
+                ask_direct(s + ST, Step<h + ST>{});
+                ask_staged(s + 1 + R, Step<h + 1 + R>{});
+                if (h == kUnroll - 2 && s + 2 < last) load_scales(s + 2);
+                read(Step<(h + 1) % kUnroll>{}, Step<0>{});
+            }
+            multiply(slab, Step<U - 1>{});
         };
         if (first < last) {
             unroll_steps<ST>([&](auto slab) { ask_direct(first + decltype(slab)::value, slab); });
@@ -504,7 +499,7 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) fc_tiles(TileParams tp) {
             put_staged(Step<0>{});
             slab_barrier<0>();
             ask_staged(first + R, Step<R>{});
-            unroll_steps<PD>([&](auto step) { read(Step<0>{}, step); });
+            read(Step<0>{}, Step<0>{});
         }
         for (int64_t s = first; s < last; s += kUnroll) {
             if constexpr (XT == CNN_MX4) {
@@ -629,7 +624,7 @@ __global__ void __launch_bounds__(256) fc_join(TileParams tp) {
     }
 }
 
-// A call's tile size (0: 64 x 256, 1: 128 x 128, 2: 256 x 256, or 128 x 256 for
+// A call's tile size (0: 64 x 128, 1: 128 x 128, 2: 256 x 256, or 128 x 256 for
 // inputs cut into parts).
 struct TileSize {
     int rows, outs, slots;  // slots: workgroups that run at once on 256 compute units
@@ -657,7 +652,7 @@ void start_tiles(const GroupedFc& p, int slots, float* partial, hipStream_t st) 
 
 template <int XT, int WT, bool VEC>
 void run_tiles(const GroupedFc& p, int size, int slots, float* partial, hipStream_t st) {
-    if (size == 0) start_tiles<XT, WT, 1, 8, 2, 1, VEC>(p, slots, partial, st);
+    if (size == 0) start_tiles<XT, WT, 1, 4, 2, 1, VEC>(p, slots, partial, st);
     else if (size == 1) start_tiles<XT, WT, 2, 2, 2, 2, VEC>(p, slots, partial, st);
     else if constexpr (Slab<XT, WT, 2, 4, 4, 2, VEC>::kCut) start_tiles<XT, WT, 2, 4, 2, 2, VEC>(p, slots, partial, st);
     else if constexpr (XT != CNN_MX4 && VEC) start_tiles<XT, WT, 2, 4, 4, 2, VEC>(p, slots, partial, st);
@@ -666,8 +661,8 @@ void run_tiles(const GroupedFc& p, int size, int slots, float* partial, hipStrea
 // vec: rows of wide operands are whole 16-byte vectors.
 template <int XT, int WT>
 void run_tiles(const GroupedFc& p, int size, int slots, bool vec, float* partial, hipStream_t st) {
-    if (XT == CNN_MX4 || vec || Slab<XT, WT, 1, 8, 2, 1, true>::kCut) run_tiles<XT, WT, true>(p, size, slots, partial, st);
-    else if constexpr (XT != CNN_MX4 && !Slab<XT, WT, 1, 8, 2, 1, true>::kCut) run_tiles<XT, WT, false>(p, size, slots, partial, st);
+    if (XT == CNN_MX4 || vec || Slab<XT, WT, 1, 4, 2, 1, true>::kCut) run_tiles<XT, WT, true>(p, size, slots, partial, st);
+    else if constexpr (XT != CNN_MX4 && !Slab<XT, WT, 1, 4, 2, 1, true>::kCut) run_tiles<XT, WT, false>(p, size, slots, partial, st);
 }
 
 void run_tiles_f32(const GroupedFc&, int size, int slots, bool vec, float* partial, hipStream_t);
