@@ -40,30 +40,46 @@ constexpr int kElemBytes = T == CNN_F32 ? 4 : 2;  // wide types
 template <int XT>
 constexpr int kParts = XT == CNN_F32 ? 3 : XT == CNN_F16 ? 2 : 1;
 
-// `count` values (0 or fewer: none) from p on in 16-byte vectors, zeros behind them.
-template <int T, int LOADS>
-__device__ inline void load_edge(const char* p, int count, u32x4* v) {
-    constexpr int ES = kElemBytes<T>;
+// A 16-byte vector of which the first `count` values are in a row (0 or
+// fewer: none), zeros behind them; `before`: values of the row in front of it.  One
+// load, of the row's last 16 bytes, and a shift; a row shorter than
+// that is taken value by value.
+template <int T>
+__device__ inline u32x4 load_vector_edge(const char* p, int count, int64_t before) {
+    constexpr int ES = kElemBytes<T>, N = 16 / ES;
+    if (count >= N) return load16(p);
+    u32x4 v = {0, 0, 0, 0};
+    if (count <= 0) return v;
+    if (before >= N - count) {
+        const u32x4 last = load16(p - (N - count) * ES);
+        const uint64_t lo = last[0] | (uint64_t)last[1] << 32, hi = last[2] | (uint64_t)last[3] << 32;
+        const int bits = (N - count) * ES * 8;  // 1 to 15 bytes
+        const uint64_t l = bits < 64 ? lo >> bits | hi << 1 << (63 - bits) : hi >> (bits - 64), h = bits < 64 ? hi >> bits : 0;
+        return u32x4{(unsigned)l, (unsigned)(l >> 32), (unsigned)h, (unsigned)(h >> 32)};
+    }
 #pragma unroll
-    for (int h = 0; h < LOADS; ++h) {
-        u32x4 u = {0, 0, 0, 0};
-#pragma unroll
-        for (int c = 0; c < 16 / ES; ++c) {
-            const int at = h * (16 / ES) + c;
-            if (at < count) {
-                if constexpr (ES == 4) {
-                    unsigned e;
-                    __builtin_memcpy(&e, p + at * 4, 4);
-                    u[c] = e;
-                } else {
-                    uint16_t e;
-                    __builtin_memcpy(&e, p + at * 2, 2);
-                    u[c / 2] |= (unsigned)e << (16 * (c % 2));
-                }
+    for (int c = 0; c < N; ++c) {
+        if (c < count) {
+            if constexpr (ES == 4) {
+                unsigned e;
+                __builtin_memcpy(&e, p + c * 4, 4);
+                v[c] = e;
+            } else {
+                uint16_t e;
+                __builtin_memcpy(&e, p + c * 2, 2);
+                v[c / 2] |= (unsigned)e << (16 * (c % 2));
             }
         }
-        v[h] = u;
     }
+    return v;
+}
+
+// `count` values (0 or fewer: none) from p on in 16-byte vectors, zeros behind them.
+template <int T, int LOADS>
+__device__ inline void load_edge(const char* p, int count, int64_t before, u32x4* v) {
+    constexpr int N = 16 / kElemBytes<T>;
+#pragma unroll
+    for (int h = 0; h < LOADS; ++h) v[h] = load_vector_edge<T>(p + h * 16, count - h * N, before + h * N);
 }
 
 // 32 values of a row that ends after `cols` of them, from k on; past the end
@@ -75,7 +91,7 @@ __device__ inline void load_run(const char* row, int64_t k, int cols, u32x4* run
 #pragma unroll
         for (int j = 0; j < kRunLoads<T>; ++j) run[j] = load16(row + k * ES + j * 16);
     } else {
-        load_edge<T, kRunLoads<T>>(row + k * ES, (int)max((int64_t)cols - k, (int64_t)0), run);
+        load_edge<T, kRunLoads<T>>(row + k * ES, (int)max((int64_t)cols - k, (int64_t)0), k, run);
     }
 }
 

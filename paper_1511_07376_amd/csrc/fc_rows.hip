@@ -85,7 +85,7 @@ __device__ inline void rows_step(const GroupedFc& p, const char* const* wrow, co
 #pragma unroll
                 for (int h = 0; h < TR::kLoads; ++h) v[e][h] = load16(src + h * 16);
             } else {
-                load_edge<XT, TR::kLoads>(src, (int)max(p.I - k, (int64_t)0), v[e]);
+                load_edge<XT, TR::kLoads>(src, (int)max(p.I - k, (int64_t)0), k, v[e]);
             }
         }
         // the reads of the step before are done: a wave's LDS accesses run in order

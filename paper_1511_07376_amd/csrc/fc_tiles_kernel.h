@@ -180,9 +180,10 @@ struct Fetch {
     }
     static __device__ constexpr int bytes(int values) { return T == CNN_MX4 ? values / 2 : values * kElemBytes<T>; }
 
-    // The next slab, of which `left` values (mx4: of whole blocks) remain, to LDS
-    // or to registers r.
-    __device__ void load(int64_t left, char* lds, int r) {
+    // The next slab, s, of rows of `cols` values (mx4: of whole blocks), to LDS or to
+    // registers r.
+    __device__ void load(int64_t cols, int64_t s, char* lds, int r) {
+        const int64_t left = cols - s * BK;
         if (left >= BK) {
 #pragma unroll
             for (int i = 0; i < kVectors; ++i) {
@@ -199,7 +200,7 @@ struct Fetch {
             for (int i = 0; i < kVectors; ++i) {
                 const int k = vector_of(i) * PER;
                 if constexpr (DIRECT) copy(i, k < left ? ptr[i] : (const char*)&kZeroVector, lds);
-                else load_edge<T, kLoads>(ptr[i], (int)min(left - k, (int64_t)PER), reg[r] + i * kLoads);
+                else load_edge<T, kLoads>(ptr[i], (int)min(left - k, (int64_t)PER), s * BK + k, reg[r] + i * kLoads);
             }
         }
     }
@@ -453,13 +454,13 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) fc_tiles(TileParams tp) {
         // are copied, or of those that go through registers.
         auto ask_direct = [&](int64_t s, auto slab) {
             if (s >= last) return;
-            if constexpr (S::ADIRECT) fa.load(acols - s * BK, abuf(slab), 0);
-            if constexpr (S::BDIRECT) fb.load(bcols - s * BK, bbuf(slab), 0);
+            if constexpr (S::ADIRECT) fa.load(acols, s, abuf(slab), 0);
+            if constexpr (S::BDIRECT) fb.load(bcols, s, bbuf(slab), 0);
         };
         auto ask_staged = [&](int64_t s, auto slab) {
             if (s >= last) return;
-            if constexpr (!S::ADIRECT) fa.load(acols - s * BK, nullptr, decltype(slab)::value % R);
-            if constexpr (!S::BDIRECT) fb.load(bcols - s * BK, nullptr, decltype(slab)::value % R);
+            if constexpr (!S::ADIRECT) fa.load(acols, s, nullptr, decltype(slab)::value % R);
+            if constexpr (!S::BDIRECT) fb.load(bcols, s, nullptr, decltype(slab)::value % R);
         };
         auto put_staged = [&](auto slab) {
             fa.store(abuf(slab), decltype(slab)::value % R);
@@ -587,40 +588,35 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) fc_tiles(TileParams tp) {
 }
 
 // Adds the parts of the tail's tiles, in their order, then bias and ReLU.  A
-// workgroup takes 8 rows of 64 (or 4 of 128, 2 of 256) work-items' outputs.
+// work-item takes 4 neighbours, a workgroup 1024 outputs of a tile.
 template <int TM, int TN, int YT>
 __global__ void __launch_bounds__(256) fc_join(TileParams tp) {
-    constexpr int ROWS = 256 * 8 / TN, CHUNKS = TM / ROWS;
+    constexpr int CHUNKS = TM * TN / 1024;
     const GroupedFc& p = tp.fc;
     const TileFinder<TM> finder{p};
     const int64_t row_tiles = finder.total();
     const Tail tail = make_tail(tp, row_tiles * tp.cols);
     if (tail.parts < 2) return;
     for (int u = blockIdx.x; u < tail.tiles * CHUNKS; u += gridDim.x) {
-        const int t = u / CHUNKS, r = u % CHUNKS * ROWS + (int)threadIdx.x * 8 / TN, c = (int)threadIdx.x * 8 % TN;
+        const int t = u / CHUNKS, e = u % CHUNKS * 1024 + (int)threadIdx.x * 4, r = e / TN, c = e % TN;
         int g, row0, hi, o0;
         locate_tile<TM, TN>(finder, tail.full + t, row_tiles, tp.cols, g, row0, hi, o0);
-        const int count = (int)min((int64_t)8, (int64_t)p.O - o0 - c);
-        if ((int64_t)row0 + r >= hi || count <= 0) continue;
-        const float* src = tp.partial + (int64_t)t * (TM * TN) + r * TN + c;
-        float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        for (int q = 0; q < tail.parts; ++q, src += (int64_t)tail.tiles * (TM * TN)) {
-            const f32x4 lo = *reinterpret_cast<const f32x4*>(src), up = *reinterpret_cast<const f32x4*>(src + 4);
+        const int64_t o = (int64_t)o0 + c, m = (int64_t)row0 + r;
+        const int count = (int)min((int64_t)4, p.O - o);
+        if (m >= hi || count <= 0) continue;
+        float bias[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                v[e] += lo[e];
-                v[4 + e] += up[e];
-            }
-        }
+        for (int i = 0; i < 4; ++i) bias[i] = p.bias && i < count ? p.bias[(size_t)g * p.O + o + i] : 0.0f;
+        const float* src = tp.partial + (int64_t)t * (TM * TN) + e;
+        f32x4 sum = {0, 0, 0, 0};
+#pragma unroll 4
+        for (int q = 0; q < tail.parts; ++q) sum += *reinterpret_cast<const f32x4*>(src + (int64_t)q * tail.tiles * (TM * TN));
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            if (p.bias && e < count) v[e] += p.bias[(size_t)g * p.O + o0 + c + e];
-            if (p.relu) v[e] = v[e] > 0.0f ? v[e] : 0.0f;
+        for (int i = 0; i < 4; ++i) {
+            float v = sum[i] + bias[i];
+            if (p.relu) v = v > 0.0f ? v : 0.0f;
+            if (i < count) store_result<YT>(p.y, (size_t)m * p.O + o + i, v);
         }
-        const size_t at = (size_t)(row0 + r) * p.O + o0 + c;
-        if constexpr (YT == CNN_F32) store_row8((float*)p.y + at, v, count);
-        else if constexpr (YT == CNN_BF16) store_row8((bf16_t*)p.y + at, v, count);
-        else store_row8((f16_t*)p.y + at, v, count);
     }
 }
 
@@ -632,7 +628,7 @@ struct TileSize {
 
 template <int TM, int TN>
 void start_join(const TileParams& tp, int64_t tiles, hipStream_t st) {
-    const dim3 grid((unsigned)(std::min<int64_t>(tiles, tp.slots) * (TM * TN / 2048))), block(256);
+    const dim3 grid((unsigned)(std::min<int64_t>(tiles, tp.slots) * (TM * TN / 1024))), block(256);
     if (tp.fc.y_type == CNN_F32) enqueue(fc_join<TM, TN, CNN_F32>, grid, block, 0, st, tp);
     else if (tp.fc.y_type == CNN_BF16) enqueue(fc_join<TM, TN, CNN_BF16>, grid, block, 0, st, tp);
     else enqueue(fc_join<TM, TN, CNN_F16>, grid, block, 0, st, tp);
