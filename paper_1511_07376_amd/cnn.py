@@ -373,12 +373,8 @@ def _gpu(t, name: str) -> torch.device:
     return t.device
 
 
-_raw_stream = torch._C._cuda_getCurrentRawStream  # a tenth of torch.cuda.current_stream()'s time
-
-
-def _elsewhere(device, stream) -> bool:
-    """Whether a call's kernels go to another device or stream than the current ones."""
-    return stream is not None or device.index != torch.cuda.current_device()
+# the current GPU and stream as numbers, in a tenth of torch.cuda.current_stream()'s time
+_current_gpu, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
 
 
 @contextlib.contextmanager
@@ -403,7 +399,7 @@ def cnn_mx4_quantize(x, q=None, scale=None, stream=None):
 
     Leading dimensions are kept: x [G][O][I] gives q [G][O][...]."""
     device = _gpu(x, "x")
-    if _elsewhere(device, stream):
+    if stream is not None or device.index != _current_gpu():
         with _there(device, stream):
             return cnn_mx4_quantize(x, q, scale)
     if x.dim() < 2:
@@ -434,7 +430,7 @@ def cnn_mx4_quantize(x, q=None, scale=None, stream=None):
 def cnn_mx4_dequantize(q, scale, cols=None, dtype=torch.float32, y=None, stream=None):
     """The values of mx4 rows, [...][cols] (cols: 32 a block if not given)."""
     device = _gpu(q, "q")
-    if _elsewhere(device, stream):
+    if stream is not None or device.index != _current_gpu():
         with _there(device, stream):
             return cnn_mx4_dequantize(q, scale, cols, dtype, y)
     blocks = scale.shape[-1]
@@ -480,7 +476,7 @@ def cnn_fc_mx4_fwd(x, w, w_scale, bias=None, fuse_relu=False, x_scale=None, y_dt
 
     With x_scale x is mx4 too, and y of type y_dtype (float32 if not given)."""
     device = _gpu(x, "x")
-    if _elsewhere(device, stream):
+    if stream is not None or device.index != _current_gpu():
         with _there(device, stream):
             return cnn_fc_mx4_fwd(x, w, w_scale, bias, fuse_relu, x_scale, y_dtype, y)
     if x_scale is None and x.dim() > 2:
@@ -515,7 +511,7 @@ def cnn_fc_grouped_fwd(x, w, offsets, bias=None, fuse_relu=False, rows=None, w_s
     With w_scale [G][O][blocks] w is mx4; with x_scale x is too, and y of type y_dtype (float32 if not given).
     Rows of y in no group are not written."""
     device = _gpu(x, "x")
-    if _elsewhere(device, stream):
+    if stream is not None or device.index != _current_gpu():
         with _there(device, stream):
             return cnn_fc_grouped_fwd(x, w, offsets, bias, fuse_relu, rows, w_scale, x_scale, y_dtype, y)
     if x.dim() != 2 or w.dim() != 3:
@@ -547,7 +543,7 @@ def cnn_route_fwd(logits, k, renormalize=False, stream=None):
     """logits [T][E] -> (expert int32 [T][k], weight float32 [T][k], rows int32 [T*k], offsets int32 [E+1],
     slot int32 [T][k]): each token's k experts and their weights, and the rows for cnn_fc_grouped_fwd."""
     device = _gpu(logits, "logits")
-    if _elsewhere(device, stream):
+    if stream is not None or device.index != _current_gpu():
         with _there(device, stream):
             return cnn_route_fwd(logits, k, renormalize)
     if logits.dim() != 2:
@@ -574,7 +570,7 @@ def cnn_route_fwd(logits, k, renormalize=False, stream=None):
 def cnn_combine_fwd(x, slot, weight, y=None, stream=None):
     """x [M][D], slot int32 [N][k], weight float32 [N][k] -> y [N][D] = sum over j of weight[n][j] * x[slot[n][j]]."""
     device = _gpu(x, "x")
-    if _elsewhere(device, stream):
+    if stream is not None or device.index != _current_gpu():
         with _there(device, stream):
             return cnn_combine_fwd(x, slot, weight, y)
     if x.dim() != 2 or slot.dim() != 2:

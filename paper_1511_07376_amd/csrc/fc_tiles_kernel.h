@@ -29,6 +29,8 @@ struct TileParams {
     int unroll;      // slabs the kernel takes at a time
     int slots;       // workgroups that run at once
     float* partial;  // sums of the tail's parts, a tile each; NULL: no tile is split
+    int slab_ns;     // a slab's time, and that of a part of a tile to be written and
+    int part_ns;     // joined, on which the number of parts is chosen
 };
 
 // The tiles of a call, of which only the last few (fewer than run at once) may
@@ -40,6 +42,7 @@ struct Tail {
     int tiles, parts, run;
 };
 constexpr int kMaxParts = 16;
+constexpr int kJoinNs = 3000;  // the second kernel's own time
 __host__ __device__ inline Tail make_tail(const TileParams& tp, int64_t tiles) {
     Tail t;
     t.full = tiles / tp.slots * tp.slots;
@@ -47,13 +50,17 @@ __host__ __device__ inline Tail make_tail(const TileParams& tp, int64_t tiles) {
     t.parts = 1;
     t.run = tp.slabs;
     if (tp.partial && t.tiles > 0) {
-        const int fours = (tp.slabs + tp.unroll - 1) / tp.unroll;
-        const int want = tp.slots / t.tiles;
-        const int most = tp.slabs / 4;  // no part is shorter than 4 slabs
-        const int parts = want < most ? (want < kMaxParts ? want : kMaxParts) : (most < kMaxParts ? most : kMaxParts);
-        if (parts > 1) {
-            t.run = (fours + parts - 1) / parts * tp.unroll;
-            t.parts = (tp.slabs + t.run - 1) / t.run;
+        const int turns = (tp.slabs + tp.unroll - 1) / tp.unroll;  // no part is shorter than one
+        const int most = tp.slots / t.tiles < kMaxParts ? tp.slots / t.tiles : kMaxParts;
+        int64_t best = (int64_t)tp.slabs * tp.slab_ns;
+        for (int parts = 2; parts <= most && parts <= turns; ++parts) {
+            const int run = (turns + parts - 1) / parts * tp.unroll, got = (tp.slabs + run - 1) / run;
+            const int64_t time = (int64_t)run * tp.slab_ns + kJoinNs + (int64_t)t.tiles * got * tp.part_ns;
+            if (time < best) {
+                best = time;
+                t.run = run;
+                t.parts = got;
+            }
         }
     }
     return t;
@@ -634,11 +641,20 @@ void start_join(const TileParams& tp, int64_t tiles, hipStream_t st) {
     else enqueue(fc_join<TM, TN, CNN_F16>, grid, block, 0, st, tp);
 }
 
+// Nanoseconds of a slab of a 64 x 128 tile: measured between reductions of 4096
+// and 9216 values, 64 rows (fp32 inputs that are cut 1150, fp16 ones 800, bf16 beside
+// 4-bit weights 475, 4 bits both 660), on the fp32 matrix cores their
+// own time.  Larger tiles take about as much more as they have products a
+// wave (256 x 256 in bf16: 1750).  Writing and joining a tile's part: 0.65 us a MB.
+template <int XT, int WT>
+constexpr int kSlabNs = XT == CNN_MX4 ? 660 : XT == CNN_F32 ? (WT == CNN_MX4 ? 1150 : 1000) : XT == CNN_F16 && WT == CNN_MX4 ? 800 : 475;
+
 template <int XT, int WT, int WM, int WN, int FM, int FN, bool VEC>
 void start_tiles(const GroupedFc& p, int slots, float* partial, hipStream_t st) {
     using S = Slab<XT, WT, WM, WN, FM, FN, VEC>;
+    constexpr int kPartNs = S::TM * S::TN * 4 * 65 / 100000, kNs = kSlabNs<XT, WT> * (FM * FN) / 2;
     const int64_t values = XT == CNN_MX4 ? ((int64_t)p.I + 31) / 32 * 32 : p.I;
-    const TileParams tp{p, ceil_div(p.O, S::TN), (int)ceil_div64(values, S::BK), S::ST, slots, partial};
+    const TileParams tp{p, ceil_div(p.O, S::TN), (int)ceil_div64(values, S::BK), S::ST, slots, partial, kNs, kPartNs};
     // groups end inside a tile: at most one more tile each
     const int64_t tiles = (ceil_div64(p.M, S::TM) + (p.offsets ? p.G : 0)) * tp.cols;
     enqueue(fc_tiles<XT, WT, WM, WN, FM, FN, VEC>, dim3((unsigned)std::min<int64_t>(tiles + slots, 1 << 22)), dim3(S::NT), 0, st, tp);
