@@ -22,6 +22,18 @@
 
 namespace cnn {
 
+// The tiles of a call, of which only the last few (fewer than run at once) may
+// be split along the reduction: into `parts` runs of `run` slabs, so that the
+// tail keeps all compute units busy for part of a tile's time instead of some of
+// them for all of it.  (With few tiles the tail is all there is.)
+struct Tail {
+    int full;  // tiles before it
+    int tiles, parts, run;
+};
+
+// Numbers of tiles fit an int: a tile of a group's rows has one row at least, so there
+// are no more than rows times tiles across the outputs, each but the last of
+// which stands for 128 outputs or more.
 struct TileParams {
     GroupedFc fc;
     int cols;        // tiles across the outputs
@@ -31,35 +43,31 @@ struct TileParams {
     float* partial;  // sums of the tail's parts, a tile each; NULL: no tile is split
     int slab_ns;     // a slab's time, and that of a part of a tile to be written and
     int part_ns;     // joined, on which the number of parts is chosen
+    Tail tail;       // without groups: known to the host
 };
 
-// The tiles of a call, of which only the last few (fewer than run at once) may
-// be split along the reduction: into `parts` runs of `run` slabs, so that the
-// tail keeps all compute units busy for part of a tile's time instead of some of
-// them for all of it.  (With few tiles the tail is all there is.)
-struct Tail {
-    int64_t full;  // tiles before it
-    int tiles, parts, run;
-};
 constexpr int kMaxParts = 16;
 constexpr int kJoinNs = 3000;  // the second kernel's own time
-__host__ __device__ inline Tail make_tail(const TileParams& tp, int64_t tiles) {
+__host__ __device__ inline Tail make_tail(const TileParams& tp, int tiles) {
     Tail t;
-    t.full = tiles / tp.slots * tp.slots;
-    t.tiles = (int)(tiles - t.full);
+    t.full = (int)((unsigned)tiles / (unsigned)tp.slots) * tp.slots;
+    t.tiles = tiles - t.full;
     t.parts = 1;
     t.run = tp.slabs;
     if (tp.partial && t.tiles > 0) {
-        const int turns = (tp.slabs + tp.unroll - 1) / tp.unroll;  // no part is shorter than one
-        const int most = tp.slots / t.tiles < kMaxParts ? tp.slots / t.tiles : kMaxParts;
-        int64_t best = (int64_t)tp.slabs * tp.slab_ns;
-        for (int parts = 2; parts <= most && parts <= turns; ++parts) {
-            const int run = (turns + parts - 1) / parts * tp.unroll, got = (tp.slabs + run - 1) / run;
-            const int64_t time = (int64_t)run * tp.slab_ns + kJoinNs + (int64_t)t.tiles * got * tp.part_ns;
-            if (time < best) {
-                best = time;
-                t.run = run;
-                t.parts = got;
+        const unsigned turns = ((unsigned)tp.slabs + tp.unroll - 1) / (unsigned)tp.unroll;  // no part is shorter than one
+        unsigned most = (unsigned)tp.slots / (unsigned)t.tiles;
+        most = most < kMaxParts ? most : kMaxParts;
+        most = most < turns ? most : turns;
+        // slabs / parts * slab_ns + tiles * parts * part_ns is least at the root of their quotient
+        const float root = __builtin_sqrtf((float)tp.slabs * (float)tp.slab_ns / ((float)t.tiles * (float)tp.part_ns));
+        const unsigned parts = root < (float)most ? (unsigned)(root + 0.5f) : most;
+        if (parts > 1) {
+            const unsigned run = (turns + parts - 1) / parts * tp.unroll, got = ((unsigned)tp.slabs + run - 1) / run;
+            const float time = (float)run * tp.slab_ns + kJoinNs + (float)t.tiles * got * tp.part_ns;
+            if (time < (float)tp.slabs * tp.slab_ns) {
+                t.run = (int)run;
+                t.parts = (int)got;
             }
         }
     }
@@ -111,9 +119,8 @@ struct TileFinder {
         if (base + lane < p.G) group_rows(p.offsets, base + lane, p.M, lo, end);
         return (int)(((unsigned)(end - lo) + TM - 1) / TM);
     }
-    // (at most 2^31 / TM tiles and one for each group)
-    __device__ int64_t total() const {
-        if (!p.offsets) return ((int64_t)p.M + TM - 1) / TM;
+    __device__ int total() const {
+        if (!p.offsets) return (int)(((unsigned)p.M + TM - 1) / TM);
         int sum = 0;
         for (int base = 0; base < p.G; base += 64) {
             int lo, end;
@@ -124,12 +131,12 @@ struct TileFinder {
         }
         return __builtin_amdgcn_readfirstlane(sum);  // so that what depends on it stays scalar
     }
-    __device__ void find(int64_t t, int& g, int& row0, int& hi) const {
+    __device__ void find(int t, int& g, int& row0, int& hi) const {
         g = 0;
         row0 = 0;
         hi = 0;
         if (!p.offsets) {
-            row0 = (int)(t * TM);
+            row0 = t * TM;
             hi = p.M;
             return;
         }
@@ -146,7 +153,7 @@ struct TileFinder {
             const unsigned long long past = __ballot(before + incl > t);
             if (past) {
                 const int at = __builtin_ctzll(past);
-                const int first = (int)t - before - (__shfl(incl, at) - __shfl(tiles, at));
+                const int first = t - before - (__shfl(incl, at) - __shfl(tiles, at));
                 g = __builtin_amdgcn_readfirstlane(base + at);
                 row0 = __builtin_amdgcn_readfirstlane(__shfl(lo, at) + first * TM);
                 hi = __builtin_amdgcn_readfirstlane(__shfl(end, at));
@@ -160,12 +167,12 @@ struct TileFinder {
 // Where tile t is: tiles are numbered in bands of 4 rows of tiles, walked column by
 // column, so that neighbours share operands in an XCD's L2.
 template <int TM, int TN>
-__device__ inline void locate_tile(const TileFinder<TM>& finder, int64_t t, int64_t row_tiles, int cols, int& g, int& row0, int& hi, int& o0) {
-    constexpr int BAND = 4;
-    const int64_t band = t / (BAND * (int64_t)cols), in_band = t % (BAND * (int64_t)cols);
-    const int band_rows = (int)min((int64_t)BAND, row_tiles - band * BAND);
+__device__ inline void locate_tile(const TileFinder<TM>& finder, int t, int row_tiles, int cols, int& g, int& row0, int& hi, int& o0) {
+    constexpr unsigned BAND = 4;
+    const unsigned band = (unsigned)t / (BAND * (unsigned)cols), in_band = (unsigned)t % (BAND * (unsigned)cols);
+    const unsigned band_rows = min(BAND, (unsigned)row_tiles - band * BAND);
     o0 = (int)(in_band / band_rows) * TN;
-    finder.find(band * BAND + in_band % band_rows, g, row0, hi);
+    finder.find((int)(band * BAND + in_band % band_rows), g, row0, hi);
 }
 
 // One operand's share of a work-item: the vectors of a slab it fetches.
@@ -333,18 +340,17 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) fc_tiles(TileParams tp) {
     // Workgroups go to the eight XCDs in turn; each XCD gets a contiguous run of
     // the tiles.
     const TileFinder<TM> finder{p};
-    const int64_t row_tiles = finder.total();
-    const Tail tail = make_tail(tp, row_tiles * tp.cols);
-    const int64_t jobs = tail.full + (int64_t)tail.tiles * tail.parts;
-    for (int64_t turn = blockIdx.x; turn < jobs; turn += gridDim.x) {
-        int64_t tile;
-        int part = 0;
+    const int row_tiles = finder.total();
+    const Tail tail = p.offsets ? make_tail(tp, row_tiles * tp.cols) : tp.tail;
+    const int jobs = tail.full + tail.tiles * tail.parts;
+    for (int turn = blockIdx.x; turn < jobs; turn += gridDim.x) {
+        int tile, part = 0;
         if (turn < tail.full) {
-            const int64_t xcd = turn % 8, each = tail.full / 8, more = tail.full % 8;
+            const int xcd = turn % 8, each = tail.full / 8, more = tail.full % 8;
             tile = xcd * each + min(xcd, more) + turn / 8;
         } else {
             tile = tail.full + (turn - tail.full) % tail.tiles;
-            part = (int)((turn - tail.full) / tail.tiles);
+            part = (turn - tail.full) / tail.tiles;
         }
         const bool split = turn >= tail.full && tail.parts > 1;
         int g, row0, hi, o0;
@@ -574,7 +580,7 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) fc_tiles(TileParams tp) {
             }
         };
         if (split) {
-            float* dst = tp.partial + (turn - tail.full) * (TM * TN) - o0;
+            float* dst = tp.partial + (int64_t)(turn - tail.full) * (TM * TN) - o0;
             finish([&](size_t, int r, float* v) { store_row8(dst + r * TN + oc, v, 8); });
         } else if constexpr (XT == CNN_F32) {
             finish([&](size_t at, int, float* v) { result(v); store_row8((float*)p.y + at, v, count); });
@@ -601,8 +607,8 @@ __global__ void __launch_bounds__(256) fc_join(TileParams tp) {
     constexpr int CHUNKS = TM * TN / 1024;
     const GroupedFc& p = tp.fc;
     const TileFinder<TM> finder{p};
-    const int64_t row_tiles = finder.total();
-    const Tail tail = make_tail(tp, row_tiles * tp.cols);
+    const int row_tiles = finder.total();
+    const Tail tail = p.offsets ? make_tail(tp, row_tiles * tp.cols) : tp.tail;
     if (tail.parts < 2) return;
     for (int u = blockIdx.x; u < tail.tiles * CHUNKS; u += gridDim.x) {
         const int t = u / CHUNKS, e = u % CHUNKS * 1024 + (int)threadIdx.x * 4, r = e / TN, c = e % TN;
@@ -654,12 +660,12 @@ void start_tiles(const GroupedFc& p, int slots, float* partial, hipStream_t st) 
     using S = Slab<XT, WT, WM, WN, FM, FN, VEC>;
     constexpr int kPartNs = S::TM * S::TN * 4 * 65 / 100000, kNs = kSlabNs<XT, WT> * (FM * FN) / 2;
     const int64_t values = XT == CNN_MX4 ? ((int64_t)p.I + 31) / 32 * 32 : p.I;
-    const TileParams tp{p, ceil_div(p.O, S::TN), (int)ceil_div64(values, S::BK), S::ST, slots, partial, kNs, kPartNs};
+    TileParams tp{p, ceil_div(p.O, S::TN), (int)ceil_div64(values, S::BK), S::ST, slots, partial, kNs, kPartNs, {}};
     // groups end inside a tile: at most one more tile each
     const int64_t tiles = (ceil_div64(p.M, S::TM) + (p.offsets ? p.G : 0)) * tp.cols;
+    if (!p.offsets) tp.tail = make_tail(tp, (int)tiles);
     enqueue(fc_tiles<XT, WT, WM, WN, FM, FN, VEC>, dim3((unsigned)std::min<int64_t>(tiles + slots, 1 << 22)), dim3(S::NT), 0, st, tp);
-    // without groups the tail is known here
-    if (partial && (p.offsets || make_tail(tp, tiles).parts > 1)) start_join<S::TM, S::TN>(tp, tiles, st);
+    if (partial && (p.offsets || tp.tail.parts > 1)) start_join<S::TM, S::TN>(tp, tiles, st);
 }
 
 template <int XT, int WT, bool VEC>
