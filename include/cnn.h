@@ -231,17 +231,17 @@ int cnn_mx4_dequantize(const uint8_t* q, const uint8_t* scale, int rows, int col
  * Wide inputs are not quantised: products are of x as it is with the values
  * that w stands for (fp32 inputs below 2^-107 in magnitude keep an absolute
  * precision of 2^-133), sums are fp32 and the result is rounded once.
- * fuse_relu = 1 applies y = max(y, 0).  The result does not change from call to
- * call. */
+ * fuse_relu = 1 applies y = y > 0 ? y : +0 (so NaN becomes 0).  The result does
+ * not change from call to call. */
 int cnn_fc_mx4_fwd(const void* x, const uint8_t* x_scale, int x_type, int N, int I,
                    const uint8_t* w, const uint8_t* w_scale, const float* bias, int O,
                    int fuse_relu, void* y, int y_type, void* ws, size_t ws_bytes,
                    cnn_stream_t stream);
 
-/* Device workspace of cnn_fc_mx4_fwd for these types and sizes: the partial
- * sums of a reduction that is split over workgroups (some tens of rows);
- * often 0, and then ws may be NULL.  0 on error.  Calls that overlap need
- * workspaces of their own. */
+/* Device workspace of cnn_fc_mx4_fwd for these types and sizes (16-byte
+ * aligned, 64 MiB at most): partial sums of tiles whose reduction is split over
+ * workgroups.  Often 0, and then ws may be NULL.  0 on error.  Calls that
+ * overlap need workspaces of their own. */
 size_t cnn_fc_mx4_workspace_bytes(int x_type, int N, int I, int O);
 
 /* Fully-connected layers of groups of rows, each with weights of its own:
@@ -283,7 +283,7 @@ size_t cnn_route_workspace_bytes(int T, int E, int k);
  *     entry is the number of choices
  *   slot int32 [T][k]: where in rows a choice stands, -1 for no choice
  * rows and offsets are cnn_fc_grouped_fwd's, slot and weight cnn_combine_fwd's.
- * E <= 1024, k <= 64, k <= E, T <= 2^27.  T = 0 clears offsets.  Calls that
+ * E <= 1024, k <= 64, k <= E, T <= 2^26.  T = 0 clears offsets.  Calls that
  * overlap need workspaces of their own. */
 int cnn_route_fwd(const void* logits, int type, int T, int E, int k, int renormalize,
                   int32_t* expert, float* weight, int32_t* rows, int32_t* offsets,

@@ -370,7 +370,14 @@ def _wide(dtype, name: str) -> int:
 def _gpu(t, name: str) -> torch.device:
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a GPU tensor")
+    _sizes(name, t.numel())
     return t.device
+
+
+def _sizes(name: str, *sizes: int) -> None:
+    """Sizes are passed as int: none is cut to one that fits."""
+    if max(sizes) > 0x7fffffff:
+        raise CnnError(CNN_ERR_UNSUPPORTED, f"{name}: a size of {max(sizes)}, above 2^31-1")
 
 
 # the current GPU and stream as numbers, in a tenth of torch.cuda.current_stream()'s time
@@ -480,13 +487,14 @@ def cnn_fc_mx4_fwd(x, w, w_scale, bias=None, fuse_relu=False, x_scale=None, y_dt
         with _there(device, stream):
             return cnn_fc_mx4_fwd(x, w, w_scale, bias, fuse_relu, x_scale, y_dtype, y)
     if x_scale is None and x.dim() > 2:
-        x = x.reshape(x.shape[0], -1) if x.is_contiguous() else x
+        x = x.flatten(1) if x.is_contiguous() else x
     if x.dim() != 2 or w.dim() != 2 or w_scale.dim() != 2:
         raise ValueError("fc_mx4: x, w and w_scale must have two dimensions")
     xp, xs, xt, xc = _operand(x, x_scale, device, "x")
     wp, ws, wt, wc = _operand(w, w_scale, device, "w")
     cols = _columns(xt, xc, wt, wc, "fc_mx4")
     N, O = x.shape[0], w.shape[0]
+    _sizes("fc_mx4", O, cols)
     bp = _on(bias, "bias", device, torch.float32, (O,))
     dtype = x.dtype if xs is None else y_dtype or torch.float32
     st = _raw_stream(device.index)
@@ -521,6 +529,7 @@ def cnn_fc_grouped_fwd(x, w, offsets, bias=None, fuse_relu=False, rows=None, w_s
     cols = _columns(xt, xc, wt, wc, "fc_grouped")
     N, (G, O) = x.shape[0], w.shape[:2]
     M = N if rows is None else rows.numel()
+    _sizes("fc_grouped", M, G, O, cols)
     bp = _on(bias, "bias", device, torch.float32, (G, O))
     op = _on(offsets, "offsets", device, torch.int32, (G + 1,))
     rp = _on(rows, "rows", device, torch.int32)
@@ -576,6 +585,7 @@ def cnn_combine_fwd(x, slot, weight, y=None, stream=None):
     if x.dim() != 2 or slot.dim() != 2:
         raise ValueError("combine: x must be [M][D], slot [N][k]")
     (M, D), (N, k) = x.shape, slot.shape
+    _sizes("combine", N, k)
     code = _wide(x.dtype, "x")
     xp = _on(x, "x", device)
     sp = _on(slot, "slot", device, torch.int32)

@@ -177,7 +177,8 @@ int check_grouped(const char* what, const GroupedFc& p) {
     if (p.M != 0 && p.N == 0) return fail(CNN_ERR_INVALID, "%s: %d rows of y from no row of x", what, p.M);
     if (too_big(p.N, p.I) || too_big(p.M, p.O) || too_big(p.O, p.I))
         return fail(CNN_ERR_UNSUPPORTED, "%s: x, y or a weight matrix exceeds 2^31-1 elements", what);
-    if (p.G > (1 << 20)) return fail(CNN_ERR_UNSUPPORTED, "%s: %d groups", what, p.G);
+    if (p.G > (1 << 20) || too_big(p.G, ceil_div64(p.O, 16)))
+        return fail(CNN_ERR_UNSUPPORTED, "%s: %d groups of %d outputs", what, p.G, p.O);
     if (p.x_type == CNN_MX4 ? !aligned(p.x, 16) : !aligned(p.x, type_bytes(p.x_type)))
         return fail(CNN_ERR_UNSUPPORTED, "%s: x not aligned", what);
     if (p.w_type == CNN_MX4 ? !aligned(p.w, 16) : !aligned(p.w, type_bytes(p.w_type)))
@@ -194,7 +195,7 @@ int check_route(int type, int T, int E, int k) {
     if (T < 0 || E <= 0 || k <= 0 || k > E) return fail(CNN_ERR_INVALID, "route: T=%d E=%d k=%d", T, E, k);
     if (E > kMaxExperts || k > kMaxChoices)
         return fail(CNN_ERR_UNSUPPORTED, "route: %d experts, %d choices: at most %d and %d", E, k, kMaxExperts, kMaxChoices);
-    if (too_big(T, E) || T > (1 << 27)) return fail(CNN_ERR_UNSUPPORTED, "route: %d tokens", T);
+    if (too_big(T, E) || T > (1 << 26)) return fail(CNN_ERR_UNSUPPORTED, "route: %d tokens", T);
     return CNN_OK;
 }
 
@@ -741,7 +742,7 @@ int run_grouped(const char* what, const GroupedFc& p, void* ws, size_t ws_bytes,
     const size_t need = fc_grouped_workspace(p);
     if (need > 0 && (!ws || ws_bytes < need))
         return fail(CNN_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", what, ws ? ws_bytes : 0, need);
-    if (!aligned(ws, 4)) return fail(CNN_ERR_UNSUPPORTED, "%s: workspace not aligned", what);
+    if (!aligned(ws, 16)) return fail(CNN_ERR_UNSUPPORTED, "%s: workspace not 16-byte aligned", what);
     return launch_fc_grouped(p, reinterpret_cast<float*>(ws), as_stream(stream));
 }
 

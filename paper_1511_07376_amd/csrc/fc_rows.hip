@@ -184,7 +184,7 @@ __device__ inline void rows_step(const GroupedFc& p, const char* const* wrow, co
 }
 
 template <int XT, int WT, int OT, int RT, int SS, int NW, bool THIN>
-__global__ void __launch_bounds__(64 * NW) fc_rows(GroupedFc p, int64_t units, int cols) {
+__global__ void __launch_bounds__(64 * NW) fc_rows(GroupedFc p, int units, int cols, FastDiv f_cols) {
     constexpr int ROWS = THIN ? kThin : 16 * RT, OUTS = 16 * OT;
     static_assert(!THIN || (RT == 1 && XT != CNN_MX4), "thin rows are wide");
     using TR = ThinRows<XT, WT, SS>;
@@ -199,8 +199,8 @@ __global__ void __launch_bounds__(64 * NW) fc_rows(GroupedFc p, int64_t units, i
     const int64_t span = SS * 128;
     const int64_t full = p.I / span, steps = (p.I + span - 1) / span;
     for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-        const int g = (int)(u / cols);
-        const int o0 = (int)(u % cols) * OUTS;
+        const int g = (int)fdiv((unsigned)u, f_cols);
+        const int o0 = ((int)u - g * cols) * OUTS;
         int lo = 0, hi = p.M;
         if (p.offsets) group_rows(p.offsets, g, p.M, lo, hi);
         const char* wrow[OT];
@@ -270,8 +270,9 @@ __global__ void __launch_bounds__(64 * NW) fc_rows(GroupedFc p, int64_t units, i
 template <int XT, int WT, int OT, int RT, int SS, int NW, bool THIN>
 void start(const GroupedFc& p, hipStream_t st) {
     const int cols = ceil_div(p.O, 16 * OT);
-    const int64_t units = (int64_t)p.G * cols;
-    enqueue(fc_rows<XT, WT, OT, RT, SS, NW, THIN>, dim3((unsigned)std::min<int64_t>(units, 1 << 22)), dim3(64 * NW), 0, st, p, units, cols);
+    const int units = p.G * cols;  // below 2^31: checked with the call's arguments
+    enqueue(fc_rows<XT, WT, OT, RT, SS, NW, THIN>, dim3((unsigned)std::min(units, 1 << 22)), dim3(64 * NW), 0, st, p, units, cols,
+            make_fastdiv(cols));
 }
 
 // The variant of a call.  Wide weights: a workgroup of 8 waves for 16 outputs.

@@ -155,8 +155,11 @@ struct TileFinder {
                 const int at = __builtin_ctzll(past);
                 const int first = t - before - (__shfl(incl, at) - __shfl(tiles, at));
                 g = __builtin_amdgcn_readfirstlane(base + at);
-                row0 = __builtin_amdgcn_readfirstlane(__shfl(lo, at) + first * TM);
-                hi = __builtin_amdgcn_readfirstlane(__shfl(end, at));
+                // offsets that are not in order can make more tiles than an int counts
+                if ((unsigned)first < (unsigned)__shfl(tiles, at)) {
+                    row0 = __builtin_amdgcn_readfirstlane(__shfl(lo, at) + first * TM);
+                    hi = __builtin_amdgcn_readfirstlane(__shfl(end, at));
+                }
                 return;
             }
             before += __builtin_amdgcn_readlane(incl, 63);
@@ -565,7 +568,7 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) fc_tiles(TileParams tp) {
                         const bool none = sRow[r] < 0;
 #pragma unroll
                         for (int c = 0; c < 8; ++c) v[c] = none ? 0.0f : v[c];
-                        if ((int64_t)row0 + r < hi && count > 0) put((size_t)(row0 + r) * p.O + oc, r, v);
+                        if ((int64_t)row0 + r < hi && count > 0) put((size_t)((int64_t)row0 + r) * p.O + oc, r, v);
                     }
                     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
                     __builtin_amdgcn_wave_barrier();

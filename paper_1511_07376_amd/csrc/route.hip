@@ -236,17 +236,25 @@ __global__ void __launch_bounds__(kThreads) route_scan(int32_t* counts, int grou
     const int64_t run = (groups + kWaves - 1) / kWaves;
     const int64_t lo = std::min<int64_t>(wave * run, groups), hi = std::min<int64_t>(lo + run, groups);
     int s = 0;
-    if (e < E)
+    if (e < E) {
+#pragma unroll 8
         for (int64_t g = lo; g < hi; ++g) s += counts[g * E + e];
+    }
     part[wave][lane] = s;
     __syncthreads();
     if (e >= E) return;
     int at = 0;
     for (int w = 0; w < wave; ++w) at += part[w][lane];
-    for (int64_t g = lo; g < hi; ++g) {
-        const int v = counts[g * E + e];
-        counts[g * E + e] = at;
-        at += v;
+    constexpr int BATCH = 8;  // loads on their way before the first store
+    for (int64_t g = lo; g < hi; g += BATCH) {
+        int v[BATCH];
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) v[i] = g + i < hi ? counts[(g + i) * E + e] : 0;
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            if (g + i < hi) counts[(g + i) * E + e] = at;
+            at += v[i];
+        }
     }
     if (wave == kWaves - 1) counts[(int64_t)groups * E + e] = at;
 }
@@ -340,13 +348,13 @@ void run_route_type(const RouteParams& p, hipStream_t st) {
 // a row of y and so 16 bytes of each of its k rows of x.
 template <typename T>
 __global__ void __launch_bounds__(256)
-combine_rows(const T* x, int M, int D, const int32_t* slot, const float* weight, int64_t items, int k, T* y,
-             int chunks) {
+combine_rows(const T* x, int M, int D, const int32_t* slot, const float* weight, unsigned items, int k, T* y,
+             int chunks, FastDiv f_chunks) {
     constexpr int N = 16 / (int)sizeof(T);
-    const int64_t step = (int64_t)gridDim.x * 256;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < items; i += step) {
-        const int64_t t = i / chunks;
-        const int d = (int)(i - t * chunks) * N;
+    const unsigned step = gridDim.x * 256;  // items and a step below 2^31: no wrap
+    for (unsigned i = blockIdx.x * 256 + threadIdx.x; i < items; i += step) {
+        const int64_t t = fdiv(i, f_chunks);
+        const int d = (int)(i - (unsigned)t * chunks) * N;
         const bool whole = d + N <= D;
         float acc[N];
 #pragma unroll
@@ -386,9 +394,9 @@ combine_rows(const T* x, int M, int D, const int32_t* slot, const float* weight,
 template <typename T>
 void run_combine(const T* x, int M, int D, const int32_t* slot, const float* weight, int N, int k, T* y, hipStream_t st) {
     const int chunks = ceil_div(D, 16 / (int)sizeof(T));
-    const int64_t items = (int64_t)N * chunks;
+    const unsigned items = (unsigned)N * chunks;  // no more than the elements of y
     enqueue(combine_rows<T>, dim3((unsigned)std::min<int64_t>(ceil_div64(items, 256), 1 << 20)), dim3(256), 0, st, x, M,
-            D, slot, weight, items, k, y, chunks);
+            D, slot, weight, items, k, y, chunks, make_fastdiv(chunks));
 }
 
 }  // namespace

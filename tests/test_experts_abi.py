@@ -52,6 +52,8 @@ def _fc(**kw):
     (dict(N=70000, I=70000), UNS), (dict(O=70000, I=70000), UNS), (dict(N=70000, O=70000), UNS),
     (dict(w=FAKE + 4), UNS), (dict(x=FAKE + 1), UNS), (dict(y=FAKE + 1), UNS), (dict(bias=FAKE + 2), UNS),
     (dict(xt=MX4, xs=FAKE, x=FAKE + 8, yt=F32), UNS),
+    (dict(N=64, I=9216, O=4096, work=0, n=1 << 30), WS),  # a split reduction without its workspace
+    (dict(N=64, I=9216, O=4096, work=FAKE, n=1024), WS), (dict(N=64, I=9216, O=4096, work=FAKE + 4, n=1 << 30), UNS),
     (dict(N=0, x=0, y=0), cnn.CNN_OK),
 ])
 def test_fc_mx4_refuses(kw, status):
@@ -74,7 +76,7 @@ def _grouped(**kw):
     (dict(xt=MX4, xs=FAKE), INV),                        # mx4 inputs, wide weights
     (dict(wt=MX4), INV), (dict(ws=FAKE), INV), (dict(yt=F16), INV),
     (dict(M=-1), INV), (dict(N=0, M=6), INV), (dict(I=0), INV),
-    (dict(G=(1 << 20) + 1), UNS), (dict(M=70000, O=70000), UNS), (dict(rows=FAKE + 2), UNS), (dict(offsets=FAKE + 1), UNS),
+    (dict(G=(1 << 20) + 1), UNS), (dict(G=1 << 20, O=40000, I=1, N=1, M=1), UNS), (dict(M=70000, O=70000), UNS), (dict(rows=FAKE + 2), UNS), (dict(offsets=FAKE + 1), UNS),
     (dict(M=0, N=0, x=0, y=0, rows=0), cnn.CNN_OK),
 ])
 def test_fc_grouped_refuses(kw, status):
@@ -92,7 +94,7 @@ def _route(**kw):
 
 @pytest.mark.parametrize("kw,status", [
     (dict(t=MX4), INV), (dict(T=-1), INV), (dict(E=0), INV), (dict(k=0), INV), (dict(k=9), INV),
-    (dict(E=1025), UNS), (dict(E=100, k=65), UNS), (dict(T=(1 << 27) + 1, E=1, k=1), UNS), (dict(T=1 << 25, E=1000), UNS),
+    (dict(E=1025), UNS), (dict(E=100, k=65), UNS), (dict(T=(1 << 26) + 1, E=1, k=1), UNS), (dict(T=1 << 25, E=1000), UNS),
     (dict(logits=0), INV), (dict(expert=0), INV), (dict(weight=0), INV), (dict(rows=0), INV), (dict(offsets=0), INV),
     (dict(slot=0), INV), (dict(logits=FAKE + 2), UNS), (dict(ws=FAKE + 2), UNS),
     (dict(ws=0), WS), (dict(n=5 * 8 * 4 - 1), WS),       # four workgroups of 32 tokens and the totals
@@ -100,6 +102,14 @@ def _route(**kw):
 def test_route_refuses(kw, status):
     assert _route(**kw) == status
     assert cnn.cnn_last_error().startswith("route")
+
+
+def test_fc_workspaces():
+    assert L.cnn_fc_mx4_workspace_bytes(BF16, 1, 4096, 4096) == 0
+    assert 0 < L.cnn_fc_mx4_workspace_bytes(F32, 64, 9216, 4096) <= 64 << 20
+    assert L.cnn_fc_mx4_workspace_bytes(7, 64, 9216, 4096) == 0 and L.cnn_fc_mx4_workspace_bytes(F32, 64, 0, 4096) == 0
+    assert 0 < L.cnn_fc_grouped_workspace_bytes(BF16, 4096, 8192, 8, BF16, 4096) <= 64 << 20
+    assert L.cnn_fc_grouped_workspace_bytes(BF16, 4096, 8192, 8, F16, 4096) == 0
 
 
 def test_route_workspace():

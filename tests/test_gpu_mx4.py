@@ -218,6 +218,7 @@ def test_fc_mx4_shapes_strides_and_empty(gpu):
     want, s = ref.product(odd, ref.values(w1, ws1, 71), None, False)
     ref.assert_product(gpu.cnn_fc_mx4_fwd(odd, w1, ws1), want, s, 71, "odd rows")
     assert gpu.cnn_fc_mx4_fwd(x[:0], w, ws).shape == (0, 40)
+    assert gpu.cnn_fc_mx4_fwd(torch.empty((0, 2, 6, 6), device="cuda"), w, ws).shape == (0, 40)
     with pytest.raises(TypeError):
         gpu.cnn_fc_mx4_fwd(randn((72, 6), g).t(), w, ws)
     with pytest.raises(ValueError):
@@ -230,6 +231,14 @@ def test_fc_mx4_shapes_strides_and_empty(gpu):
         gpu.cnn_fc_mx4_fwd(randn((6, 72), g), w, ws, bias=torch.zeros(39, device="cuda"))
     with pytest.raises(TypeError):
         gpu.cnn_fc_mx4_fwd(randn((6, 72), g), w, ws, y=torch.empty((6, 40), device="cuda", dtype=torch.float16))
+
+
+def test_sizes_past_the_limit_are_refused(gpu):
+    x = torch.empty(2**31 + 64, dtype=torch.bfloat16, device="cuda").reshape(-1, 32)
+    with pytest.raises(gpu.CnnError):
+        gpu.cnn_mx4_quantize(x)
+    with pytest.raises(gpu.CnnError):
+        gpu.cnn_combine_fwd(x, torch.zeros((1, 1), dtype=torch.int32, device="cuda"), torch.zeros((1, 1), device="cuda"))
 
 
 def test_fc_mx4_rows_past_32_bits(gpu):
