@@ -87,6 +87,29 @@ def test_fc_grouped(gpu, dtype, kind, i, o, sizes):
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("kind", ["wide", "mx4"])
+@pytest.mark.parametrize("sizes,i,o", [([3000, 0, 1300], 272, 6200), ([2300, 1], 1032, 2300), ([700, 400, 0, 900], 101, 3000)])
+def test_fc_grouped_large(gpu, dtype, kind, sizes, i, o):
+    """Rows and outputs for the larger tiles, the last of them split along the reduction; weights at an address that
+    is aligned to their elements only."""
+    g = gen(i + o)
+    w, ws, wv = make_weights(kind, len(sizes), o, i, g, dtype)
+    b = 0.1 * randn((len(sizes), o), g)
+    m = sum(sizes)
+    offsets = ints([0] + list(torch.tensor(sizes).cumsum(0)))
+    x = randn((m // 3, i), g, dtype)
+    rows = torch.randint(-1, m // 3, (m + 5,), generator=g, device="cuda", dtype=torch.int32)
+    y = torch.full((m + 5, o), 2.0, device="cuda", dtype=dtype)
+    gpu.cnn_fc_grouped_fwd(x, w, offsets, b, True, rows=rows, w_scale=ws, y=y)
+    check_grouped(y, x, wv, offsets, rows, b, True, f"{dtype} {kind}", untouched=2.0)
+    if kind == "wide":
+        flat = torch.empty(w.numel() + 1, dtype=dtype, device="cuda")
+        flat[1:] = w.reshape(-1)
+        again = gpu.cnn_fc_grouped_fwd(x, flat[1:].view(w.shape), offsets, b, True, rows=rows)
+        check_grouped(again, x, wv, offsets, rows, b, True, f"{dtype} unaligned")
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
 @pytest.mark.parametrize("sizes", list(SIZES.values()), ids=list(SIZES))
 @pytest.mark.parametrize("i,o", [(96, 64), (333, 190)])
 def test_fc_grouped_of_mx4_inputs(gpu, dtype, sizes, i, o):

@@ -140,6 +140,33 @@ def test_fc_mx4_of_mx4_inputs(gpu, dtype, n, i, o):
     ref.assert_product(y, want, s, i, f"mx4 to {dtype} {n}x{i}x{o}")
 
 
+def off_by_one(x):
+    """The same tensor at an address that is aligned to its elements only."""
+    flat = torch.empty(x.numel() + 1, dtype=x.dtype, device=x.device)
+    flat[1:] = x.reshape(-1)
+    return flat[1:].view(x.shape)
+
+
+# enough rows and outputs for the larger tiles, with and without a tail that is split along the reduction
+LARGE = [(2100, 304, 4100), (4200, 136, 4100), (4200, 1032, 4100), (1500, 2048, 2100)]
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("n,i,o", LARGE)
+def test_fc_mx4_large(gpu, dtype, n, i, o):
+    g = gen(n + i + o)
+    x = randn((n, i), g, dtype, spread=0.5)
+    w, ws = ref.random_mx4((o,), i, g)
+    b = 0.1 * randn((o,), g)
+    wv = ref.values(w, ws, i)
+    want, s = ref.product(x, wv, b, True)
+    ref.assert_product(gpu.cnn_fc_mx4_fwd(x, w, ws, b, True), want, s, i, f"{dtype} {n}x{i}x{o}")
+    ref.assert_product(gpu.cnn_fc_mx4_fwd(off_by_one(x), w, ws, b, True), want, s, i, f"{dtype} {n}x{i}x{o} unaligned")
+    xq, xs = gpu.cnn_mx4_quantize(x)
+    want, s = ref.product(ref.values(xq, xs, i), wv, b, False)
+    ref.assert_product(gpu.cnn_fc_mx4_fwd(xq, w, ws, b, x_scale=xs, y_dtype=dtype), want, s, i, f"mx4 to {dtype} {n}x{i}x{o}")
+
+
 @pytest.mark.parametrize("n", [1, 40, 300])
 @pytest.mark.parametrize("dtype", TYPES, ids=IDS)
 def test_fc_mx4_is_the_same_from_call_to_call(gpu, n, dtype):
