@@ -12,6 +12,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import functools
 import os
 from dataclasses import dataclass
 from typing import Dict, List, Optional, Sequence, Tuple
@@ -345,6 +346,9 @@ def cnn_softmax_fwd(x, y=None, stream=None):
 _WIDE = {torch.float32: CNN_F32, torch.bfloat16: CNN_BF16, torch.float16: CNN_F16}
 
 
+_INT_MAX = 0x7fffffff
+
+
 def _on(t, name: str, device: torch.device, dtype=None, shape=None):
     """Device pointer of a contiguous tensor on `device`, of this type and shape where given; None for None."""
     if t is None:
@@ -370,14 +374,19 @@ def _wide(dtype, name: str) -> int:
 def _gpu(t, name: str) -> torch.device:
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a GPU tensor")
-    _sizes(name, t.numel())
+    if t.numel() > _INT_MAX:
+        _too_large(name)
     return t.device
 
 
-def _sizes(name: str, *sizes: int) -> None:
+def _too_large(name: str):
     """Sizes are passed as int: none is cut to one that fits."""
-    if max(sizes) > 0x7fffffff:
-        raise CnnError(CNN_ERR_UNSUPPORTED, f"{name}: a size of {max(sizes)}, above 2^31-1")
+    raise CnnError(CNN_ERR_UNSUPPORTED, f"{name}: a size above 2^31-1")
+
+
+# what a workspace takes is a matter of sizes and types alone
+_fc_mx4_workspace = functools.lru_cache(maxsize=4096)(lib.cnn_fc_mx4_workspace_bytes)
+_fc_grouped_workspace = functools.lru_cache(maxsize=4096)(lib.cnn_fc_grouped_workspace_bytes)
 
 
 # the current GPU and stream as numbers, in a tenth of torch.cuda.current_stream()'s time
@@ -494,7 +503,8 @@ def cnn_fc_mx4_fwd(x, w, w_scale, bias=None, fuse_relu=False, x_scale=None, y_dt
     wp, ws, wt, wc = _operand(w, w_scale, device, "w")
     cols = _columns(xt, xc, wt, wc, "fc_mx4")
     N, O = x.shape[0], w.shape[0]
-    _sizes("fc_mx4", O, cols)
+    if O > _INT_MAX or cols > _INT_MAX:
+        _too_large("fc_mx4")
     bp = _on(bias, "bias", device, torch.float32, (O,))
     dtype = x.dtype if xs is None else y_dtype or torch.float32
     st = _raw_stream(device.index)
@@ -503,7 +513,7 @@ def cnn_fc_mx4_fwd(x, w, w_scale, bias=None, fuse_relu=False, x_scale=None, y_dt
         yp = y.data_ptr()
     else:
         yp = _on(y, "y", device, dtype, (N, O))
-    need = lib.cnn_fc_mx4_workspace_bytes(xt, N, cols, O)
+    need = _fc_mx4_workspace(xt, N, cols, O)
     work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
     _ok(lib.cnn_fc_mx4_fwd(xp, xs, xt, N, cols, wp, ws, bp, O, 1 if fuse_relu else 0,
                            yp, _WIDE.get(dtype, -1),
@@ -529,7 +539,8 @@ def cnn_fc_grouped_fwd(x, w, offsets, bias=None, fuse_relu=False, rows=None, w_s
     cols = _columns(xt, xc, wt, wc, "fc_grouped")
     N, (G, O) = x.shape[0], w.shape[:2]
     M = N if rows is None else rows.numel()
-    _sizes("fc_grouped", M, G, O, cols)
+    if max(M, G, O, cols) > _INT_MAX:
+        _too_large("fc_grouped")
     bp = _on(bias, "bias", device, torch.float32, (G, O))
     op = _on(offsets, "offsets", device, torch.int32, (G + 1,))
     rp = _on(rows, "rows", device, torch.int32)
@@ -540,7 +551,7 @@ def cnn_fc_grouped_fwd(x, w, offsets, bias=None, fuse_relu=False, rows=None, w_s
         yp = y.data_ptr()
     else:
         yp = _on(y, "y", device, dtype, (M, O))
-    need = lib.cnn_fc_grouped_workspace_bytes(xt, cols, M, G, wt, O)
+    need = _fc_grouped_workspace(xt, cols, M, G, wt, O)
     work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
     _ok(lib.cnn_fc_grouped_fwd(xp, xs, xt, N, cols, rp, M, op, G, wp, ws, wt, bp, O, 1 if fuse_relu else 0,
                                yp, _WIDE.get(dtype, -1),
@@ -563,16 +574,18 @@ def cnn_route_fwd(logits, k, renormalize=False, stream=None):
     lp = _on(logits, "logits", device)
     need = lib.cnn_route_workspace_bytes(T, E, k)
     st = _raw_stream(device.index)
-    n = max(T * k, 0)
-    expert = torch.empty((T, max(k, 0)), dtype=torch.int32, device=device)
-    weight = torch.empty((T, max(k, 0)), dtype=torch.float32, device=device)
-    slot = torch.empty((T, max(k, 0)), dtype=torch.int32, device=device)
-    rows = torch.empty(n, dtype=torch.int32, device=device)
-    offsets = torch.empty(E + 1, dtype=torch.int32, device=device)
+    n = T * k
+    if k <= 0 or n > _INT_MAX:
+        _ok(lib.cnn_route_fwd(None, code, T, E, k, 0, None, None, None, None, None, None, 0, None))  # says why not
+        _too_large("route")
+    # one allocation: what is handed out are parts of it
+    parts = torch.empty(4 * n + E + 1, dtype=torch.int32, device=device)
+    expert, slot, rows, weight, offsets = parts.split_with_sizes((n, n, n, n, E + 1))
+    base = parts.data_ptr()
     ws = torch.empty(need, dtype=torch.uint8, device=device) if need else None
-    _ok(lib.cnn_route_fwd(lp, code, T, E, k, 1 if renormalize else 0, expert.data_ptr(), weight.data_ptr(),
-                          rows.data_ptr(), offsets.data_ptr(), slot.data_ptr(),
-                          ws.data_ptr() if need else None, need, st))
+    _ok(lib.cnn_route_fwd(lp, code, T, E, k, 1 if renormalize else 0, base, base + 12 * n, base + 8 * n,
+                          base + 16 * n, base + 4 * n, ws.data_ptr() if need else None, need, st))
+    expert, slot, weight = expert.view(T, k), slot.view(T, k), weight.view(torch.float32).view(T, k)
     return expert, weight, rows, offsets, slot
 
 
@@ -585,7 +598,8 @@ def cnn_combine_fwd(x, slot, weight, y=None, stream=None):
     if x.dim() != 2 or slot.dim() != 2:
         raise ValueError("combine: x must be [M][D], slot [N][k]")
     (M, D), (N, k) = x.shape, slot.shape
-    _sizes("combine", N, k)
+    if N > _INT_MAX or k > _INT_MAX:
+        _too_large("combine")
     code = _wide(x.dtype, "x")
     xp = _on(x, "x", device)
     sp = _on(slot, "slot", device, torch.int32)
