@@ -639,7 +639,9 @@ __global__ void __launch_bounds__(256) fc_join(TileParams tp) {
 // A call's tile size (0: 64 x 128, 1: 128 x 128, 2: 256 x 256, or 128 x 256 for
 // inputs cut into parts).
 struct TileSize {
-    int rows, outs, slots;  // slots: workgroups that run at once on 256 compute units
+    int index, rows, outs;
+    int slots;              // workgroups that run at once on 256 compute units
+    int slab_ns, part_ns;   // as TileParams
 };
 
 template <int TM, int TN>
@@ -650,46 +652,37 @@ void start_join(const TileParams& tp, int64_t tiles, hipStream_t st) {
     else enqueue(fc_join<TM, TN, CNN_F16>, grid, block, 0, st, tp);
 }
 
-// Nanoseconds of a slab of a 64 x 128 tile: measured between reductions of 4096
-// and 9216 values, 64 rows (fp32 inputs that are cut 1150, fp16 ones 800, bf16 beside
-// 4-bit weights 475, 4 bits both 660), on the fp32 matrix cores their
-// own time.  Larger tiles take about as much more as they have products a
-// wave (256 x 256 in bf16: 1750).  Writing and joining a tile's part: 0.65 us a MB.
-template <int XT, int WT>
-constexpr int kSlabNs = XT == CNN_MX4 ? 660 : XT == CNN_F32 ? (WT == CNN_MX4 ? 1150 : 1000) : XT == CNN_F16 && WT == CNN_MX4 ? 800 : 475;
-
 template <int XT, int WT, int WM, int WN, int FM, int FN, bool VEC>
-void start_tiles(const GroupedFc& p, int slots, float* partial, hipStream_t st) {
+void start_tiles(const GroupedFc& p, const TileSize& size, float* partial, hipStream_t st) {
     using S = Slab<XT, WT, WM, WN, FM, FN, VEC>;
-    constexpr int kPartNs = S::TM * S::TN * 4 * 65 / 100000, kNs = kSlabNs<XT, WT> * (FM * FN) / 2;
     const int64_t values = XT == CNN_MX4 ? ((int64_t)p.I + 31) / 32 * 32 : p.I;
-    TileParams tp{p, ceil_div(p.O, S::TN), (int)ceil_div64(values, S::BK), S::ST, slots, partial, kNs, kPartNs, {}};
+    TileParams tp{p, ceil_div(p.O, S::TN), (int)ceil_div64(values, S::BK), S::ST, size.slots, partial, size.slab_ns, size.part_ns, {}};
     // groups end inside a tile: at most one more tile each
     const int64_t tiles = (ceil_div64(p.M, S::TM) + (p.offsets ? p.G : 0)) * tp.cols;
     if (!p.offsets) tp.tail = make_tail(tp, (int)tiles);
-    enqueue(fc_tiles<XT, WT, WM, WN, FM, FN, VEC>, dim3((unsigned)std::min<int64_t>(tiles + slots, 1 << 22)), dim3(S::NT), 0, st, tp);
+    enqueue(fc_tiles<XT, WT, WM, WN, FM, FN, VEC>, dim3((unsigned)std::min<int64_t>(tiles + size.slots, 1 << 22)), dim3(S::NT), 0, st, tp);
     if (partial && (p.offsets || tp.tail.parts > 1)) start_join<S::TM, S::TN>(tp, tiles, st);
 }
 
 template <int XT, int WT, bool VEC>
-void run_tiles(const GroupedFc& p, int size, int slots, float* partial, hipStream_t st) {
-    if (size == 0) start_tiles<XT, WT, 1, 4, 2, 1, VEC>(p, slots, partial, st);
-    else if (size == 1) start_tiles<XT, WT, 2, 2, 2, 2, VEC>(p, slots, partial, st);
-    else if constexpr (Slab<XT, WT, 2, 4, 4, 2, VEC>::kCut) start_tiles<XT, WT, 2, 4, 2, 2, VEC>(p, slots, partial, st);
-    else if constexpr (XT != CNN_MX4 && VEC) start_tiles<XT, WT, 2, 4, 4, 2, VEC>(p, slots, partial, st);
+void run_tiles(const GroupedFc& p, const TileSize& size, float* partial, hipStream_t st) {
+    if (size.index == 0) start_tiles<XT, WT, 1, 4, 2, 1, VEC>(p, size, partial, st);
+    else if (size.index == 1) start_tiles<XT, WT, 2, 2, 2, 2, VEC>(p, size, partial, st);
+    else if constexpr (Slab<XT, WT, 2, 4, 4, 2, VEC>::kCut) start_tiles<XT, WT, 2, 4, 2, 2, VEC>(p, size, partial, st);
+    else if constexpr (XT != CNN_MX4 && VEC) start_tiles<XT, WT, 2, 4, 4, 2, VEC>(p, size, partial, st);
 }
 
 // vec: rows of wide operands are whole 16-byte vectors.
 template <int XT, int WT>
-void run_tiles(const GroupedFc& p, int size, int slots, bool vec, float* partial, hipStream_t st) {
-    if (XT == CNN_MX4 || vec || Slab<XT, WT, 1, 4, 2, 1, true>::kCut) run_tiles<XT, WT, true>(p, size, slots, partial, st);
-    else if constexpr (XT != CNN_MX4 && !Slab<XT, WT, 1, 4, 2, 1, true>::kCut) run_tiles<XT, WT, false>(p, size, slots, partial, st);
+void run_tiles(const GroupedFc& p, const TileSize& size, bool vec, float* partial, hipStream_t st) {
+    if (XT == CNN_MX4 || vec || Slab<XT, WT, 1, 4, 2, 1, true>::kCut) run_tiles<XT, WT, true>(p, size, partial, st);
+    else if constexpr (XT != CNN_MX4 && !Slab<XT, WT, 1, 4, 2, 1, true>::kCut) run_tiles<XT, WT, false>(p, size, partial, st);
 }
 
-void run_tiles_f32(const GroupedFc&, int size, int slots, bool vec, float* partial, hipStream_t);
-void run_tiles_16(const GroupedFc&, int size, int slots, bool vec, float* partial, hipStream_t);
-void run_tiles_mx4(const GroupedFc&, int size, int slots, bool vec, float* partial, hipStream_t);
-void run_tiles_wide_mx4(const GroupedFc&, int size, int slots, bool vec, float* partial, hipStream_t);
-void run_tiles_cut(const GroupedFc&, int size, int slots, bool vec, float* partial, hipStream_t);
+void run_tiles_f32(const GroupedFc&, const TileSize&, bool vec, float* partial, hipStream_t);
+void run_tiles_16(const GroupedFc&, const TileSize&, bool vec, float* partial, hipStream_t);
+void run_tiles_mx4(const GroupedFc&, const TileSize&, bool vec, float* partial, hipStream_t);
+void run_tiles_wide_mx4(const GroupedFc&, const TileSize&, bool vec, float* partial, hipStream_t);
+void run_tiles_cut(const GroupedFc&, const TileSize&, bool vec, float* partial, hipStream_t);
 
 }  // namespace cnn

@@ -3,8 +3,8 @@
 
 namespace cnn {
 
-void run_tiles_mx4(const GroupedFc& p, int size, int slots, bool vec, float* partial, hipStream_t st) {
-    run_tiles<CNN_MX4, CNN_MX4>(p, size, slots, vec, partial, st);
+void run_tiles_mx4(const GroupedFc& p, const TileSize& size, bool vec, float* partial, hipStream_t st) {
+    run_tiles<CNN_MX4, CNN_MX4>(p, size, vec, partial, st);
 }
 
 }  // namespace cnn
