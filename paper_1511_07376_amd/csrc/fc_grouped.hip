@@ -33,18 +33,26 @@ bool whole_vectors(const GroupedFc& p) {
 // Inputs that are cut into parts beside 4-bit weights.
 bool cut_inputs(const GroupedFc& p) { return p.w_type == CNN_MX4 && (p.x_type == CNN_F32 || p.x_type == CNN_F16); }
 
-// A slab's nanoseconds on a 64 x 128 tile were measured between reductions of
-// 4096 and 9216 values, 64 rows: fp32 inputs that are cut 1150, fp16 ones 800,
-// bf16 beside 4-bit weights 475, 4 bits both 660; wide products in fp32 take the fp32
-// matrix cores' own time.  Larger tiles take about as much more as they have products a
-// wave (256 x 256 in bf16: 1750).  Writing and joining a part: 0.65 us a MB.
+// Of the smallest tiles the fp32 ones are bound by the matrix cores at any number of
+// rows: 32 rows up to 64 a group (128 tokens, 4 of 16 experts of 2048 x 2048: 85 us
+// against 150 on 64 rows), 64 above (900 tokens, 2 of 4 of 1000 x 2000: 78 against 90).
+//
+// A slab's nanoseconds with two workgroups a compute unit were measured between
+// reductions of 4096 and 9216 values, 64 rows: fp32 inputs that are cut 1150, fp16 ones
+// 800, bf16 beside 4-bit weights 475, 4 bits both 660.  Larger tiles take about as much
+// more as they have products a wave (256 x 256 in bf16: 1750).  One workgroup alone
+// is no faster (share 0.5: it waits half the time), but in fp32, where two take 1.1
+// (32 rows) to 1.7 times as long.  Writing and joining a part: 0.65 us a MB.
 TileSize tile_size(const GroupedFc& p, int index) {
-    const bool cut = cut_inputs(p), cut32 = cut && p.x_type == CNN_F32;
-    const int ns = p.x_type == CNN_MX4 ? 660 : cut32 ? 1150 : cut ? 800 : p.x_type == CNN_F32 ? 1000 : 475;
-    TileSize t = index == 0 ? TileSize{0, 64, 128, 512, ns, 0}
-               : index == 1 ? TileSize{1, 128, 128, cut32 ? 256 : 512, 2 * ns, 0}
-                            : TileSize{2, cut ? 128 : 256, 256, 256, (cut ? 2 : 4) * ns, 0};
-    t.part_ns = t.rows * t.outs * 4 * 65 / 100000;
+    const bool cut = cut_inputs(p), wide32 = p.w_type == CNN_F32, small32 = wide32 && ceil_div64(p.M, p.G) <= 64;
+    const float ns = p.x_type == CNN_MX4 ? 660 : wide32 ? 1300 : !cut ? 475 : p.x_type == CNN_F32 ? 1150 : 800;
+    const float share = wide32 ? 0.85f : 0.5f;
+    TileSize t;
+    if (index == 0) t = small32 ? TileSize{0, 32, 128, 512, 0, 1200, 0.55f, 0} : TileSize{0, 64, 128, 512, 0, ns, share, 0};
+    else if (index == 1) t = {1, 128, 128, 512, 0, 2 * ns, share, 0};
+    else t = {2, cut ? 128 : 256, 256, 256, 0, (cut ? 2 : 4) * ns, 1, 0};
+    t.room = std::min(2 * t.slots, (64 << 20) / (t.rows * t.outs * (int)sizeof(float)));  // no workspace above 64 MB
+    t.part_ns = (float)(t.rows * t.outs) * 4 * 0.00065f;
     return t;
 }
 
@@ -72,16 +80,23 @@ int choose_size(const GroupedFc& p) {
 // 41.9 us against 45.9 with a join that finds next to nothing to do.
 bool may_split(const GroupedFc& p, const TileSize& size) {
     TileParams tp{};
-    float some = 0.0f;
     tp.cols = ceil_div(p.O, size.outs);
     tp.slabs = ceil_div(p.I, p.x_type == CNN_MX4 ? 256 : p.w_type == CNN_F32 ? 32 : 64);
     tp.unroll = 4;
     tp.slots = size.slots;
-    tp.partial = &some;  // not written
+    tp.room = size.room;
     tp.slab_ns = size.slab_ns;
+    tp.share = size.share;
     tp.part_ns = size.part_ns;
     const int64_t row_tiles = ceil_div64(p.M, size.rows) + (p.offsets ? std::min(p.G, p.M) / 2 : 0);
     return make_tail(tp, (int)std::min<int64_t>(row_tiles * tp.cols, INT32_MAX)).parts > 1;
+}
+
+// The parts that the workspace holds for a call's tiles: 0 if none is split.
+int parts_held(const GroupedFc& p, const TileSize& size) {
+    if (!may_split(p, size)) return 0;
+    const int64_t tiles = (ceil_div64(p.M, size.rows) + (p.offsets ? p.G : 0)) * ceil_div(p.O, size.outs);
+    return (int)std::min<int64_t>(size.room, tiles * kMaxParts);
 }
 
 }  // namespace
@@ -89,9 +104,7 @@ bool may_split(const GroupedFc& p, const TileSize& size) {
 size_t fc_grouped_workspace(const GroupedFc& p) {
     if (p.M == 0 || few_rows(p)) return 0;
     const TileSize size = tile_size(p, choose_size(p));
-    if (!may_split(p, size)) return 0;
-    const int64_t tiles = (ceil_div64(p.M, size.rows) + (p.offsets ? p.G : 0)) * ceil_div(p.O, size.outs);
-    return (size_t)std::min<int64_t>(size.slots, tiles * kMaxParts) * size.rows * size.outs * sizeof(float);
+    return (size_t)parts_held(p, size) * size.rows * size.outs * sizeof(float);
 }
 
 int launch_fc_grouped(const GroupedFc& p, float* ws, hipStream_t st) {
@@ -99,14 +112,15 @@ int launch_fc_grouped(const GroupedFc& p, float* ws, hipStream_t st) {
     if (few_rows(p)) return run_fc_rows(p, st);
     const bool vec = whole_vectors(p);
     int index = choose_size(p);
-    float* partial = fc_grouped_workspace(p) > 0 ? ws : nullptr;
-    // rows of whole vectors at an address that is none: the 128 x 128 tiles need no more workspace
+    const size_t bytes = fc_grouped_workspace(p);
+    // rows of whole vectors at an address that is none
     if (index == 2 && !vec && !cut_inputs(p)) index = 1;
-    const TileSize size = tile_size(p, index);
-    if (p.x_type == CNN_MX4) run_tiles_mx4(p, size, vec, partial, st);
-    else if (p.w_type != CNN_MX4) p.x_type == CNN_F32 ? run_tiles_f32(p, size, vec, partial, st) : run_tiles_16(p, size, vec, partial, st);
-    else if (p.x_type == CNN_BF16) run_tiles_wide_mx4(p, size, vec, partial, st);
-    else run_tiles_cut(p, size, vec, partial, st);
+    TileSize size = tile_size(p, index);
+    size.room = std::min(parts_held(p, size), (int)(bytes / ((size_t)size.rows * size.outs * sizeof(float))));
+    if (p.x_type == CNN_MX4) run_tiles_mx4(p, size, vec, ws, st);
+    else if (p.w_type != CNN_MX4) p.x_type == CNN_F32 ? run_tiles_f32(p, size, vec, ws, st) : run_tiles_16(p, size, vec, ws, st);
+    else if (p.x_type == CNN_BF16) run_tiles_wide_mx4(p, size, vec, ws, st);
+    else run_tiles_cut(p, size, vec, ws, st);
     return check_launch("fc_tiles");
 }
 

@@ -25,7 +25,8 @@ namespace cnn {
 // The tiles of a call, of which only the last few (fewer than run at once) may
 // be split along the reduction: into `parts` runs of `run` slabs, so that the
 // tail keeps all compute units busy for part of a tile's time instead of some of
-// them for all of it.  (With few tiles the tail is all there is.)
+// them for all of it, or for one part more instead of one tile.  (With few tiles the
+// tail is all there is.)
 struct Tail {
     int full;  // tiles before it
     int tiles, parts, run;
@@ -40,37 +41,56 @@ struct TileParams {
     int slabs;       // slabs of the reduction
     int unroll;      // slabs the kernel takes at a time
     int slots;       // workgroups that run at once
-    float* partial;  // sums of the tail's parts, a tile each; NULL: no tile is split
-    int slab_ns;     // a slab's time, and that of a part of a tile to be written and
-    int part_ns;     // joined, on which the number of parts is chosen
+    int room;        // parts the workspace holds; 0: no tile is split
+    float* partial;  // sums of the tail's parts, a tile each
+    float slab_ns;   // what the number of parts is chosen on: a slab's time,
+    float share;     // how much of a compute unit's time a workgroup fills,
+    float part_ns;   // and the time of a part to be written and joined
     Tail tail;       // without groups: known to the host
 };
 
 constexpr int kMaxParts = 16;
-constexpr int kJoinNs = 3000;  // the second kernel's own time
+constexpr float kJoinNs = 3000;  // the second kernel's own time
+// The time of a tail in `parts`, as bits that compare like it, with the parts in the
+// lowest 4 (less one).
+__host__ __device__ inline unsigned tail_key(const TileParams& tp, int tiles, unsigned parts, int& run) {
+    const unsigned turns = ((unsigned)tp.slabs + tp.unroll - 1) / (unsigned)tp.unroll;
+    run = parts == 1 ? tp.slabs : (int)min((turns + parts - 1) / parts * (unsigned)tp.unroll, (unsigned)tp.slabs);
+    const unsigned got = ((unsigned)tp.slabs + run - 1) / (unsigned)run;
+    const float jobs = (float)tiles * (float)got;
+    const float each = (float)(((unsigned)jobs + 255) / 256);  // of a compute unit
+    float time = (float)run * tp.slab_ns * fmaxf(1.0f, each * tp.share);
+    if (got > 1) time += kJoinNs + jobs * tp.part_ns;
+    if (got != parts || (got > 1 && jobs > (float)tp.room)) time = 3e38f;
+    return (__builtin_bit_cast(unsigned, time) & ~15u) | (parts - 1);
+}
 __host__ __device__ inline Tail make_tail(const TileParams& tp, int tiles) {
     Tail t;
     t.full = (int)((unsigned)tiles / (unsigned)tp.slots) * tp.slots;
     t.tiles = tiles - t.full;
     t.parts = 1;
     t.run = tp.slabs;
-    if (tp.partial && t.tiles > 0) {
-        const unsigned turns = ((unsigned)tp.slabs + tp.unroll - 1) / (unsigned)tp.unroll;  // no part is shorter than one
-        unsigned most = (unsigned)tp.slots / (unsigned)t.tiles;
-        most = most < kMaxParts ? most : kMaxParts;
-        most = most < turns ? most : turns;
-        // slabs / parts * slab_ns + tiles * parts * part_ns is least at the root of their quotient
-        const float root = __builtin_sqrtf((float)tp.slabs * (float)tp.slab_ns / ((float)t.tiles * (float)tp.part_ns));
-        const unsigned parts = root < (float)most ? (unsigned)(root + 0.5f) : most;
-        if (parts > 1) {
-            const unsigned run = (turns + parts - 1) / parts * tp.unroll, got = ((unsigned)tp.slabs + run - 1) / run;
-            const float time = (float)run * tp.slab_ns + kJoinNs + (float)t.tiles * got * tp.part_ns;
-            if (time < (float)tp.slabs * tp.slab_ns) {
-                t.run = (int)run;
-                t.parts = (int)got;
-            }
-        }
+    if (tp.room == 0 || t.tiles == 0) return t;
+#ifdef __HIP_DEVICE_COMPILE__
+    // 16 lanes, a number of parts each
+    unsigned key = tail_key(tp, t.tiles, (threadIdx.x & 15) + 1, t.run);
+    const int run = t.run;
+    unsigned best = key;
+    best = min(best, (unsigned)__builtin_amdgcn_mov_dpp((int)best, 0x128, 0xf, 0xf, true));  // row_ror 8, 4, 2, 1
+    best = min(best, (unsigned)__builtin_amdgcn_mov_dpp((int)best, 0x124, 0xf, 0xf, true));
+    best = min(best, (unsigned)__builtin_amdgcn_mov_dpp((int)best, 0x122, 0xf, 0xf, true));
+    best = min(best, (unsigned)__builtin_amdgcn_mov_dpp((int)best, 0x121, 0xf, 0xf, true));
+    best = (unsigned)__builtin_amdgcn_readfirstlane((int)best);
+    t.parts = (int)(best & 15) + 1;
+    t.run = __builtin_amdgcn_readlane(run, t.parts - 1);
+#else
+    unsigned best = ~0u;
+    for (unsigned parts = 1; parts <= kMaxParts; ++parts) {
+        int run;
+        const unsigned key = tail_key(tp, t.tiles, parts, run);
+        if (key < best) best = key, t.parts = (int)parts, t.run = run;
     }
+#endif
     return t;
 }
 
@@ -636,12 +656,13 @@ __global__ void __launch_bounds__(256) fc_join(TileParams tp) {
     }
 }
 
-// A call's tile size (0: 64 x 128, 1: 128 x 128, 2: 256 x 256, or 128 x 256 for
-// inputs cut into parts).
+// A call's tile size (0: 64 x 128, or 32 x 128 in fp32, 1: 128 x 128, 2: 256 x 256, or
+// 128 x 256 for inputs cut into parts).
 struct TileSize {
     int index, rows, outs;
-    int slots;              // workgroups that run at once on 256 compute units
-    int slab_ns, part_ns;   // as TileParams
+    int slots;                      // workgroups that run at once on 256 compute units
+    int room;                       // parts of split tiles
+    float slab_ns, share, part_ns;  // as TileParams
 };
 
 template <int TM, int TN>
@@ -656,19 +677,22 @@ template <int XT, int WT, int WM, int WN, int FM, int FN, bool VEC>
 void start_tiles(const GroupedFc& p, const TileSize& size, float* partial, hipStream_t st) {
     using S = Slab<XT, WT, WM, WN, FM, FN, VEC>;
     const int64_t values = XT == CNN_MX4 ? ((int64_t)p.I + 31) / 32 * 32 : p.I;
-    TileParams tp{p, ceil_div(p.O, S::TN), (int)ceil_div64(values, S::BK), S::ST, size.slots, partial, size.slab_ns, size.part_ns, {}};
+    TileParams tp{p, ceil_div(p.O, S::TN), (int)ceil_div64(values, S::BK), S::ST, size.slots, size.room, partial, size.slab_ns, size.share, size.part_ns, {}};
     // groups end inside a tile: at most one more tile each
     const int64_t tiles = (ceil_div64(p.M, S::TM) + (p.offsets ? p.G : 0)) * tp.cols;
     if (!p.offsets) tp.tail = make_tail(tp, (int)tiles);
-    enqueue(fc_tiles<XT, WT, WM, WN, FM, FN, VEC>, dim3((unsigned)std::min<int64_t>(tiles + size.slots, 1 << 22)), dim3(S::NT), 0, st, tp);
-    if (partial && (p.offsets || tp.tail.parts > 1)) start_join<S::TM, S::TN>(tp, tiles, st);
+    enqueue(fc_tiles<XT, WT, WM, WN, FM, FN, VEC>, dim3((unsigned)std::min<int64_t>(tiles + size.room, 1 << 22)), dim3(S::NT), 0, st, tp);
+    if (size.room > 0 && (p.offsets || tp.tail.parts > 1)) start_join<S::TM, S::TN>(tp, tiles, st);
 }
 
 template <int XT, int WT, bool VEC>
 void run_tiles(const GroupedFc& p, const TileSize& size, float* partial, hipStream_t st) {
+    if constexpr (XT == CNN_F32 && WT == CNN_F32) {
+        if (size.rows == 32) return start_tiles<XT, WT, 1, 4, 1, 1, VEC>(p, size, partial, st);
+    }
     if (size.index == 0) start_tiles<XT, WT, 1, 4, 2, 1, VEC>(p, size, partial, st);
-    else if (size.index == 1) start_tiles<XT, WT, 2, 2, 2, 2, VEC>(p, size, partial, st);
     else if constexpr (Slab<XT, WT, 2, 4, 4, 2, VEC>::kCut) start_tiles<XT, WT, 2, 4, 2, 2, VEC>(p, size, partial, st);
+    else if (size.index == 1) start_tiles<XT, WT, 2, 2, 2, 2, VEC>(p, size, partial, st);
     else if constexpr (XT != CNN_MX4 && VEC) start_tiles<XT, WT, 2, 4, 4, 2, VEC>(p, size, partial, st);
 }
 
