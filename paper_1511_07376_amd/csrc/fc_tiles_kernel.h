@@ -656,10 +656,10 @@ __global__ void __launch_bounds__(256) fc_join(TileParams tp) {
     }
 }
 
-// A call's tile size (0: 64 x 128, or 32 x 128 in fp32, 1: 128 x 128, 2: 256 x 256, or
-// 128 x 256 for inputs cut into parts).
+// A call's tile size: 32 x 128, 64 x 128, 128 x 128 or 256 x 256; 32 x 128 or 128 x 256
+// for inputs cut into parts.
 struct TileSize {
-    int index, rows, outs;
+    int rows, outs;
     int slots;                      // workgroups that run at once on 256 compute units
     int room;                       // parts of split tiles
     float slab_ns, share, part_ns;  // as TileParams
@@ -687,12 +687,10 @@ void start_tiles(const GroupedFc& p, const TileSize& size, float* partial, hipSt
 
 template <int XT, int WT, bool VEC>
 void run_tiles(const GroupedFc& p, const TileSize& size, float* partial, hipStream_t st) {
-    if constexpr (XT == CNN_F32 && WT == CNN_F32) {
-        if (size.rows == 32) return start_tiles<XT, WT, 1, 4, 1, 1, VEC>(p, size, partial, st);
-    }
-    if (size.index == 0) start_tiles<XT, WT, 1, 4, 2, 1, VEC>(p, size, partial, st);
+    if (size.rows == 32) start_tiles<XT, WT, 1, 4, 1, 1, VEC>(p, size, partial, st);
     else if constexpr (Slab<XT, WT, 2, 4, 4, 2, VEC>::kCut) start_tiles<XT, WT, 2, 4, 2, 2, VEC>(p, size, partial, st);
-    else if (size.index == 1) start_tiles<XT, WT, 2, 2, 2, 2, VEC>(p, size, partial, st);
+    else if (size.rows == 64) start_tiles<XT, WT, 1, 4, 2, 1, VEC>(p, size, partial, st);
+    else if (size.outs == 128) start_tiles<XT, WT, 2, 2, 2, 2, VEC>(p, size, partial, st);
     else if constexpr (XT != CNN_MX4 && VEC) start_tiles<XT, WT, 2, 4, 4, 2, VEC>(p, size, partial, st);
 }
 
