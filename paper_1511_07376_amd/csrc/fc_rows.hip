@@ -36,14 +36,14 @@ struct ThinRows {
     static constexpr int kBytes = kPlanes * kThin * kRow;
 };
 
-template <int XT, int WT, int OT, int RT, int SS, bool THIN, bool FULL>
+template <int XT, int WT, int OT, int RT, int SS, bool THIN, bool ODD, bool FULL>
 __device__ inline void rows_step(const GroupedFc& p, const char* const* wrow, const uint8_t* const* wscale,
                                  const char* const* xrow, const uint8_t* const* xscale, char* thin, int64_t s, int nb,
                                  f32x4 (&acc)[OT][RT]) {
     const int lane = threadIdx.x & 63, l16 = lane & 15, quad = lane >> 4;
     constexpr int XLOADS = THIN && ThinRows<XT, WT, SS>::kCut ? 1 : kRunLoads<XT>;
     u32x4 w[OT][SS][kRunLoads<WT>];
-    unsigned ws[OT][SS], xs[RT][SS];
+    unsigned ws[OT][SS], xs[RT][SS];  // scales, or the last words of runs to be straightened
     u32x4 x[RT][SS][XLOADS];
     // block (32 values) of step t for this lane
     auto block = [&](int t) { return (s * SS + t) * 4 + quad; };
@@ -71,7 +71,7 @@ __device__ inline void rows_step(const GroupedFc& p, const char* const* wrow, co
             load_mx4(wrow[i], wscale[i], &w[i][0][0], ws[i]);
         } else {
 #pragma unroll
-            for (int t = 0; t < SS; ++t) load_run<WT, FULL>(wrow[i], block(t) * 32, p.I, w[i][t]);
+            for (int t = 0; t < SS; ++t) load_run<WT, FULL, ODD>(wrow[i], block(t) * 32, p.I, w[i][t], ws[i][t]);
         }
     }
     using TR = ThinRows<XT, WT, SS>;
@@ -119,12 +119,20 @@ __device__ inline void rows_step(const GroupedFc& p, const char* const* wrow, co
                 load_mx4(xrow[r], xscale[r], &x[r][0][0], xs[r]);
             } else {
 #pragma unroll
-                for (int t = 0; t < SS; ++t) load_run<XT, FULL>(xrow[r], block(t) * 32, p.I, x[r][t]);
+                for (int t = 0; t < SS; ++t) load_run<XT, FULL, ODD>(xrow[r], block(t) * 32, p.I, x[r][t], xs[r][t]);
             }
         }
     }
 #pragma unroll
     for (int t = 0; t < SS; ++t) {
+        if constexpr (WT != CNN_MX4) {
+#pragma unroll
+            for (int i = 0; i < OT; ++i) straighten_run<WT, FULL, ODD>(wrow[i], w[i][t], ws[i][t]);
+        }
+        if constexpr (XT != CNN_MX4 && !THIN) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r) straighten_run<XT, FULL, ODD>(xrow[r], x[r][t], xs[r][t]);
+        }
         if constexpr (XT == CNN_MX4) {
 #pragma unroll
             for (int i = 0; i < OT; ++i)
@@ -183,7 +191,7 @@ __device__ inline void rows_step(const GroupedFc& p, const char* const* wrow, co
     }
 }
 
-template <int XT, int WT, int OT, int RT, int SS, int NW, bool THIN>
+template <int XT, int WT, int OT, int RT, int SS, int NW, bool THIN, bool ODD>
 __global__ void __launch_bounds__(64 * NW) fc_rows(GroupedFc p, int units, int cols, FastDiv f_cols) {
     constexpr int ROWS = THIN ? kThin : 16 * RT, OUTS = 16 * OT;
     static_assert(!THIN || (RT == 1 && XT != CNN_MX4), "thin rows are wide");
@@ -238,8 +246,8 @@ __global__ void __launch_bounds__(64 * NW) fc_rows(GroupedFc p, int units, int c
                 none[c] = p.rows && source_row(p, (int)m) < 0;
             }
             int64_t s = wave;
-            for (; s < full; s += NW) rows_step<XT, WT, OT, RT, SS, THIN, true>(p, wrow, wscale, xrow, xscale, thin + wave * TR::kBytes * THIN, s, nb, acc);
-            if (s < steps) rows_step<XT, WT, OT, RT, SS, THIN, false>(p, wrow, wscale, xrow, xscale, thin + wave * TR::kBytes * THIN, s, nb, acc);
+            for (; s < full; s += NW) rows_step<XT, WT, OT, RT, SS, THIN, ODD, true>(p, wrow, wscale, xrow, xscale, thin + wave * TR::kBytes * THIN, s, nb, acc);
+            if (s < steps) rows_step<XT, WT, OT, RT, SS, THIN, ODD, false>(p, wrow, wscale, xrow, xscale, thin + wave * TR::kBytes * THIN, s, nb, acc);
 #pragma unroll
             for (int i = 0; i < OT; ++i)
 #pragma unroll
@@ -271,8 +279,16 @@ template <int XT, int WT, int OT, int RT, int SS, int NW, bool THIN>
 void start(const GroupedFc& p, hipStream_t st) {
     const int cols = ceil_div(p.O, 16 * OT);
     const int units = p.G * cols;  // below 2^31: checked with the call's arguments
-    enqueue(fc_rows<XT, WT, OT, RT, SS, NW, THIN>, dim3((unsigned)std::min(units, 1 << 22)), dim3(64 * NW), 0, st, p, units, cols,
-            make_fastdiv(cols));
+    const dim3 grid((unsigned)std::min(units, 1 << 22)), block(64 * NW);
+    constexpr bool kX16 = XT == CNN_BF16 || XT == CNN_F16, kW16 = kX16 && WT != CNN_MX4;
+    // rows of 16-bit values at addresses that are no multiples of 4 (thin ones of x: few loads)
+    if constexpr (kW16 || (kX16 && !THIN)) {
+        if (p.I % 2 || (uintptr_t)p.x % 4 || (kW16 && (uintptr_t)p.w % 4)) {
+            enqueue(fc_rows<XT, WT, OT, RT, SS, NW, THIN, true>, grid, block, 0, st, p, units, cols, make_fastdiv(cols));
+            return;
+        }
+    }
+    enqueue(fc_rows<XT, WT, OT, RT, SS, NW, THIN, false>, grid, block, 0, st, p, units, cols, make_fastdiv(cols));
 }
 
 // The variant of a call.  Wide weights: a workgroup of 8 waves for 16 outputs.
