@@ -109,6 +109,82 @@ def test_fc_grouped_large(gpu, dtype, kind, sizes, i, o):
         check_grouped(again, x, wv, offsets, rows, b, True, f"{dtype} unaligned")
 
 
+def one_behind(t):
+    """The same values, contiguous, one element behind an aligned address."""
+    flat = torch.empty(t.numel() + 1, dtype=t.dtype, device=t.device)
+    flat[1:] = t.reshape(-1)
+    return flat[1:].view(t.shape)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("kind", ["wide", "mx4"])
+@pytest.mark.parametrize("i", [1, 131, 517, 518, 1031, 4099])
+@pytest.mark.parametrize("sizes", [[2, 1, 0, 4], [9, 0, 7, 12], [6] * 9], ids=["thin", "few", "even"])
+def test_fc_grouped_few_rows_at_odd_addresses(gpu, dtype, kind, i, sizes):
+    """Rows that begin at any element, in streams of weights: the values beside them are NaN and infinite."""
+    g = gen(i + len(sizes))
+    o = 77
+    w, ws, wv = make_weights(kind, len(sizes), o, i, g, dtype)
+    m = sum(sizes)
+    offsets = ints([0] + list(torch.tensor(sizes).cumsum(0)))
+    x = randn((m, i), g, dtype)
+    want = gpu.cnn_fc_grouped_fwd(x, w, offsets, w_scale=ws)
+    check_grouped(want, x, wv, offsets, None, None, False, f"{dtype} {kind}")
+    for beside in (math.nan, math.inf):
+        def between(t):
+            flat = torch.full((t.numel() + 2,), beside, dtype=t.dtype, device="cuda")
+            flat[1:-1] = t.reshape(-1)
+            return flat[1:-1].view(t.shape)
+        xo, wo = between(x), between(w) if kind == "wide" else w
+        for a, b in ((xo, w), (x, wo), (xo, wo)):
+            y = gpu.cnn_fc_grouped_fwd(a, b, offsets, w_scale=ws)
+            check_grouped(y, x, wv, offsets, None, None, False, f"{dtype} {kind} beside {beside}")
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("kind", ["wide", "mx4", "mx4 both"])
+@pytest.mark.parametrize("sizes,i,o", [([17, 40, 0, 64, 31, 1, 33, 90], 610, 1013), ([33] * 3, 4136, 500), ([20, 25] * 40, 198, 600),
+                                       ([150, 0, 90], 521, 300), ([16, 9, 40, 0, 15] * 20, 40, 500)])
+def test_fc_grouped_some_rows_each(gpu, dtype, kind, sizes, i, o):
+    """Groups of some tens of rows: tiles of 32, with and without a split reduction."""
+    g = gen(i + o)
+    both = kind == "mx4 both"
+    w, ws, wv = make_weights("mx4" if both else kind, len(sizes), o, i, g, dtype)
+    b = 0.1 * randn((len(sizes), o), g)
+    m = sum(sizes)
+    offsets = ints([0] + list(torch.tensor(sizes).cumsum(0)))
+    rows = torch.randint(-1, m // 2, (m + 3,), generator=g, device="cuda", dtype=torch.int32)
+    y = torch.full((m + 3, o), 4.0, device="cuda", dtype=dtype)
+    if both:
+        xq, xs = ref.random_mx4((m // 2,), i, g)
+        gpu.cnn_fc_grouped_fwd(xq, w, offsets, b, True, rows=rows, w_scale=ws, x_scale=xs, y_dtype=dtype, y=y)
+        x = ref.values(xq, xs, i)
+    else:
+        x = randn((m // 2, i), g, dtype)
+        gpu.cnn_fc_grouped_fwd(x, w, offsets, b, True, rows=rows, w_scale=ws, y=y)
+        again = gpu.cnn_fc_grouped_fwd(one_behind(x), one_behind(w) if kind == "wide" else w, offsets, b, True, rows=rows, w_scale=ws)
+        check_grouped(again, x, wv, offsets, rows, b, True, f"{dtype} {kind} unaligned")
+    check_grouped(y, x, wv, offsets, rows, b, True, f"{dtype} {kind}", untouched=4.0)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("kind", ["wide", "mx4"])
+@pytest.mark.parametrize("each,i,o", [(125, 1024, 2100), (300, 2088, 2100), (575, 1536, 2100)])
+def test_fc_grouped_tails_in_rounds(gpu, dtype, kind, each, i, o):
+    """Tails of more tiles than half of what runs at once, split along the reduction; the number of tiles is not
+    the expected one where groups are uneven."""
+    for sizes in ([each] * 8, [each * 3, 0, 1, each * 4 - 1, 0, 0, each, 0]):
+        g = gen(each)
+        w, ws, wv = make_weights(kind, 8, o, i, g, dtype)
+        b = 0.1 * randn((8, o), g)
+        offsets = ints([0] + list(torch.tensor(sizes).cumsum(0)))
+        m = sum(sizes)
+        x = randn((m, i), g, dtype)
+        y = gpu.cnn_fc_grouped_fwd(x, w, offsets, b, True, w_scale=ws)
+        check_grouped(y, x, wv, offsets, None, b, True, f"{dtype} {kind} {sizes}")
+        assert torch.equal(gpu.cnn_fc_grouped_fwd(x, w, offsets, b, True, w_scale=ws), y)
+
+
 @pytest.mark.parametrize("dtype", TYPES, ids=IDS)
 @pytest.mark.parametrize("sizes", list(SIZES.values()), ids=list(SIZES))
 @pytest.mark.parametrize("i,o", [(96, 64), (333, 190)])
