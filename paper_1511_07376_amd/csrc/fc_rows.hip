@@ -10,6 +10,10 @@
 // are the matrix row, the rows of x the column: with one row of x the
 // matrix cores idle to 15/16, which costs nothing while the weights arrive.
 // A group of more than 16 RT rows takes as many passes over its weights.
+// Bound by HBM where weights are many (16 tokens, 4 of 64 experts of 2048 x 4096, bf16 on 4
+// bits: 185 MB in 33.5 us, 5.5 TB/s), by one chain of load, product and join where
+// they are few (one token, 4096 x 4096: 8.9 MB in 4.4 to 4.9 us, of which an empty
+// kernel takes 2.3).
 #include "fc_operands.h"
 
 #include <algorithm>

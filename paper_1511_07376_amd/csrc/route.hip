@@ -9,7 +9,10 @@
 // and a choice's place among them is the number of bits below its own: the
 // order does not depend on when an atomic lands.
 //
-// Up to 64 tokens, one workgroup does it all.  Above, one kernel chooses, 32
+// Bound by the choices' chains of instructions, not by the bytes (2 MB for 8192 tokens of
+// 64 experts in bf16, which take 6.1 us to choose 8 each from and 5.0 to place).
+//
+// Up to 64 tokens, one workgroup does it all (16 tokens, 4 of 128: 4.4 us).  Above, one kernel chooses, 32
 // tokens a workgroup (a wave takes two), and counts the choices of every expert
 // in them, and a second one adds up what stands before each 64 tokens and
 // places them.  Where that sum is
@@ -345,7 +348,9 @@ void run_route_type(const RouteParams& p, hipStream_t st) {
 
 // Combine: y[t, d] = sum_j weight[t, j] x[slot[t, j], d], sums in fp32, j
 // ascending.  Moves bytes and little else: a work-item takes 16 bytes of
-// a row of y and so 16 bytes of each of its k rows of x.
+// a row of y and so 16 bytes of each of its k rows of x (bf16, 4096 tokens of 8 rows of
+// 2048: 30 to 32 us, 4.7 to 5.0 TB/s; odd widths, whose vectors begin at any
+// element, take a sixth more).
 template <typename T>
 __global__ void __launch_bounds__(256)
 combine_rows(const T* x, int M, int D, const int32_t* slot, const float* weight, unsigned items, int k, T* y,
