@@ -88,9 +88,14 @@ TileSize tile_of(const GroupedFc& p, int rows, int outs) {
 // value is cut once a workgroup, so the one with the most outputs.
 //
 // Else the larger tile where there are enough of them for all compute units: 2048 x 4096 x
-// 4096 in bf16 on 4-bit weights 94, 77 and 106 us by size (512 of 128 x 128), 4096
-// x 8192 x 8192 644, 555 and 482 (512 of 256 x 256), 512 tokens, 2 of 8 experts of
-// 2048 x 2048 34, 38 and 56.
+// 4096 in bf16 on 4-bit weights 94, 77 and 106 us by size (512 of 128 x 128), 512 tokens, 2
+// of 8 experts of 2048 x 2048 34, 38 and 56.  256 x 256 of wide types where they also
+// fill the last round of compute units (4096 x 4096 x 4096 on 4-bit weights 129 against 147
+// on 128 x 128, 384 of them, 4096 x 2048 x 6144, 135 against 116), and with groups, whose
+// last tiles are half empty, in two rounds or more of 1024 rows each (4096 tokens, 2 of 8
+// experts of 4096 x 4096, bf16: 346 against 382; of 2048 x 2048 120 against 107; 8 of 64 of
+// 2048 x 1024 234 against 222).  In fp32 64 rows pad less of groups up to 512 (700 tokens,
+// 2 of 8 of 4096 x 4096: 474 against 533).
 TileSize choose_size(const GroupedFc& p) {
     const int64_t each = ceil_div64(p.M, p.G);
     const bool little = (float)p.M * p.I * p.O <= 3e9f;
@@ -99,8 +104,10 @@ TileSize choose_size(const GroupedFc& p) {
     const bool wide16 = p.w_type == CNN_BF16 || p.w_type == CNN_F16;
     if (each <= 32 || (little && !wide16 && tiles(32, 128) <= 512)) return tile_of(p, 32, 128);
     if (p.offsets && !wide16 && each <= (p.w_type == CNN_F32 ? 64 : 40)) return tile_of(p, 32, 128);
-    if (each <= 64) return tile_of(p, 64, 128);
-    if (p.x_type != CNN_MX4 && (int64_t)p.I * type_bytes(p.x_type) % 16 == 0 && tiles(256, 256) >= 256) return tile_of(p, 256, 256);
+    if (each <= (p.w_type == CNN_F32 ? 512 : 64)) return tile_of(p, 64, 128);
+    const int64_t most = tiles(256, 256), last = most % 256;
+    const bool large = p.offsets ? each >= 1024 && most >= 512 : most >= 1024 || (most >= 256 && (last == 0 || last >= 192));
+    if (p.x_type != CNN_MX4 && (int64_t)p.I * type_bytes(p.x_type) % 16 == 0 && large) return tile_of(p, 256, 256);
     return tiles(128, 128) >= 384 ? tile_of(p, 128, 128) : tile_of(p, 64, 128);
 }
 
