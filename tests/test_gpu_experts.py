@@ -186,6 +186,26 @@ def test_fc_grouped_tails_in_rounds(gpu, dtype, kind, each, i, o):
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("kind", ["wide", "mx4"])
+@pytest.mark.parametrize("sizes,i,o", [([2500, 0, 800], 136, 8800), ([1100, 1201, 999], 1096, 8800), ([1500, 1210, 1100], 2056, 8800), ([3810, 0, 0], 2056, 8800)])
+def test_fc_grouped_largest(gpu, dtype, kind, sizes, i, o):
+    """The largest tiles, in more than two rounds; operands at an address that is aligned to their elements only."""
+    g = gen(i + o)
+    w, ws, wv = make_weights(kind, 3, o, i, g, dtype)
+    b = 0.1 * randn((3, o), g)
+    m = sum(sizes)
+    offsets = ints([0] + list(torch.tensor(sizes).cumsum(0)))
+    x = randn((m // 2, i), g, dtype)
+    rows = torch.randint(-1, m // 2, (m + 2,), generator=g, device="cuda", dtype=torch.int32)
+    y = torch.full((m + 2, o), 2.0, device="cuda", dtype=dtype)
+    gpu.cnn_fc_grouped_fwd(x, w, offsets, b, True, rows=rows, w_scale=ws, y=y)
+    check_grouped(y, x, wv, offsets, rows, b, True, f"{dtype} {kind}", untouched=2.0)
+    del y
+    again = gpu.cnn_fc_grouped_fwd(one_behind(x), w, offsets, b, True, rows=rows, w_scale=ws)
+    check_grouped(again, x, wv, offsets, rows, b, True, f"{dtype} {kind} unaligned")
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
 @pytest.mark.parametrize("sizes", list(SIZES.values()), ids=list(SIZES))
 @pytest.mark.parametrize("i,o", [(96, 64), (333, 190)])
 def test_fc_grouped_of_mx4_inputs(gpu, dtype, sizes, i, o):

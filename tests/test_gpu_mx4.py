@@ -167,6 +167,20 @@ def test_fc_mx4_large(gpu, dtype, n, i, o):
     ref.assert_product(gpu.cnn_fc_mx4_fwd(xq, w, ws, b, x_scale=xs, y_dtype=dtype), want, s, i, f"mx4 to {dtype} {n}x{i}x{o}")
 
 
+@pytest.mark.parametrize("n,i,o", [(4000, 304, 4000), (3800, 136, 7900), (8100, 1032, 8300)])
+def test_fc_mx4_largest(gpu, n, i, o):
+    """The largest tiles: one whole round of them, a last one that is nearly whole, a tail that is split."""
+    g = gen(n + i + o)
+    x = randn((n, i), g, torch.bfloat16, spread=0.5)
+    w, ws = ref.random_mx4((o,), i, g)
+    b = 0.1 * randn((o,), g)
+    want, s = ref.product(x, ref.values(w, ws, i), b, True)
+    y = gpu.cnn_fc_mx4_fwd(x, w, ws, b, True)
+    ref.assert_product(y, want, s, i, f"{n}x{i}x{o}")
+    assert torch.equal(gpu.cnn_fc_mx4_fwd(x, w, ws, b, True), y)
+    ref.assert_product(gpu.cnn_fc_mx4_fwd(off_by_one(x), w, ws, b, True), want, s, i, f"{n}x{i}x{o} unaligned")
+
+
 @pytest.mark.parametrize("n", [1, 40, 300])
 @pytest.mark.parametrize("dtype", TYPES, ids=IDS)
 def test_fc_mx4_is_the_same_from_call_to_call(gpu, n, dtype):
