@@ -12,10 +12,10 @@
 // Bound, where there is work for all compute units, by the copies into LDS: 8192 x 4096 x
 // 4096 in bf16 takes 196 us for its copies alone on 256 x 256 tiles (11 TB/s, from
 // the L2s and behind them) and 280 on 128 x 128 (15), the products alone 213 (1290
-// TFLOP/s); together 4096 tokens, 2 of 8 experts of 4096 x 4096, take 345 (800 TFLOP/s).
-// 4 bits on both sides, 2048 x 9216 x 4096: 61 to 65 us (2.4 to 2.5 PFLOP/s).  With few
+// TFLOP/s); together 4096 tokens, 2 of 8 experts of 4096 x 4096, take 333 (825 TFLOP/s).
+// 4 bits on both sides, 2048 x 9216 x 4096: 59 to 63 us (2.5 to 2.6 PFLOP/s).  With few
 // workgroups bound by a slab's latency, and in fp32 by the matrix cores (4096 tokens, 2
-// of 8 of 2048 x 2048: 625 us, 110 of 154 TFLOP/s).
+// of 8 of 2048 x 2048: 553 us, 124 of 154 TFLOP/s).
 //
 // LDS rows are 32 to 256 bytes without padding (the copying loads write 64
 // consecutive vectors); the 16-byte vectors of a row are exchanged by an XOR with
