@@ -300,16 +300,21 @@ void start(const GroupedFc& p, hipStream_t st) {
 // flight a wave (one token, 4096 x 4096: 4.5 us; with 32 outputs a workgroup
 // 6.4); from 1024 workgroups on 32 outputs share the rows of x, and a wave
 // takes about four steps, so that fewer waves meet in LDS (16 tokens, 4 of 64
-// experts of 2048 x 4096: 38.7 us; 16 outputs and 8 waves 63).
+// experts of 2048 x 4096: 38.7 us; 16 outputs and 8 waves 63).  Short reductions leave
+// all but the first waves without a step (13 tokens, 6 of 115 experts of 64 x 2752: bf16
+// 39.9 us with 8 waves, 12.1 with 2, 8.7 with 1, on 4-bit weights 11.5 with 2, 8.1 with 1; of
+// 512 x 1000 18.6, 11.8 and 13.4; 40 tokens, 8 experts of 512 x 1024, fp32 on 4-bit
+// weights 7.0, 5.9 and 6.3).
 template <int XT, int WT>
 void choose(const GroupedFc& p, hipStream_t st) {
     const bool thin = XT != CNN_MX4 && ceil_div64(p.M, p.G) <= kThin;
+    // groups without rows cost next to nothing
+    const bool many = (int64_t)std::min(p.G, p.M) * ceil_div(p.O, 16) >= 1024;
     if constexpr (WT == CNN_MX4) {
-        // groups without rows cost next to nothing
-        const bool many = (int64_t)std::min(p.G, p.M) * ceil_div(p.O, 16) >= 1024;
         if constexpr (XT != CNN_MX4) {
             if (thin) {
-                if (!many) start<XT, WT, 1, 1, 2, 8, true>(p, st);
+                if (p.I <= 256) many ? start<XT, WT, 2, 1, 2, 1, true>(p, st) : start<XT, WT, 1, 1, 2, 1, true>(p, st);
+                else if (!many) p.I <= 512 ? start<XT, WT, 1, 1, 2, 2, true>(p, st) : start<XT, WT, 1, 1, 2, 8, true>(p, st);
                 else if (p.I <= 2048) start<XT, WT, 2, 1, 2, 2, true>(p, st);
                 else start<XT, WT, 2, 1, 2, 4, true>(p, st);
                 return;
@@ -322,12 +327,18 @@ void choose(const GroupedFc& p, hipStream_t st) {
                 return;
             }
         }
+        if constexpr (XT == CNN_MX4) {
+            // with more rows the epilogue takes 4 waves (58 groups of 16 rows, 145 x 384: 8.4 us against 9.9)
+            if (many && p.I <= 512 && ceil_div64(p.M, p.G) <= 8) return start<XT, WT, 2, 1, 2, 2, false>(p, st);
+        }
         if (many) start<XT, WT, 2, 1, 2, 4, false>(p, st);
+        else if (p.I <= 512) start<XT, WT, 1, 1, 2, 2, false>(p, st);
         else start<XT, WT, 1, 1, 2, 8, false>(p, st);
     } else {
         constexpr int SS = WT == CNN_F32 ? 1 : 2;  // 8 loads of a weight row in flight a lane
-        if (thin) start<XT, WT, 1, 1, 1, 8, true>(p, st);
-        else start<XT, WT, 1, 1, SS, 8, false>(p, st);
+        if (p.I <= 128) thin ? start<XT, WT, 1, 1, 1, 1, true>(p, st) : start<XT, WT, 1, 1, SS, 1, false>(p, st);
+        else if (p.I <= (WT == CNN_F32 && !many ? 512 : 1024)) thin ? start<XT, WT, 1, 1, 1, 2, true>(p, st) : start<XT, WT, 1, 1, SS, 2, false>(p, st);
+        else thin ? start<XT, WT, 1, 1, 1, 8, true>(p, st) : start<XT, WT, 1, 1, SS, 8, false>(p, st);
     }
 }
 

@@ -143,6 +143,27 @@ def test_fc_grouped_few_rows_at_odd_addresses(gpu, dtype, kind, i, sizes):
 
 @pytest.mark.parametrize("dtype", TYPES, ids=IDS)
 @pytest.mark.parametrize("kind", ["wide", "mx4", "mx4 both"])
+@pytest.mark.parametrize("sizes", [[1, 0, 3] * 60, [7, 0, 9, 20] * 30, [2, 5], [0, 11]], ids=["thin", "few", "thin2", "few2"])
+@pytest.mark.parametrize("i,o", [(32, 270), (128, 270), (129, 270), (256, 100), (500, 270), (513, 270), (1024, 100), (1025, 270)])
+def test_fc_grouped_short_reductions(gpu, dtype, kind, sizes, i, o):
+    """Reductions that a wave or two take, in many workgroups and in few."""
+    g = gen(i + len(sizes))
+    w, ws, wv = make_weights("wide" if kind == "wide" else "mx4", len(sizes), o, i, g, dtype)
+    b = 0.1 * randn((len(sizes), o), g)
+    m = sum(sizes)
+    offsets = ints([0] + list(torch.tensor(sizes).cumsum(0)))
+    if kind == "mx4 both":
+        xq, xs = ref.random_mx4((m,), i, g)
+        y = gpu.cnn_fc_grouped_fwd(xq, w, offsets, b, w_scale=ws, x_scale=xs, y_dtype=dtype)
+        x = ref.values(xq, xs, i)
+    else:
+        x = randn((m, i), g, dtype)
+        y = gpu.cnn_fc_grouped_fwd(x, w, offsets, b, w_scale=ws)
+    check_grouped(y, x, wv, offsets, None, b, False, f"{dtype} {kind}")
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("kind", ["wide", "mx4", "mx4 both"])
 @pytest.mark.parametrize("sizes,i,o", [([17, 40, 0, 64, 31, 1, 33, 90], 610, 1013), ([33] * 3, 4136, 500), ([20, 25] * 40, 198, 600),
                                        ([150, 0, 90], 521, 300), ([16, 9, 40, 0, 15] * 20, 40, 500)])
 def test_fc_grouped_some_rows_each(gpu, dtype, kind, sizes, i, o):
