@@ -266,7 +266,7 @@ int cnn_fc_grouped_fwd(const void* x, const uint8_t* x_scale, int x_type, int N,
 /* Device workspace of cnn_fc_grouped_fwd, as cnn_fc_mx4_workspace_bytes. */
 size_t cnn_fc_grouped_workspace_bytes(int x_type, int I, int M, int groups, int w_type, int O);
 
-/* Device workspace of cnn_route_fwd (0 up to 64 tokens, and on error). */
+/* Device workspace of cnn_route_fwd (0 for few tokens, and on error). */
 size_t cnn_route_workspace_bytes(int T, int E, int k);
 
 /* Routing of T tokens to k of E experts each.

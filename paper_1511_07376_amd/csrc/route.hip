@@ -10,9 +10,9 @@
 // order does not depend on when an atomic lands.
 //
 // Bound by the choices' chains of instructions, not by the bytes (2 MB for 8192 tokens of
-// 64 experts in bf16, which take 6.1 us to choose 8 each from and 5.0 to place).
+// 64 experts in bf16, which take 6.0 us to choose 8 each from and 4.9 to place).
 //
-// Up to 64 tokens, one workgroup does it all (16 tokens, 4 of 128: 4.4 us).  Above, one kernel chooses, 32
+// Of few tokens one workgroup does it all (16 tokens, 4 of 128: 4.4 us).  Above, one kernel chooses, 32
 // tokens a workgroup (a wave takes two), and counts the choices of every expert
 // in them, and a second one adds up what stands before each 64 tokens and
 // places them.  Where that sum is
@@ -27,7 +27,7 @@ namespace cnn {
 namespace {
 
 constexpr int kTokens = 32;      // tokens a workgroup, where there are several
-constexpr int kOne = 64;         // tokens up to which one does it all
+constexpr int kOne = 64;         // tokens that a workgroup places, and the most up to which one does it all
 constexpr int kThreads = 1024;
 constexpr int kWaves = kThreads / 64;
 
@@ -61,11 +61,10 @@ __device__ inline float wave_sum(float f) {
 }
 
 // A number that orders as the logit does, -0 as 0; 0 for what is never chosen (minus
-// infinity and NaN).
-__device__ inline unsigned order_key(float v) {
-    if (!(v > -INFINITY)) return 0;
+// infinity and NaN) or not `there`.  Without branches: a token has up to 16 a lane.
+__device__ inline unsigned order_key(float v, bool there) {
     const unsigned u = __float_as_uint(v + 0.0f);
-    return (u >> 31) ? ~u : u | 0x80000000u;
+    return (u ^ ((unsigned)((int)u >> 31) | 0x80000000u)) & -(unsigned)(there & (v > -INFINITY));
 }
 __device__ inline float key_logit(unsigned key) {
     return __uint_as_float((key >> 31) ? key & 0x7fffffffu : ~key);
@@ -97,7 +96,7 @@ __device__ inline void choose(unsigned (&key)[J], int k, bool renorm, int32_t* e
             if (!renorm) {
 #pragma unroll
                 for (int j = 0; j < J; ++j)
-                    if (key[j]) sum += expf(key_logit(key[j]) - top);
+                    sum += expf(key[j] ? key_logit(key[j]) - top : -INFINITY);
             }
         }
         if (lane == c) {
@@ -196,12 +195,18 @@ __global__ void __launch_bounds__(kThreads) route_choose(RouteParams p) {
     const int n = min(MOST, p.T - t0);
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     // all of the wave's logits are on their way before the first token's choices
-    unsigned key[EACH][J];
+    T logit[EACH][J];
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
         const T* row = (const T*)p.logits + (size_t)(t0 + min(wave + i * kWaves, n - 1)) * p.E;
 #pragma unroll
-        for (int j = 0; j < J; ++j) key[i][j] = lane + 64 * j < p.E ? order_key(to_f32(row[lane + 64 * j])) : 0;
+        for (int j = 0; j < J; ++j) logit[i][j] = row[min(lane + 64 * j, p.E - 1)];
+    }
+    unsigned key[EACH][J];
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+#pragma unroll
+        for (int j = 0; j < J; ++j) key[i][j] = order_key(to_f32(logit[i][j]), lane + 64 * j < p.E);
     }
     for (int e = threadIdx.x; e < p.E; e += kThreads) mask[e] = 0;
     __syncthreads();
@@ -322,10 +327,15 @@ __global__ void __launch_bounds__(kThreads) route_empty(int32_t* offsets, int E)
 // 128 KiB of them.
 constexpr int64_t kMaxCounts = 32768;
 
+// One workgroup's waves choose for a token each at a time, in a time that grows with the
+// experts: 64 tokens take 6.3 us of 8 experts (two kernels 6.8), 9.8 of 64 (8.7) and 16.4 of
+// 256 (12.4); 16 tokens 4.0, 4.9 and 7.3.
+bool one_workgroup(int T, int E) { return T <= (E <= 32 ? kOne : E <= 128 ? 48 : 32); }
+
 template <typename T, int J>
 void run_route(const RouteParams& p, hipStream_t st) {
     const int groups = ceil_div(p.T, kTokens);
-    if (p.T <= kOne) {
+    if (one_workgroup(p.T, p.E)) {
         enqueue(route_choose<T, J, true>, dim3(1), dim3(kThreads), 0, st, p);
         return;
     }
@@ -343,6 +353,7 @@ void run_route_type(const RouteParams& p, hipStream_t st) {
     if (p.E <= 64) run_route<T, 1>(p, st);
     else if (p.E <= 128) run_route<T, 2>(p, st);
     else if (p.E <= 256) run_route<T, 4>(p, st);
+    else if (p.E <= 512) run_route<T, 8>(p, st);
     else run_route<T, 16>(p, st);
 }
 
@@ -408,7 +419,7 @@ void run_combine(const T* x, int M, int D, const int32_t* slot, const float* wei
 
 size_t route_workspace(int T, int E) {
     const int64_t groups = ceil_div(T, kTokens);
-    return T <= kOne ? 0 : (size_t)(groups + 1) * E * sizeof(int32_t);
+    return one_workgroup(T, E) ? 0 : (size_t)(groups + 1) * E * sizeof(int32_t);
 }
 
 int launch_route(const void* logits, int type, int T, int E, int k, int renorm, int32_t* expert, float* weight,

@@ -358,6 +358,19 @@ def test_route(gpu, dtype, renorm, t, e, k):
     check_route(gpu, 2 * randn((t, e), gen(t + e + k), dtype), k, renorm)
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("renorm", [False, True])
+@pytest.mark.parametrize("t,e,k", [(33, 64, 8), (48, 128, 4), (49, 128, 4), (64, 33, 5), (64, 256, 8), (32, 257, 3), (33, 512, 8),
+                                   (1, 512, 2), (200, 300, 64), (3000, 511, 8), (64, 1024, 64)])
+def test_route_of_more_experts(gpu, dtype, renorm, t, e, k):
+    logits = randn((t, e), gen(t + e), dtype)
+    logits[::3, ::7] = -math.inf
+    logits[1::5, 1::11] = math.nan
+    logits[::2, 3::13] = 0.0
+    logits[::2, 4::13] = -0.0
+    check_route(gpu, logits, k, renorm)
+
+
 @pytest.mark.parametrize("t", [3, 200])
 def test_route_ties(gpu, t):
     """Equal logits go to the lower expert; +0 and -0 are equal."""
