@@ -109,6 +109,22 @@ def test_fc_grouped_large(gpu, dtype, kind, sizes, i, o):
         check_grouped(again, x, wv, offsets, rows, b, True, f"{dtype} unaligned")
 
 
+@pytest.mark.parametrize("kind", ["wide", "mx4"])
+@pytest.mark.parametrize("each,i", [(2, 200), (12, 1000), (30, 4096), (100, 2048), (200, 4096)])
+def test_fc_grouped_rows_before_the_first_group(gpu, kind, each, i):
+    """Groups that begin behind the first row and end before the last: the rows outside keep what they hold."""
+    g = gen(each)
+    o = 200
+    w, ws, wv = make_weights(kind, 3, o, i, g, torch.float32)
+    m, first = 3 * each + 12, 5
+    offsets = ints([first, first + each, first + each, first + 3 * each])
+    x = randn((m, i), g)
+    y = torch.full((m, o), 7.0, device="cuda")
+    gpu.cnn_fc_grouped_fwd(x, w, offsets, w_scale=ws, y=y)
+    check_grouped(y, x, wv, offsets, None, None, False, f"{kind} {each}", untouched=7.0)
+    assert bool((y[:first] == 7.0).all())
+
+
 def one_behind(t):
     """The same values, contiguous, one element behind an aligned address."""
     flat = torch.empty(t.numel() + 1, dtype=t.dtype, device=t.device)
