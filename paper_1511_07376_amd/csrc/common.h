@@ -69,7 +69,8 @@ inline FastDiv make_fastdiv(unsigned d) {
 }
 __device__ inline unsigned fdiv(unsigned n, FastDiv f) { return (__umulhi(f.m, n) + n) >> f.l; }
 
-inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
+// In 64 bits: the sum passes an int's range for the largest sizes.
+inline int ceil_div(int a, int b) { return (int)(((int64_t)a + b - 1) / b); }
 inline int64_t ceil_div64(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Largest element count a tensor may have (offsets inside kernels are int32).
