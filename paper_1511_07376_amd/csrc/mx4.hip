@@ -28,10 +28,11 @@ constexpr int kThreads = 256;
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
-// 8 values of a row from column c on; columns past the row read as zero.
+// 8 values of a row from column c on; columns past the row read as zero.  (The end is
+// not computed as c + 8, which for the longest rows is 2^31.)
 template <typename T>
 __device__ inline void load8(const T* row, int c, int cols, float* v) {
-    if (c + 8 <= cols) {
+    if (c <= cols - 8) {
         constexpr int N = 16 / (int)sizeof(T);
 #pragma unroll
         for (int h = 0; h < 8 / N; ++h) {
@@ -49,7 +50,7 @@ __device__ inline void load8(const T* row, int c, int cols, float* v) {
 
 template <typename T>
 __device__ inline void store8(T* row, int c, int cols, const float* v) {
-    if (c + 8 <= cols) {
+    if (c <= cols - 8) {
         constexpr int N = 16 / (int)sizeof(T);
 #pragma unroll
         for (int h = 0; h < 8 / N; ++h) {

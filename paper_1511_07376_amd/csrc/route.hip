@@ -371,7 +371,7 @@ combine_rows(const T* x, int M, int D, const int32_t* slot, const float* weight,
     for (unsigned i = blockIdx.x * 256 + threadIdx.x; i < items; i += step) {
         const int64_t t = fdiv(i, f_chunks);
         const int d = (int)(i - (unsigned)t * chunks) * N;
-        const bool whole = d + N <= D;
+        const bool whole = d <= D - N;  // d + N can be 2^31
         float acc[N];
 #pragma unroll
         for (int c = 0; c < N; ++c) acc[c] = 0.0f;

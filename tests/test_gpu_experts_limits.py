@@ -24,3 +24,36 @@ def test_fc_grouped_most_outputs(gpu, o):
     gpu.cnn_fc_grouped_fwd(x, w, torch.tensor([0, 1], dtype=torch.int32, device="cuda"), y=y)
     assert torch.equal(y[0, -40:], 2 * w[0, -40:, 0])
     assert bool((y[0, :-40] == 2).all()) and bool((rest == -1).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("cols", [MOST, MOST - 1, MOST - 7, MOST - 30])
+def test_mx4_longest_row(gpu, dtype, cols):
+    """One row, to mx4 and back, as its two halves are."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(cols % 100)
+    x = torch.empty((1, cols), dtype=dtype, device="cuda").normal_(generator=g)
+    q, scale = gpu.cnn_mx4_quantize(x)
+    y, rest = behind(cols, dtype, -1.0)
+    gpu.cnn_mx4_dequantize(q, scale, cols, y=y.view(1, cols))
+    assert bool((rest == -1).all())
+    half = 2**30
+    for lo, hi in ((0, half), (half, cols)):
+        part = x[0, lo:hi].unsqueeze(0)
+        pq, ps = gpu.cnn_mx4_quantize(part)
+        assert torch.equal(q[:, lo // 2:lo // 2 + pq.shape[1]], pq)
+        assert torch.equal(scale[:, lo // 32:lo // 32 + ps.shape[1]], ps)
+        assert torch.equal(y[lo:hi].unsqueeze(0), gpu.cnn_mx4_dequantize(pq, ps, hi - lo, dtype=dtype))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("d", [MOST, MOST - 2, MOST - 3, MOST - 7])
+def test_combine_longest_row(gpu, dtype, d):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(d % 100)
+    x = torch.empty((1, d), dtype=dtype, device="cuda").normal_(generator=g)
+    y, rest = behind(d, dtype, -1.0)
+    gpu.cnn_combine_fwd(x, torch.zeros((1, 1), dtype=torch.int32, device="cuda"), torch.full((1, 1), 0.5, device="cuda"),
+                        y=y.view(1, d))
+    assert bool((rest == -1).all())
+    assert torch.equal(y, x[0].mul_(0.5))
