@@ -391,7 +391,7 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) fc_tiles(TileParams tp) {
         __syncthreads();
 
         const int nb = (int)(((int64_t)p.I + 31) / 32);
-        const int acols = XT == CNN_MX4 ? nb * 32 : p.I, bcols = WT == CNN_MX4 ? nb * 32 : p.I;
+        const int64_t acols = XT == CNN_MX4 ? (int64_t)nb * 32 : p.I, bcols = WT == CNN_MX4 ? (int64_t)nb * 32 : p.I;
         const int64_t abytes = XT == CNN_MX4 ? (int64_t)nb * 16 : (int64_t)p.I * kElemBytes<XT>;
         const int64_t bbytes = WT == CNN_MX4 ? (int64_t)nb * 16 : (int64_t)p.I * kElemBytes<WT>;
         const int64_t first = split ? (int64_t)part * tail.run : 0, last = split ? min(first + tail.run, (int64_t)tp.slabs) : tp.slabs;

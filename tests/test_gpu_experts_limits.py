@@ -57,3 +57,44 @@ def test_combine_longest_row(gpu, dtype, d):
                         y=y.view(1, d))
     assert bool((rest == -1).all())
     assert torch.equal(y, x[0].mul_(0.5))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "mx4 on 4 bits", "bf16 on 4 bits"])
+def test_fc_grouped_longest_reduction(gpu, kind):
+    """One row of x, 40 times, through one of weights: tiles.  Whole blocks of the longest row are 2^31 values."""
+    m, cols = 40, MOST
+    offsets = torch.tensor([0, m], dtype=torch.int32, device="cuda")
+    rows = torch.zeros(m, dtype=torch.int32, device="cuda")
+    blocks = -(-cols // 32)
+    y = torch.full((m, 1), -1.0, dtype=torch.bfloat16, device="cuda")
+    # x: 1 at a few places, -1 at the last value; 4-bit codes of 1 and -1 are 2 and 10
+    ones = [0, 1, 2**30 - 1, 2**30, 2**30 + 77, MOST - 40, MOST - 32, MOST - 31, MOST - 2]
+    if kind == "mx4 on 4 bits":
+        x = torch.zeros((1, blocks * 16), dtype=torch.uint8, device="cuda")
+        for c in ones:
+            x[0, c // 2] += 2 << (4 * (c % 2))
+        x[0, (cols - 1) // 2] += 10 << (4 * ((cols - 1) % 2))
+        xs = torch.full((1, blocks), 127, dtype=torch.uint8, device="cuda")
+        x_type = gpu.CNN_MX4
+    else:
+        x = torch.zeros((1, cols), dtype=torch.bfloat16, device="cuda")
+        x[0, ones] = 1
+        x[0, -1] = -1
+        xs, x_type = None, gpu.CNN_BF16
+    if kind == "bf16":
+        w = torch.ones((1, 1, cols), dtype=torch.bfloat16, device="cuda")
+        ws, w_type = None, gpu.CNN_BF16
+        w[0, 0, -1] = 4
+    else:
+        w = torch.full((1, 1, blocks * 16), 0x22, dtype=torch.uint8, device="cuda")
+        ws, w_type = torch.full((1, 1, blocks), 127, dtype=torch.uint8, device="cuda"), gpu.CNN_MX4
+        w[0, 0, -1] = 0x06                            # 4, and nothing behind the last column
+    need = gpu.lib.cnn_fc_grouped_workspace_bytes(x_type, cols, m, 1, w_type, 1)
+    work = torch.empty(need, dtype=torch.uint8, device="cuda")
+    pointer = lambda t: None if t is None else t.data_ptr()
+    # the binding knows the columns of 4-bit rows as whole blocks only
+    status = gpu.lib.cnn_fc_grouped_fwd(pointer(x), pointer(xs), x_type, 1, cols, pointer(rows), m, pointer(offsets), 1,
+                                        pointer(w), pointer(ws), w_type, None, 1, 0, pointer(y), gpu.CNN_BF16,
+                                        pointer(work), need, torch.cuda.current_stream().cuda_stream)
+    assert status == gpu.CNN_OK
+    assert y.flatten().tolist() == [len(ones) - 4.0] * m
