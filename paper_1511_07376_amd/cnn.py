@@ -570,6 +570,8 @@ def cnn_route_fwd(logits, k, renormalize=False, stream=None):
         raise ValueError("route: logits must be [T][E]")
     T, E = logits.shape
     k = int(k)
+    if max(T, E, abs(k)) > _INT_MAX:
+        _too_large("route")
     code = _wide(logits.dtype, "logits")
     lp = _on(logits, "logits", device)
     need = lib.cnn_route_workspace_bytes(T, E, k)
@@ -598,7 +600,7 @@ def cnn_combine_fwd(x, slot, weight, y=None, stream=None):
     if x.dim() != 2 or slot.dim() != 2:
         raise ValueError("combine: x must be [M][D], slot [N][k]")
     (M, D), (N, k) = x.shape, slot.shape
-    if N > _INT_MAX or k > _INT_MAX:
+    if max(M, D, N, k) > _INT_MAX:
         _too_large("combine")
     code = _wide(x.dtype, "x")
     xp = _on(x, "x", device)

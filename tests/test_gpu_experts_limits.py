@@ -98,3 +98,14 @@ def test_fc_grouped_longest_reduction(gpu, kind):
                                         pointer(work), need, torch.cuda.current_stream().cuda_stream)
     assert status == gpu.CNN_OK
     assert y.flatten().tolist() == [len(ones) - 4.0] * m
+
+
+def test_sizes_no_int_holds_are_refused_without_elements(gpu):
+    """Tensors of no elements can have any width: it is not cut to the width that an int takes of it."""
+    slot, weight = torch.zeros((1, 1), dtype=torch.int32, device="cuda"), torch.ones((1, 1), device="cuda")
+    with pytest.raises(gpu.CnnError):
+        gpu.cnn_combine_fwd(torch.empty((0, 2**32 + 8), dtype=torch.bfloat16, device="cuda"), slot, weight)
+    with pytest.raises(gpu.CnnError):
+        gpu.cnn_route_fwd(torch.empty((0, 2**32 + 8), device="cuda"), 2)
+    with pytest.raises(gpu.CnnError):
+        gpu.cnn_route_fwd(torch.empty((0, 8), device="cuda"), 2**32 + 2)
