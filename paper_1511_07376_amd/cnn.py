@@ -443,8 +443,9 @@ def cnn_mx4_quantize(x, q=None, scale=None, stream=None):
     return q, scale
 
 
-def cnn_mx4_dequantize(q, scale, cols=None, dtype=torch.float32, y=None, stream=None):
-    """The values of mx4 rows, [...][cols] (cols: 32 a block if not given)."""
+def cnn_mx4_dequantize(q, scale, cols=None, dtype=None, y=None, stream=None):
+    """The values of mx4 rows, [...][cols] (cols: 32 a block if not given), of type dtype (y's, or float32, if not
+    given)."""
     device = _gpu(q, "q")
     if stream is not None or device.index != _current_gpu():
         with _there(device, stream):
@@ -461,10 +462,10 @@ def cnn_mx4_dequantize(q, scale, cols=None, dtype=torch.float32, y=None, stream=
     sp = _on(scale, "scale", device, torch.uint8)
     st = _raw_stream(device.index)
     if y is None:
-        y = torch.empty(lead + (cols,), dtype=dtype, device=device)
+        y = torch.empty(lead + (cols,), dtype=dtype or torch.float32, device=device)
         yp = y.data_ptr()
     else:
-        yp = _on(y, "y", device, None, lead + (cols,))
+        yp = _on(y, "y", device, dtype, lead + (cols,))
     _ok(lib.cnn_mx4_dequantize(qp, sp, rows, cols, yp,
                                _wide(y.dtype, "y"), st))
     return y
@@ -487,6 +488,15 @@ def _columns(x_type: int, x_cols: int, w_type: int, w_cols: int, what: str) -> i
     return x_cols
 
 
+def _result_type(x, xs, y_dtype):
+    """The type of a product's result: that of wide inputs; of mx4 ones the asked one, float32 if none."""
+    if xs is not None:
+        return y_dtype or torch.float32
+    if y_dtype is not None and y_dtype is not x.dtype:
+        raise TypeError(f"y_dtype must be {x.dtype}, the type of x, got {y_dtype}")
+    return x.dtype
+
+
 def cnn_fc_mx4_fwd(x, w, w_scale, bias=None, fuse_relu=False, x_scale=None, y_dtype=None, y=None, stream=None):
     """x [N][I] (or [N][C][H][W], read flattened), w and w_scale mx4 of [O][I] -> y [N][O], of x's type.
 
@@ -506,7 +516,7 @@ def cnn_fc_mx4_fwd(x, w, w_scale, bias=None, fuse_relu=False, x_scale=None, y_dt
     if O > _INT_MAX or cols > _INT_MAX:
         _too_large("fc_mx4")
     bp = _on(bias, "bias", device, torch.float32, (O,))
-    dtype = x.dtype if xs is None else y_dtype or torch.float32
+    dtype = _result_type(x, xs, y_dtype)
     st = _raw_stream(device.index)
     if y is None:
         y = torch.empty((N, O), dtype=dtype, device=device)
@@ -544,7 +554,7 @@ def cnn_fc_grouped_fwd(x, w, offsets, bias=None, fuse_relu=False, rows=None, w_s
     bp = _on(bias, "bias", device, torch.float32, (G, O))
     op = _on(offsets, "offsets", device, torch.int32, (G + 1,))
     rp = _on(rows, "rows", device, torch.int32)
-    dtype = x.dtype if xs is None else y_dtype or torch.float32
+    dtype = _result_type(x, xs, y_dtype)
     st = _raw_stream(device.index)
     if y is None:
         y = torch.empty((M, O), dtype=dtype, device=device)
