@@ -60,8 +60,11 @@ struct TileParams {
 constexpr int kMaxParts = 16;
 constexpr float kJoinNs = 3000;  // the second kernel's own time
 // The time of a tail in `parts`, as bits that compare like it, with the parts in the
-// lowest 4 (less one).
+// lowest 4 (less one).  fc_tiles and fc_join each work it out and have to agree to the
+// last bit: every operation is rounded by itself, whatever stands around it where this is
+// inlined.
 __host__ __device__ inline unsigned tail_key(const TileParams& tp, int tiles, unsigned parts, int& run) {
+#pragma clang fp contract(off)
     const unsigned turns = ((unsigned)tp.slabs + tp.unroll - 1) / (unsigned)tp.unroll;
     run = parts == 1 ? tp.slabs : (int)min((turns + parts - 1) / parts * (unsigned)tp.unroll, (unsigned)tp.slabs);
     const unsigned got = ((unsigned)tp.slabs + run - 1) / (unsigned)run;
