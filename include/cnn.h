@@ -230,7 +230,9 @@ int cnn_mx4_dequantize(const uint8_t* q, const uint8_t* scale, int rows, int col
  *   y [N][O]
  * Wide inputs are not quantised: products are of x as it is with the values
  * that w stands for (fp32 inputs below 2^-107 in magnitude keep an absolute
- * precision of 2^-133), sums are fp32 and the result is rounded once.
+ * precision of 2^-133), sums are fp32 and the result is rounded once.  Weights
+ * of 2^128 and more, which s = 253 and 254 allow, are not finite beside wide
+ * inputs: a sum that has one is infinite or NaN.
  * fuse_relu = 1 applies y = y > 0 ? y : +0 (so NaN becomes 0).  The result does
  * not change from call to call. */
 int cnn_fc_mx4_fwd(const void* x, const uint8_t* x_scale, int x_type, int N, int I,

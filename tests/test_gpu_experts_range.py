@@ -138,3 +138,30 @@ def test_fc_grouped_subnormal_operands(gpu, dtype, e, n):
         want, s = ref.product(x, w, None, False)
         y = gpu.cnn_fc_grouped_fwd(x, w.reshape(1, o, i), offsets)
         assert_bound(y, want, s, i, 0.0, f"{dtype} 2^{e} n {n}")
+
+
+@pytest.mark.parametrize("n", ROWS)
+@pytest.mark.parametrize("dtype", [F32, BF16, F16], ids=["f32", "bf16", "f16"])
+@pytest.mark.parametrize("scale", [253, 254])
+def test_fc_mx4_weights_above_the_range(gpu, dtype, scale, n):
+    """Beside wide inputs a weight of 2^128 or more is not finite, and no output that has one is; all others are what
+    they are without it.  What is below 2^128 is held."""
+    g = gen(n)
+    i, o = 300, 70
+    w, ws = ref.random_mx4((o,), i, g)
+    x = randn((n, i), g).to(dtype)
+    good = gpu.cnn_fc_mx4_fwd(x, w, ws)
+    w2, ws2 = w.clone(), ws.clone()
+    w2[33, 3 * 16:4 * 16] = 0
+    w2[33, 3 * 16] = 6                                # one code of 4, the rest of the block zero
+    ws2[33, 3] = scale
+    y = gpu.cnn_fc_mx4_fwd(x, w2, ws2)
+    keep = torch.arange(o, device="cuda") != 33
+    assert torch.equal(y[:, keep], good[:, keep])
+    assert not bool(torch.isfinite(y[:, 33]).any())
+    w2[33, 3 * 16] = 3 if scale == 254 else 5        # 1.5 * 2^127 and 3 * 2^126, the largest
+    x2 = torch.zeros_like(x)
+    x2[:, 96] = 2.0 ** -14
+    y = gpu.cnn_fc_mx4_fwd(x2, w2, ws2)
+    want = 1.5 * 2.0 ** 113
+    assert bool((y[:, 33].float() == (math.inf if dtype == F16 else want)).all())
