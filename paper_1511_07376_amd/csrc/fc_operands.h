@@ -53,7 +53,7 @@ __device__ inline u32x4 load_vector_edge(const char* p, int count, int64_t befor
     if (before >= N - count) {
         const u32x4 last = load16(p - (N - count) * ES);
         const uint64_t lo = last[0] | (uint64_t)last[1] << 32, hi = last[2] | (uint64_t)last[3] << 32;
-        const int bits = (N - count) * ES * 8;  // 1 to 15 bytes
+        const int bits = (N - count) * ES * 8;  // of 2 to 14 bytes
         const uint64_t l = bits < 64 ? lo >> bits | hi << 1 << (63 - bits) : hi >> (bits - 64), h = bits < 64 ? hi >> bits : 0;
         return u32x4{(unsigned)l, (unsigned)(l >> 32), (unsigned)h, (unsigned)(h >> 32)};
     }

@@ -17,9 +17,10 @@
 // workgroups bound by a slab's latency, and in fp32 by the matrix cores (4096 tokens, 2
 // of 8 of 2048 x 2048: 553 us, 124 of 154 TFLOP/s).
 //
-// LDS rows are 32 to 256 bytes without padding (the copying loads write 64
-// consecutive vectors); the 16-byte vectors of a row are exchanged by an XOR with
-// some bits of the row, so that lanes on consecutive rows read different banks.
+// LDS rows are 128 bytes (4-bit weights beside wide inputs: 32) without padding (the
+// copying loads write 64 consecutive vectors); the 16-byte vectors of a row are
+// exchanged by an XOR with some bits of the row, so that lanes on consecutive rows read
+// different banks.
 #pragma once
 
 #include "fc_operands.h"
@@ -110,7 +111,8 @@ static __device__ const u32x4 kZeroVector = {0, 0, 0, 0};
 // The XOR of a row's vectors, C vectors a row.
 template <int C>
 __device__ constexpr int vector_swap(int row) {
-    return C == 16 ? row & 15 : C == 8 ? (row >> 1) & 7 : C == 4 ? (row >> 1) & 3 : (row >> 2) & 1;
+    static_assert(C == 8 || C == 2, "rows of 128 bytes, or of 4-bit weights beside wide inputs");
+    return C == 8 ? (row >> 1) & 7 : (row >> 2) & 1;
 }
 
 // The slabs of a kernel.  VEC: rows of wide operands are whole 16-byte vectors.
