@@ -687,13 +687,15 @@ struct TileSize {
     float slab_ns, share, part_ns;  // as TileParams
 };
 
-template <int TM, int TN>
+// Wide inputs have results of their own type, 4-bit ones of any.
+template <int XT, int TM, int TN>
 void start_join(const TileParams& tp, int64_t tiles, hipStream_t st) {
     if (!tp.fc.offsets) tiles = tp.tail.tiles;
     // no more than are there at once (8 a compute unit): the tail of groups can be far shorter than it might (4096
     // tokens, 2 of 8 experts of 2048 x 2048, bf16: 120 us against 129)
     const dim3 grid((unsigned)std::min<int64_t>(std::min<int64_t>(tiles, tp.slots) * (TM * TN / 1024), 2048)), block(256);
-    if (tp.fc.y_type == CNN_F32) enqueue(fc_join<TM, TN, CNN_F32>, grid, block, 0, st, tp);
+    if constexpr (XT != CNN_MX4) enqueue(fc_join<TM, TN, XT>, grid, block, 0, st, tp);
+    else if (tp.fc.y_type == CNN_F32) enqueue(fc_join<TM, TN, CNN_F32>, grid, block, 0, st, tp);
     else if (tp.fc.y_type == CNN_BF16) enqueue(fc_join<TM, TN, CNN_BF16>, grid, block, 0, st, tp);
     else enqueue(fc_join<TM, TN, CNN_F16>, grid, block, 0, st, tp);
 }
@@ -708,7 +710,7 @@ void start_tiles(const GroupedFc& p, const TileSize& size, float* partial, hipSt
     if (!p.offsets) tp.tail = make_tail(tp, (int)tiles);
     const int64_t jobs = p.offsets ? tiles + size.room : tp.tail.full + (int64_t)tp.tail.tiles * tp.tail.parts;
     enqueue(fc_tiles<XT, WT, WM, WN, FM, FN, VEC>, dim3((unsigned)std::min<int64_t>(jobs, 1 << 22)), dim3(S::NT), 0, st, tp);
-    if (size.room > 0 && (p.offsets || tp.tail.parts > 1)) start_join<S::TM, S::TN>(tp, tiles, st);
+    if (size.room > 0 && (p.offsets || tp.tail.parts > 1)) start_join<XT, S::TM, S::TN>(tp, tiles, st);
 }
 
 template <int XT, int WT, bool VEC>
