@@ -109,3 +109,21 @@ def test_sizes_no_int_holds_are_refused_without_elements(gpu):
         gpu.cnn_route_fwd(torch.empty((0, 2**32 + 8), device="cuda"), 2)
     with pytest.raises(gpu.CnnError):
         gpu.cnn_route_fwd(torch.empty((0, 8), device="cuda"), 2**32 + 2)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+def test_fc_grouped_most_rows(gpu, dtype):
+    """2^31 - 1 rows of results, gathered from a thousand, in groups that end anywhere."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+    x = torch.randint(-8, 9, (1000, 1), generator=g, device="cuda").to(dtype)
+    w = torch.tensor([1.0, 2.0, 4.0], device="cuda").to(dtype).view(3, 1, 1)
+    rows = torch.randint(0, 1000, (MOST,), generator=g, device="cuda", dtype=torch.int32)
+    bounds = [0, 5, 2**30 + 1, MOST - 3]
+    y, rest = behind(MOST, dtype, -1.0)
+    gpu.cnn_fc_grouped_fwd(x, w, torch.tensor(bounds, dtype=torch.int32, device="cuda"), rows=rows, y=y.view(MOST, 1))
+    assert bool((rest == -1).all()) and bool((y[MOST - 3:] == -1).all())
+    for k, (lo, hi) in enumerate(zip(bounds, bounds[1:])):
+        for at in range(lo, hi, 2**28):
+            end = min(at + 2**28, hi)
+            assert torch.equal(y[at:end], x[:, 0][rows[at:end].long()] * w[k, 0, 0]), (k, at)
