@@ -571,7 +571,10 @@ def cnn_fc_grouped_fwd(x, w, offsets, bias=None, fuse_relu=False, rows=None, w_s
 
 def cnn_route_fwd(logits, k, renormalize=False, stream=None):
     """logits [T][E] -> (expert int32 [T][k], weight float32 [T][k], rows int32 [T*k], offsets int32 [E+1],
-    slot int32 [T][k]): each token's k experts and their weights, and the rows for cnn_fc_grouped_fwd."""
+    slot int32 [T][k]): each token's k experts and their weights, and the rows for cnn_fc_grouped_fwd.
+
+    The five are parts of one allocation: it lives as long as any of them (clone what is to be kept alone), and
+    autograd takes a write in place to one as a write to all."""
     device = _gpu(logits, "logits")
     if stream is not None or device.index != _current_gpu():
         with _there(device, stream):

@@ -16,7 +16,8 @@ namespace {
 // Inputs that are cut into parts beside 4-bit weights.
 bool cut_inputs(const GroupedFc& p) { return p.w_type == CNN_MX4 && (p.x_type == CNN_F32 || p.x_type == CNN_F16); }
 
-// Few rows a group (on average: offsets are on the device): the weights are streamed,
+// Few rows a group (on average: offsets are on the device, and what uneven groups cost the
+// kernel says): the weights are streamed,
 // once for every 16 rows, by many small workgroups.  Tiles take some 10 us at least, but read
 // the weights once and feed the matrix cores better, so with more rows the
 // streamed weights have to be few: of a plain layer on 4-bit weights up to 32 rows

@@ -9,9 +9,10 @@
 // order of the waves, so results do not change from call to call.  The weights
 // are the matrix row, the rows of x the column: with one row of x the
 // matrix cores idle to 15/16, which costs nothing while the weights arrive.
-// A group of more than 16 RT rows takes as many passes over its weights.
+// A group of more than 16 RT rows (THIN: 4) takes as many passes over its weights, one after
+// another: 256 rows in 64 groups of 2048 x 4096, bf16 on 4 bits, 59 us evenly spread, 144 in one group.
 // Bound by HBM where weights are many (16 tokens, 4 of 64 experts of 2048 x 4096, bf16 on 4
-// bits: 185 MB in 33.5 us, 5.5 TB/s), by one chain of load, product and join where
+// bits: 185 MB in 33.5 to 38 us, 4.9 to 5.5 TB/s), by one chain of load, product and join where
 // they are few (one token, 4096 x 4096: 8.9 MB in 4.4 to 4.9 us, of which an empty
 // kernel takes 2.3).
 #include "fc_operands.h"
@@ -300,7 +301,7 @@ void start(const GroupedFc& p, hipStream_t st) {
 // flight a wave (one token, 4096 x 4096: 4.5 us; with 32 outputs a workgroup
 // 6.4); from 1024 workgroups on 32 outputs share the rows of x, and a wave
 // takes about four steps, so that fewer waves meet in LDS (16 tokens, 4 of 64
-// experts of 2048 x 4096: 38.7 us; 16 outputs and 8 waves 63).  Short reductions leave
+// experts of 2048 x 4096, side by side: 38.7 us; 16 outputs and 8 waves 63).  Short reductions leave
 // all but the first waves without a step (13 tokens, 6 of 115 experts of 64 x 2752: bf16
 // 39.9 us with 8 waves, 12.1 with 2, 8.7 with 1, on 4-bit weights 11.5 with 2, 8.1 with 1; of
 // 512 x 1000 18.6, 11.8 and 13.4; 40 tokens, 8 experts of 512 x 1024, fp32 on 4-bit

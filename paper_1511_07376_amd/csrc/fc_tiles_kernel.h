@@ -13,9 +13,11 @@
 // 4096 in bf16 takes 196 us for its copies alone on 256 x 256 tiles (11 TB/s, from
 // the L2s and behind them) and 280 on 128 x 128 (15), the products alone 213 (1290
 // TFLOP/s); together 4096 tokens, 2 of 8 experts of 4096 x 4096, take 333 (825 TFLOP/s).
-// 4 bits on both sides, 2048 x 9216 x 4096: 59 to 63 us (2.5 to 2.6 PFLOP/s).  With few
-// workgroups bound by a slab's latency, and in fp32 by the matrix cores (4096 tokens, 2
-// of 8 of 2048 x 2048: 553 us, 124 of 154 TFLOP/s).
+// 4 bits on both sides, 2048 x 9216 x 4096: 59 to 67 us (2.3 to 2.6 PFLOP/s), bound by
+// products that the compiler moves behind the barrier, where they cover neither copies nor
+// reads (matrix cores busy for 25%; 52 registers spilled).  With few workgroups bound by a
+// slab's latency, and in fp32 by the matrix cores (4096 tokens, 2 of 8 of 2048 x 2048: 553
+// us, 124 of 154 TFLOP/s).
 //
 // LDS rows are 128 bytes (4-bit weights beside wide inputs: 32) without padding (the
 // copying loads write 64 consecutive vectors); the 16-byte vectors of a row are

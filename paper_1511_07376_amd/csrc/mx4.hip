@@ -14,7 +14,7 @@
 // Both directions move bytes and little else (HBM bound).  A work-item takes 8
 // values, a quarter of a block: 16 or 32 bytes of wide values against 4 of
 // 4-bit ones, the conversion instructions of gfx950 in between.  fp32 4096 x 9216:
-// 35.9 us to mx4 and 28.6 back (4.8 and 6.0 TB/s, some of them from the memory-side
+// 36.2 us to mx4 and 28.3 back (4.7 and 6.0 TB/s, some of them from the memory-side
 // cache), bf16 64 x 4096: 2.6 and 2.5 (a kernel's least).
 #include "common.h"
 #include "wide_types.h"
