@@ -89,16 +89,20 @@ def layer_work(net, batch, cnn):
 # Host-only sources (argument checks, tuning table, NetFile parser): they do
 # not change what a kernel reads or writes.
 HOST_ONLY_SOURCES = ("api.hip", "tuner.hip", "netfile.cpp")
+# Operators that no network runs: on 4-bit values and on groups of rows.
+EXPERT_SOURCES = ("experts.h", "wide_types.h", "mx4.hip", "route.hip", "fc_grouped.hip", "fc_operands.h", "fc_rows.hip",
+                  "fc_tiles_kernel.h", "fc_tiles_16.hip", "fc_tiles_bf16_mx4.hip", "fc_tiles_cut.hip", "fc_tiles_f32.hip",
+                  "fc_tiles_mx4.hip")
 
 
 def source_digest():
-    """Digest of the kernel sources (and their launchers) under csrc/, without
-    their comments and blank lines (a comment edit changes no kernel)."""
+    """Digest of the networks' kernel sources (and their launchers) under csrc/,
+    without their comments and blank lines (a comment edit changes no kernel)."""
     import re
     h = hashlib.sha256()
     csrc = os.path.join(ROOT, "paper_1511_07376_amd", "csrc")
     for f in sorted(os.listdir(csrc)):
-        if f in HOST_ONLY_SOURCES:
+        if f in HOST_ONLY_SOURCES + EXPERT_SOURCES:
             continue
         with open(os.path.join(csrc, f), encoding="utf-8") as fh:
             text = fh.read()

@@ -11,6 +11,7 @@
 #include <vector>
 
 #include "common.h"
+#include "experts.h"
 #include "wide_types.h"
 
 namespace cnn {

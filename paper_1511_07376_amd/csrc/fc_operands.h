@@ -14,7 +14,7 @@
 // fp32 sums.
 #pragma once
 
-#include "common.h"
+#include "experts.h"
 #include "wide_types.h"
 
 #include <cmath>

@@ -16,7 +16,7 @@
 // 4-bit ones, the conversion instructions of gfx950 in between.  fp32 4096 x 9216:
 // 36.2 us to mx4 and 28.3 back (4.7 and 6.0 TB/s, some of them from the memory-side
 // cache), bf16 64 x 4096: 2.6 and 2.5 (a kernel's least).
-#include "common.h"
+#include "experts.h"
 #include "wide_types.h"
 
 #include <algorithm>

@@ -17,7 +17,7 @@
 // in them, and a second one adds up what stands before each 64 tokens and
 // places them.  Where that sum is
 // long (kMaxCounts) a kernel between the two turns the counts into sums.
-#include "common.h"
+#include "experts.h"
 #include "wide_types.h"
 
 #include <algorithm>
