@@ -1,0 +1,335 @@
+"""The operators around a language model's 8-bit products, from the norm to the chosen token, and the calls they are
+measured by.
+
+Each case is what a program calls of the Python binding of libcnn for one step, with its plain form in elementary
+torch operations.  8-bit values ("f8") are torch.float8_e4m3fn, in blocks of 128 along a row with an fp32 scale for
+each: one per row and block for activations, one per 128 x 128 block for weights.  Wide types are those of the
+activations and results; biases, norm weights and sampling parameters are fp32.
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False  # True: run() calls the library's kernels; False: their plain forms
+
+_TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+_BYTES = {"f32": 4, "bf16": 2, "f16": 2}
+_F8 = torch.float8_e4m3fn
+_EPS = 1e-6
+_MOST_F8 = 448.0
+_LEAST_TOP = 2.0 ** -100  # a block's largest magnitude counts as this at least
+
+
+def _norm(rows, cols, dtype, residual, f8):
+    """residual: x is added to it first, and the sum is an output; f8: the result is brought to 8 bits."""
+    return {"op": "norm", "rows": rows, "cols": cols, "dtype": dtype, "residual": residual, "f8": f8}
+
+
+def _fc(n, i, o, dtype, x8, relu):
+    """x8: the activations are in 8 bits already; otherwise they are of the result's type, and the call brings them."""
+    return {"op": "fc_f8", "n": n, "i": i, "o": o, "dtype": dtype, "x8": x8, "relu": relu}
+
+
+def _sample(n, v, dtype, cut):
+    """cut: rows have a top-k, a top-p and a min-p of their own; otherwise a temperature alone."""
+    return {"op": "sample", "n": n, "v": v, "dtype": dtype, "cut": cut}
+
+
+def listed():
+    cases = {
+        # one token between two layers: the smallest call, where latency counts
+        "norm_1x4096_bf16": _norm(1, 4096, "bf16", True, False),
+        # a batch of 64 before an 8-bit product
+        "norm_64x4096_bf16_f8": _norm(64, 4096, "bf16", True, True),
+        # a long prompt before an 8-bit product
+        "norm_8192x4096_bf16_f8": _norm(8192, 4096, "bf16", True, True),
+        # odd sizes, no residual, in the library's own type
+        "norm_odd_77x1013_f32": _norm(77, 1013, "f32", False, False),
+        # one token through a square layer: a stream of 8-bit weights
+        "fc_f8_1x4096x4096_bf16": _fc(1, 4096, 4096, "bf16", True, False),
+        # AlexNet's largest fully connected layer on a batch, in the library's own type
+        "fc_f8_64x9216x4096_f32": _fc(64, 9216, 4096, "f32", False, True),
+        # the same layer on a long prompt: the largest product
+        "fc_f8_2048x9216x4096_bf16": _fc(2048, 9216, 4096, "bf16", True, False),
+        # odd sizes throughout: blocks and rows that end anywhere
+        "fc_f8_odd_77x1013x610_f16": _fc(77, 1013, 610, "f16", False, True),
+        # AlexNet's classes, a few rows
+        "sample_7x1000_f32": _sample(7, 1000, "f32", True),
+        # one sequence's next token
+        "sample_1x32768_f32": _sample(1, 32768, "f32", True),
+        # a served batch over a large vocabulary, every row with parameters of its own
+        "sample_64x131072_bf16": _sample(64, 131072, "bf16", True),
+        # many rows with a temperature alone, odd vocabulary
+        "sample_256x50021_f16": _sample(256, 50021, "f16", False),
+    }
+    return [{"name": name, **case} for name, case in cases.items()]
+
+
+def _log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def _width(rng, lo, hi):
+    """A layer's width: mostly a multiple of 128, as layers have, else any number."""
+    w = _log_int(rng, lo, hi)
+    return max(128, w // 128 * 128) if rng.random() < 0.6 else w
+
+
+def draw(rng):
+    most = max(work(c)["flops"] for c in listed() if c["op"] == "fc_f8")
+    u = rng.random()
+    dtype = rng.choice(("f32", "bf16", "bf16", "f16"))
+    if u < 0.3:
+        while True:
+            case = _norm(_log_int(rng, 1, 16384), _width(rng, 64, 16384), dtype, rng.random() < 0.6, rng.random() < 0.5)
+            if case["rows"] * case["cols"] <= 8192 * 4096:
+                return case
+    if u < 0.7:
+        while True:
+            case = _fc(_log_int(rng, 1, 4096), _width(rng, 64, 9216), _width(rng, 10, 8192), dtype, rng.random() < 0.5,
+                       rng.random() < 0.5)
+            if work(case)["flops"] <= most:
+                return case
+    while True:
+        case = _sample(_log_int(rng, 1, 256), _log_int(rng, 10, 200000), dtype, rng.random() < 0.7)
+        if case["n"] * case["v"] <= 256 * 50021:
+            return case
+
+
+# ------------------------------------------------------------------ inputs
+def _normal(shape, gen):
+    return torch.randn(shape, generator=gen, device="cuda")
+
+
+def _uniform(shape, gen):
+    return torch.rand(shape, generator=gen, device="cuda")
+
+
+def _activations(rows, cols, gen):
+    """Normal values whose channels differ in size, some by a lot, as the activations inside large models do."""
+    return _normal((rows, cols), gen) * torch.exp(0.5 * _normal((cols,), gen))
+
+
+def _blocks(cols):
+    return -(-cols // 128)
+
+
+def _logits(n, v, gen):
+    """A broad bulk, a few dozen likely tokens a row, and some that are masked."""
+    x = 2.0 * _normal((n, v), gen)
+    likely = torch.randint(0, v, (n, min(v, 24)), generator=gen, device="cuda")
+    x.scatter_add_(1, likely, 8.0 * _uniform(likely.shape, gen))
+    x[:, 1:].masked_fill_(_uniform((n, v - 1), gen) < 0.02, -math.inf)
+    return x
+
+
+def prepare(case, seed):
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+    s = {"case": case}
+    op, dtype = case["op"], _TYPES[case["dtype"]]
+    if op == "norm":
+        rows, cols = case["rows"], case["cols"]
+        s["x"] = _activations(rows, cols, gen).to(dtype)
+        s["r"] = (2 * _activations(rows, cols, gen)).to(dtype) if case["residual"] else None
+        s["w"] = 1 + 0.2 * _normal((cols,), gen)
+    elif op == "fc_f8":
+        n, i, o = case["n"], case["i"], case["o"]
+        if case["x8"]:
+            # as a quantisation leaves them: every block's largest value near 448
+            s["x"] = (112 * _normal((n, i), gen)).clamp(-448, 448).to(_F8)
+            s["xs"] = torch.exp(0.5 * _normal((n, _blocks(i)), gen)) / 112
+        else:
+            s["x"], s["xs"] = _activations(n, i, gen).to(dtype), None
+        s["w"] = (100 * _normal((o, i), gen)).clamp(-448, 448).to(_F8)
+        s["ws"] = torch.exp(0.2 * _normal((_blocks(o), _blocks(i)), gen)) / (100 * math.sqrt(i))
+        s["b"] = 0.1 * _normal((o,), gen)
+    else:
+        n, v = case["n"], case["v"]
+        s["logits"] = _logits(n, v, gen).to(dtype)
+        s["u"] = _uniform((n,), gen)
+        s["temperature"] = 0.6 + 0.8 * _uniform((n,), gen)
+        s["top_k"] = s["top_p"] = s["min_p"] = None
+        if case["cut"]:
+            # a row in eight is greedy, a quarter has no top-k, a quarter no top-p, half no min-p
+            s["temperature"] = s["temperature"].masked_fill(_uniform((n,), gen) < 0.125, 0.0)
+            k = torch.randint(1, 201, (n,), generator=gen, device="cuda", dtype=torch.int32)
+            s["top_k"] = k.masked_fill(_uniform((n,), gen) < 0.25, 0)
+            s["top_p"] = (0.5 + 0.49 * _uniform((n,), gen)).masked_fill(_uniform((n,), gen) < 0.25, 1.0)
+            s["min_p"] = (0.1 * _uniform((n,), gen)).masked_fill(_uniform((n,), gen) < 0.5, 0.0)
+    return s
+
+
+# ------------------------------------------------------------------ plain forms
+def _to_f8(x):
+    """x (fp32) in 8 bits: values [rows][cols], scales [rows][blocks]."""
+    rows, cols = x.shape
+    b = torch.nn.functional.pad(x, (0, -cols % 128)).reshape(rows, -1, 128)
+    top = b.abs().amax(-1, keepdim=True).clamp(min=_LEAST_TOP)
+    most = torch.full_like(top, _MOST_F8)  # a tensor: a number's quotients go through a reciprocal, rounded once more
+    q = (b * (most / top)).to(_F8)
+    return q.reshape(rows, -1)[:, :cols].contiguous(), (top / most).squeeze(-1)
+
+
+def _plain_norm(s):
+    case = s["case"]
+    x = s["x"].float()
+    x = x + s["r"].float() if case["residual"] else x
+    y = x * torch.rsqrt((x * x).mean(-1, keepdim=True) + _EPS) * s["w"]
+    out = {}
+    if case["f8"]:
+        out["y"], out["scale"] = _to_f8(y)
+    else:
+        out["y"] = y.to(s["x"].dtype)
+    if case["residual"]:
+        out["sum"] = x.to(s["x"].dtype)
+    return out
+
+
+def _plain_fc(s):
+    case = s["case"]
+    q, scale = (s["x"], s["xs"]) if case["x8"] else _to_f8(s["x"].float())
+    x = q.float() * scale.repeat_interleave(128, dim=1)[:, :case["i"]]
+    ws = s["ws"].repeat_interleave(128, dim=0)[:case["o"]].repeat_interleave(128, dim=1)[:, :case["i"]]
+    y = x @ (s["w"].float() * ws).T + s["b"]
+    return (torch.relu(y) if case["relu"] else y).to(_TYPES[case["dtype"]])
+
+
+def _plain_sample(s):
+    # in 64 bits: which token a random number falls on is a matter of sums next to a border
+    case = s["case"]
+    x = s["logits"].double()
+    n, v = x.shape
+    t = s["temperature"].double().unsqueeze(1)
+    greedy = t == 0
+    top = x.amax(1, keepdim=True)
+    weight = torch.exp((x - top) / torch.where(greedy, 1.0, t))
+    # a stable descending order gives ties to the lowest index
+    order = torch.sort(x, dim=1, descending=True, stable=True).indices
+    w = weight.gather(1, order)
+    rank = torch.arange(v, device=x.device)
+    keep = torch.where(greedy, rank < 1, x.gather(1, order) > -math.inf)
+    if case["cut"]:
+        k = s["top_k"].unsqueeze(1)
+        keep = keep & ((k <= 0) | (rank < k))
+        w = torch.where(keep, w, 0.0)
+        sums = w.cumsum(1)
+        p = s["top_p"].double().unsqueeze(1)
+        keep = keep & ((p >= 1) | (sums - w < p * sums[:, -1:]) | (rank < 1))
+        keep = keep & (w >= s["min_p"].double().unsqueeze(1))
+    kept = torch.zeros_like(weight).scatter(1, order, torch.where(keep, w, 0.0))
+    sums = kept.cumsum(1)
+    token = (sums <= s["u"].double().unsqueeze(1) * sums[:, -1:]).sum(1)
+    prob = kept.gather(1, token.unsqueeze(1)) / sums[:, -1:]
+    return {"token": token.to(torch.int32), "prob": prob.squeeze(1).float()}
+
+
+def _plain(s):
+    return {"norm": _plain_norm, "fc_f8": _plain_fc, "sample": _plain_sample}[s["case"]["op"]](s)
+
+
+# ------------------------------------------------------------------ the library's calls
+def _library(s):
+    from paper_1511_07376_amd import cnn
+
+    case = s["case"]
+    op = case["op"]
+    if op == "norm":
+        got = cnn.cnn_rms_norm_fwd(s["x"], s["w"], s["r"], eps=_EPS, f8=case["f8"])
+        names = ["y"] + ["scale"] * case["f8"] + ["sum"] * case["residual"]
+        return dict(zip(names, got)) if len(names) > 1 else {"y": got}
+    if op == "fc_f8":
+        x, xs = (s["x"], s["xs"]) if case["x8"] else cnn.cnn_f8_quantize(s["x"])
+        return cnn.cnn_fc_f8_fwd(x, xs, s["w"], s["ws"], s["b"], case["relu"], y_dtype=_TYPES[case["dtype"]])
+    token, prob = cnn.cnn_sample_fwd(s["logits"], s["u"], s["temperature"], s["top_k"], s["top_p"], s["min_p"])
+    return {"token": token, "prob": prob}
+
+
+def run(state):
+    return _library(state) if own else _plain(state)
+
+
+def work(case):
+    op, sz = case["op"], _BYTES[case["dtype"]]
+    if op == "norm":
+        n = case["rows"] * case["cols"]
+        out = (1 + 4 / 128) if case["f8"] else sz
+        return {"bytes": n * (sz * (3 if case["residual"] else 1) + out) + 4 * case["cols"], "flops": 6 * n}
+    if op == "fc_f8":
+        n, i, o = case["n"], case["i"], case["o"]
+        x = n * i * (1 + 4 / 128 if case["x8"] else sz)
+        return {"bytes": x + o * i * (1 + 4 / 128 ** 2) + 4 * o + n * o * sz, "flops": 2 * n * i * o}
+    n, v = case["n"], case["v"]
+    return {"bytes": n * v * sz + n * (28 if case["cut"] else 16), "flops": 4 * n * v}
+
+
+# ------------------------------------------------------------------ 64 bits
+def _quantized64(x):
+    """f8 values and scales of x (64 bits) by the definition, whose factor 448 / top and whose products with it are
+    fp32 numbers; the nearest f8 value by its step, which is 2^-9 at least."""
+    rows, cols = x.shape
+    b = torch.nn.functional.pad(x, (0, -cols % 128)).reshape(rows, -1, 128)
+    top = b.abs().amax(-1, keepdim=True).clamp(min=_LEAST_TOP)
+    most = torch.full_like(top, _MOST_F8)
+    v = (b * (most / top).float().double()).float().double()
+    _, e = torch.frexp(v)
+    step = torch.ldexp(torch.ones_like(v), (e - 4).clamp(min=-9))
+    q = (torch.round(v / step) * step).clamp(-_MOST_F8, _MOST_F8)
+    return q.reshape(rows, -1)[:, :cols], (top / most).squeeze(-1)
+
+
+def _exact_norm(s):
+    case = s["case"]
+    x = s["x"].double() + (s["r"].double() if case["residual"] else 0.0)
+    y = x / ((x ** 2).sum(-1, keepdim=True) / case["cols"] + _EPS).sqrt() * s["w"].double()
+    y, scale = _quantized64(y) if case["f8"] else (y, None)
+    out = {"y": y, "scale": scale, "sum": x if case["residual"] else None}
+    return {name: v for name, v in out.items() if v is not None}
+
+
+def _exact_fc(s):
+    case = s["case"]
+    q, scale = (s["x"].double(), s["xs"].double()) if case["x8"] else _quantized64(s["x"].double())
+    scale = scale if case["x8"] else scale.float().double()
+    y = s["b"].double().repeat(case["n"], 1)
+    for k in range(_blocks(case["i"])):
+        at = slice(128 * k, min(128 * k + 128, case["i"]))
+        ws = s["ws"][:, k].double().repeat_interleave(128)[:case["o"]]
+        y += (q[:, at] @ s["w"][:, at].double().T) * scale[:, k:k + 1] * ws
+    return y.clamp(min=0) if case["relu"] else y
+
+
+def _exact_sample(s):
+    """Row by row: the tokens in order of (-logit, index), cut one rule after the other, then walked by index."""
+    probs = []
+    host = {name: s[name].double().cpu() for name in ("logits", "u", "temperature")}
+    cut = {name: s[name].double().cpu() for name in ("top_k", "top_p", "min_p")} if s["case"]["cut"] else None
+    for r in range(s["case"]["n"]):
+        x, t = host["logits"][r], float(host["temperature"][r])
+        if t == 0:
+            probs.append(1.0)
+            continue
+        live = torch.nonzero(x > -math.inf).squeeze(1)
+        live = live[torch.argsort(-x[live], stable=True)]
+        w = torch.exp(x[live] / t - float(x[live[0]]) / t)
+        if cut is not None:
+            k, p, least = (float(cut[name][r]) for name in ("top_k", "top_p", "min_p"))
+            if k > 0:
+                live, w = live[:int(k)], w[:int(k)]
+            if p < 1:
+                before = torch.cat([w.new_zeros(1), w.cumsum(0)[:-1]])
+                many = max(1, int((before < p * float(w.sum())).sum()))
+                live, w = live[:many], w[:many]
+            live, w = live[w >= least], w[w >= least]
+        w = w[torch.argsort(live)]
+        sums = w.cumsum(0)
+        at = int(torch.searchsorted(sums, float(host["u"][r]) * float(sums[-1]), right=True))
+        probs.append(float(w[at] / sums[-1]))
+    return {"token": None, "prob": torch.tensor(probs, dtype=torch.float64)}
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    return {"norm": _exact_norm, "fc_f8": _exact_fc, "sample": _exact_sample}[case["op"]](s)
