@@ -275,7 +275,7 @@ def _quantized64(x):
     most = torch.full_like(top, _MOST_F8)
     v = (b * (most / top).float().double()).float().double()
     _, e = torch.frexp(v)
-    step = torch.ldexp(torch.ones_like(v), (e - 4).clamp(min=-9))
+    step = (((e.long() - 4).clamp(min=-9) + 1023) << 52).view(torch.float64)  # a power of two, exactly
     q = (torch.round(v / step) * step).clamp(-_MOST_F8, _MOST_F8)
     return q.reshape(rows, -1)[:, :cols], (top / most).squeeze(-1)
 
