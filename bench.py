@@ -89,10 +89,11 @@ def layer_work(net, batch, cnn):
 # Host-only sources (argument checks, tuning table, NetFile parser): they do
 # not change what a kernel reads or writes.
 HOST_ONLY_SOURCES = ("api.hip", "tuner.hip", "netfile.cpp")
-# Operators that no network runs: on 4-bit values and on groups of rows.
+# Operators that no network runs: on 4-bit values, on groups of rows, and around products on 8-bit floats.
 EXPERT_SOURCES = ("experts.h", "wide_types.h", "mx4.hip", "route.hip", "fc_grouped.hip", "fc_operands.h", "fc_rows.hip",
                   "fc_tiles_kernel.h", "fc_tiles_16.hip", "fc_tiles_bf16_mx4.hip", "fc_tiles_cut.hip", "fc_tiles_f32.hip",
-                  "fc_tiles_mx4.hip")
+                  "fc_tiles_mx4.hip", "f8.h", "f8.hip", "norm.hip", "fc_f8.h", "fc_f8.hip", "fc_f8_tiles.hip",
+                  "sample.hip")
 
 
 def source_digest():

@@ -11,14 +11,14 @@
  * Conventions for every entry point:
  *  - Tensors are fp32, NCHW, row-major, contiguous, in DEVICE memory,
  *    allocated and owned by the caller.  The library allocates nothing.
- *    The operators of the section on mixtures of experts also take bf16,
- *    fp16 and microscaled 4-bit tensors.
+ *    The operators of the sections on mixtures of experts and on the norm, 8-bit
+ *    floats and sampling also take bf16, fp16 and microscaled 4-bit or 8-bit tensors.
  *  - Calls are asynchronous: argument checks run on the host first and a
  *    negative status means nothing was enqueued; on CNN_OK the kernels are
  *    enqueued on `stream` (a hipStream_t; NULL = the null stream) and the
  *    caller synchronises.
  *  - Input and output buffers must not overlap, except that cnn_relu_fwd
- *    and cnn_softmax_fwd allow y == x.  A pointer to a tensor with no elements (batch N = 0,
+ *    and cnn_softmax_fwd allow y == x, and cnn_rms_norm_fwd what it says.  A pointer to a tensor with no elements (batch N = 0,
  *    length n = 0) may be NULL; such a call validates and enqueues nothing.
  *  - No exception or abort crosses the ABI.  cnn_last_error() returns a
  *    thread-local message describing the last non-OK status of this thread.
@@ -208,7 +208,14 @@ typedef enum cnn_dtype {
      * own, multiplies them by 2^(s - 127); s = 255 makes the whole block
      * NaN.  So R rows are uint8 [R][ceil(C/32)*16], 16-byte aligned, and
      * uint8 [R][ceil(C/32)].  The values behind column C must be 0. */
-    CNN_MX4 = 3
+    CNN_MX4 = 3,
+    /* 8-bit floats ("f8"): a sign, 4 exponent bits biased by 7, 3 mantissa
+     * bits; 448 is the largest value, 0x7f and 0xff are NaN, there is no
+     * infinity.  A row of C values is C bytes, at any address, and
+     * ceil(C / 128) blocks of 128 with a scale each, fp32, in a tensor of its
+     * own: [R][ceil(C/128)] for the rows of activations, [ceil(R/128)]
+     * [ceil(C/128)] for weights, whose blocks are 128 rows of 128. */
+    CNN_F8 = 4
 } cnn_dtype;
 
 /* x [rows][cols] (fp32, bf16 or fp16) to mx4: s = floor(log2(a)) - 2 + 127
@@ -297,6 +304,93 @@ int cnn_route_fwd(const void* logits, int type, int T, int E, int k, int renorma
  * [0, M) adds nothing, whatever its weight. */
 int cnn_combine_fwd(const void* x, int type, int M, int D, const int32_t* slot,
                     const float* weight, int N, int k, void* y, cnn_stream_t stream);
+
+/* ---------------------------------------------------------------- norm, 8-bit floats, sampling
+ * What a decode step does around its products and after the last of them:
+ *   cnn_rms_norm_fwd   the residual's addition and the norm, to 8 bits where a
+ *                      product on 8 bits follows
+ *   cnn_fc_f8_fwd      that product
+ *   cnn_sample_fwd     a token from the last product's results
+ * with weights brought to 8 bits once, by cnn_f8_quantize.  Nothing here reads
+ * device data on the host, so that all of it can be captured.  Results do not
+ * change from call to call.
+ */
+
+/* x [rows][cols] (fp32, bf16 or fp16) to f8, block_rows = 1 for activations or
+ * 128 for weights.  With a = max(the block's largest magnitude, 2^-100):
+ * scale = a / 448, and every value times f = 448 / a (both quotients and the
+ * products rounded to fp32), rounded to the nearest f8, ties to the even code.  A
+ * block with a NaN or an infinity gets NaN for its scale, and zeros.
+ * q uint8 [rows][cols]; scale fp32 [ceil(rows/block_rows)][ceil(cols/128)]. */
+int cnn_f8_quantize(const void* x, int x_type, int rows, int cols, int block_rows,
+                    uint8_t* q, float* scale, cnn_stream_t stream);
+
+/* The values of f8 rows, each times its block's scale in fp32, rounded to y's type. */
+int cnn_f8_dequantize(const uint8_t* q, const float* scale, int rows, int cols,
+                      int block_rows, void* y, int y_type, cnn_stream_t stream);
+
+/* Root-mean-square norm of rows, after the residual's addition:
+ *   s = x + residual (fp32)     y[r,c] = s[r,c] / sqrt(mean over c of s[r,c]^2 + eps) * weight[c]
+ *   x, residual [rows][cols], fp32, bf16 or fp16, one type; residual or NULL
+ *   weight fp32 [cols] or NULL (ones)      eps finite, 0 or more
+ *   sum [rows][cols], s rounded to x's type, or NULL
+ *   y [rows][cols]; y_type that of x (then y_scale is NULL), or CNN_F8: brought
+ *     to 8 bits from the fp32 results as by cnn_f8_quantize with block_rows 1,
+ *     y_scale fp32 [rows][ceil(cols/128)]
+ * The norm is of s as it is before it is rounded.  Squares are summed in 64
+ * bits.  y (if not CNN_F8) and sum may each be x or residual, but not both the
+ * same one. */
+int cnn_rms_norm_fwd(const void* x, const void* residual, int type, int rows, int cols,
+                     const float* weight, float eps, void* sum, void* y, int y_type,
+                     float* y_scale, cnn_stream_t stream);
+
+/* Fully-connected layer on f8, a scale for each block of 128:
+ *   y[n,o] = b[o] + sum over blocks k of (x_scale[n,k] * w_scale[o/128,k]) *
+ *            sum over i in block k of x[n,i] * w[o,i]
+ *   x [N][I], x_scale [N][ceil(I/128)]
+ *   w [O][I], w_scale [ceil(O/128)][ceil(I/128)]       bias fp32 [O] or NULL
+ *   y [N][O], fp32, bf16 or fp16
+ * Sums are fp32, the product of two scales is rounded to fp32 (and has to be in
+ * its range), the result is rounded once.  fuse_relu = 1 applies y = y > 0 ? y : +0
+ * (so NaN becomes 0). */
+int cnn_fc_f8_fwd(const uint8_t* x, const float* x_scale, int N, int I,
+                  const uint8_t* w, const float* w_scale, const float* bias, int O,
+                  int fuse_relu, void* y, int y_type, void* ws, size_t ws_bytes,
+                  cnn_stream_t stream);
+
+/* Device workspace of cnn_fc_f8_fwd (16-byte aligned, 64 MiB at most), as
+ * cnn_fc_mx4_workspace_bytes. */
+size_t cnn_fc_f8_workspace_bytes(int N, int I, int O);
+
+/* A token for each row of logits, from a random number of the caller's.
+ *   logits [N][V], fp32, bf16 or fp16
+ *   u fp32 [N], uniform in [0, 1)
+ *   temperature, top_p, min_p fp32 [N], top_k int32 [N], in device memory, or
+ *     NULL: 1, 1, 0 and none for every row
+ *   token int32 [N]         prob fp32 [N], or NULL
+ * Token i weighs w_i = exp((l_i - max l) / temperature).  In the order of falling
+ * logits, ties to the lower token, the row keeps
+ *   the first top_k tokens (all, if top_k <= 0),
+ *   of those the ones before which weights of less than top_p of theirs stand,
+ *     and the first in any case (all, if top_p >= 1),
+ *   of those the ones with w_i >= min_p (the first always).
+ * token is the first one, by number, at which the sum of the weights kept
+ * exceeds u times all of it; u below 0 counts as 0, and 1 and more as just below 1.  prob
+ * is its weight over that sum.  temperature = 0 takes the largest logit's, with
+ * prob 1.  Minus infinity and NaN are never taken; beside plus infinity no
+ * finite logit is.  A row without anything to take, or with a temperature
+ * that is negative, NaN or infinite, or NaN for u, top_p or min_p, gets -1, and prob 0.
+ * Weights are held to 2^-51 of the largest (2^-(63 - log2 V) for V above 2^12) and summed
+ * as whole numbers, so that the order of additions changes nothing: a weight
+ * below half of that is never drawn. */
+int cnn_sample_fwd(const void* logits, int type, int N, int V, const float* u,
+                   const float* temperature, const int32_t* top_k, const float* top_p,
+                   const float* min_p, int32_t* token, float* prob, void* ws,
+                   size_t ws_bytes, cnn_stream_t stream);
+
+/* Device workspace of cnn_sample_fwd (8-byte aligned; 0 for many rows or few
+ * logits, and on error).  Calls that overlap need workspaces of their own. */
+size_t cnn_sample_workspace_bytes(int type, int N, int V);
 
 /* ---------------------------------------------------------------- networks
  * A network is an array of layer descriptors executed in order (the paper's

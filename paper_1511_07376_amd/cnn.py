@@ -1,8 +1,9 @@
 """Python binding of libcnn (include/cnn.h): argument marshalling only.
 
 Every function here checks that its tensors are contiguous float32 CUDA
-(ROCm) tensors (those of the section on mixtures of experts: contiguous, on one
-GPU, of the types and shapes they state), passes their device pointers and the current torch stream to
+(ROCm) tensors (those of the sections on mixtures of experts and on the norm,
+8-bit floats and sampling: contiguous, on one GPU, of the types and shapes they
+state), passes their device pointers and the current torch stream to
 the C entry point of the same name, and raises ``CnnError`` with
 ``cnn_last_error()`` on a non-OK status.  All computation happens in the HIP
 kernels of libcnn; torch provides device memory and the stream.  Importing
@@ -38,7 +39,7 @@ CNN_OK, CNN_ERR_INVALID, CNN_ERR_UNSUPPORTED, CNN_ERR_HIP, CNN_ERR_WORKSPACE = 0
 CNN_POOL_MAX, CNN_POOL_AVG = 0, 1
 CNN_LAYER_CONV, CNN_LAYER_FC, CNN_LAYER_POOL, CNN_LAYER_LRN, CNN_LAYER_RELU = 0, 1, 2, 3, 4
 CNN_LAYER_SOFTMAX = 5
-CNN_F32, CNN_BF16, CNN_F16, CNN_MX4 = 0, 1, 2, 3
+CNN_F32, CNN_BF16, CNN_F16, CNN_MX4, CNN_F8 = 0, 1, 2, 3, 4
 
 
 class cnn_layer_desc(ctypes.Structure):
@@ -78,6 +79,15 @@ lib.cnn_route_workspace_bytes.argtypes = [_i, _i, _i]
 lib.cnn_route_workspace_bytes.restype = ctypes.c_size_t
 lib.cnn_route_fwd.argtypes = [_p, _i, _i, _i, _i, _i, _p, _p, _p, _p, _p, _p, ctypes.c_size_t, _p]
 lib.cnn_combine_fwd.argtypes = [_p, _i, _i, _i, _p, _p, _i, _i, _p, _p]
+lib.cnn_f8_quantize.argtypes = [_p, _i, _i, _i, _i, _p, _p, _p]
+lib.cnn_f8_dequantize.argtypes = [_p, _p, _i, _i, _i, _p, _i, _p]
+lib.cnn_rms_norm_fwd.argtypes = [_p, _p, _i, _i, _i, _p, ctypes.c_float, _p, _p, _i, _p, _p]
+lib.cnn_fc_f8_fwd.argtypes = [_p, _p, _i, _i, _p, _p, _p, _i, _i, _p, _i, _p, ctypes.c_size_t, _p]
+lib.cnn_fc_f8_workspace_bytes.argtypes = [_i, _i, _i]
+lib.cnn_fc_f8_workspace_bytes.restype = ctypes.c_size_t
+lib.cnn_sample_fwd.argtypes = [_p, _i, _i, _i, _p, _p, _p, _p, _p, _p, _p, _p, ctypes.c_size_t, _p]
+lib.cnn_sample_workspace_bytes.argtypes = [_i, _i, _i]
+lib.cnn_sample_workspace_bytes.restype = ctypes.c_size_t
 
 
 class cnn_netfile_config(ctypes.Structure):
@@ -124,6 +134,7 @@ for _name in ("cnn_conv2d_out_shape", "cnn_pool_out_shape", "cnn_conv2d_fwd", "c
               "cnn_pool_fwd", "cnn_lrn_fwd", "cnn_relu_fwd", "cnn_softmax_fwd", "cnn_net_out_shape",
               "cnn_mx4_quantize", "cnn_mx4_dequantize", "cnn_fc_mx4_fwd", "cnn_fc_grouped_fwd",
               "cnn_route_fwd", "cnn_combine_fwd",
+              "cnn_f8_quantize", "cnn_f8_dequantize", "cnn_rms_norm_fwd", "cnn_fc_f8_fwd", "cnn_sample_fwd",
               "cnn_net_fwd",
               "cnn_net_fwd_timed", "cnn_net_fwd_kernel_timed", "cnn_net_fwd_dump", "cnn_net_fwd_noalloc",
               "cnn_conv2d_fwd_config",
@@ -137,6 +148,8 @@ EXPORTED = ("cnn_conv2d_out_shape", "cnn_pool_out_shape", "cnn_conv2d_fwd", "cnn
             "cnn_mx4_quantize", "cnn_mx4_dequantize", "cnn_fc_mx4_fwd", "cnn_fc_grouped_fwd",
             "cnn_fc_mx4_workspace_bytes", "cnn_fc_grouped_workspace_bytes",
             "cnn_route_workspace_bytes", "cnn_route_fwd", "cnn_combine_fwd",
+            "cnn_f8_quantize", "cnn_f8_dequantize", "cnn_rms_norm_fwd", "cnn_fc_f8_fwd",
+            "cnn_fc_f8_workspace_bytes", "cnn_sample_fwd", "cnn_sample_workspace_bytes",
             "cnn_net_workspace_bytes", "cnn_net_fwd", "cnn_net_fwd_timed", "cnn_net_fwd_kernel_timed",
             "cnn_net_fwd_dump",
             "cnn_net_fwd_noalloc", "cnn_last_error",
@@ -627,6 +640,208 @@ def cnn_combine_fwd(x, slot, weight, y=None, stream=None):
         yp = _on(y, "y", device, x.dtype, (N, D))
     _ok(lib.cnn_combine_fwd(xp, code, M, D, sp, wp, N, k, yp, st))
     return y
+
+
+# ---------------------------------------------------------------- norm, 8-bit floats, sampling
+_F8 = torch.float8_e4m3fn
+
+_fc_f8_workspace = functools.lru_cache(maxsize=4096)(lib.cnn_fc_f8_workspace_bytes)
+_sample_workspace = functools.lru_cache(maxsize=4096)(lib.cnn_sample_workspace_bytes)
+
+
+def _f8_shapes(lead, cols: int, block_rows: int, what: str):
+    """(rows, shape of the scales) of f8 rows [lead][cols]; blocks of 128 rows: of one matrix."""
+    if block_rows not in (1, 128):
+        raise ValueError(f"{what}: blocks of {block_rows} rows, not 1 or 128")
+    if block_rows == 128 and len(lead) != 1:
+        raise ValueError(f"{what}: blocks of 128 rows are those of a matrix [rows][cols]")
+    rows = 1
+    for d in lead:
+        rows *= d
+    blocks = (cols + 127) // 128
+    return rows, (lead + (blocks,) if block_rows == 1 else ((rows + 127) // 128, blocks))
+
+
+def cnn_f8_quantize(x, block_rows=1, q=None, scale=None, stream=None):
+    """x [rows][cols] -> (q float8_e4m3fn [rows][cols], scale float32 [ceil(rows/block_rows)][ceil(cols/128)]): f8
+    (CNN_F8), block_rows 1 for activations or 128 for weights.
+
+    With block_rows 1 leading dimensions are kept: x [G][N][I] gives q [G][N][I] and scale [G][N][blocks]."""
+    device = _gpu(x, "x")
+    if stream is not None or device.index != _current_gpu():
+        with _there(device, stream):
+            return cnn_f8_quantize(x, block_rows, q, scale)
+    if x.dim() < 2:
+        raise ValueError("f8_quantize: x must be [rows][cols]")
+    lead, cols = tuple(x.shape[:-1]), x.shape[-1]
+    rows, scales = _f8_shapes(lead, cols, block_rows, "f8_quantize")
+    if max(rows, cols) > _INT_MAX:
+        _too_large("f8_quantize")
+    code = _wide(x.dtype, "x")
+    xp = _on(x, "x", device)
+    st = _raw_stream(device.index)
+    if q is None:
+        q = torch.empty(x.shape, dtype=_F8, device=device)
+        qp = q.data_ptr()
+    else:
+        qp = _on(q, "q", device, _F8, x.shape)
+    if scale is None:
+        scale = torch.empty(scales, dtype=torch.float32, device=device)
+        sp = scale.data_ptr()
+    else:
+        sp = _on(scale, "scale", device, torch.float32, scales)
+    _ok(lib.cnn_f8_quantize(xp, code, rows, cols, block_rows, qp, sp, st))
+    return q, scale
+
+
+def cnn_f8_dequantize(q, scale, block_rows=1, dtype=None, y=None, stream=None):
+    """The values of f8 rows, [...][cols], of type dtype (y's, or float32, if not given)."""
+    device = _gpu(q, "q")
+    if stream is not None or device.index != _current_gpu():
+        with _there(device, stream):
+            return cnn_f8_dequantize(q, scale, block_rows, dtype, y)
+    if q.dim() < 2:
+        raise ValueError("f8_dequantize: q must be [rows][cols]")
+    lead, cols = tuple(q.shape[:-1]), q.shape[-1]
+    rows, scales = _f8_shapes(lead, cols, block_rows, "f8_dequantize")
+    if max(rows, cols) > _INT_MAX:
+        _too_large("f8_dequantize")
+    qp = _on(q, "q", device, _F8)
+    sp = _on(scale, "scale", device, torch.float32, scales)
+    st = _raw_stream(device.index)
+    if y is None:
+        y = torch.empty(q.shape, dtype=dtype or torch.float32, device=device)
+        yp = y.data_ptr()
+    else:
+        yp = _on(y, "y", device, dtype, q.shape)
+    _ok(lib.cnn_f8_dequantize(qp, sp, rows, cols, block_rows, yp, _wide(y.dtype, "y"), st))
+    return y
+
+
+def cnn_rms_norm_fwd(x, weight=None, residual=None, eps=1e-6, f8=False, sum=None, y=None, y_scale=None, stream=None):
+    """s = x + residual; y = s / sqrt(mean of s^2 over the last dimension + eps) * weight.
+
+    x [...][cols], residual like it or None, weight float32 [cols] or None.  Returns y, of x's type; with f8 (y
+    float8_e4m3fn, y_scale float32 [...][ceil(cols/128)]); with a residual s, rounded to x's type, as one more.  y and
+    sum may each be x or residual (y not with f8), but not both the same one."""
+    device = _gpu(x, "x")
+    if stream is not None or device.index != _current_gpu():
+        with _there(device, stream):
+            return cnn_rms_norm_fwd(x, weight, residual, eps, f8, sum, y, y_scale)
+    if x.dim() < 1:
+        raise ValueError("rms_norm: x must be [...][cols]")
+    shape = x.shape
+    cols = shape[-1]
+    if cols == 0:
+        raise ValueError("rms_norm: rows of no values")
+    rows = 1
+    for d in shape[:-1]:
+        rows *= d
+    if max(rows, cols) > _INT_MAX:
+        _too_large("rms_norm")
+    code = _wide(x.dtype, "x")
+    xp = _on(x, "x", device)
+    rp = _on(residual, "residual", device, x.dtype, shape)
+    wp = _on(weight, "weight", device, torch.float32, (cols,))
+    st = _raw_stream(device.index)
+    if sum is not None:
+        if residual is None:
+            raise ValueError("rms_norm: sum goes with a residual")
+        sump = _on(sum, "sum", device, x.dtype, shape)
+    elif residual is not None:
+        sum = torch.empty(shape, dtype=x.dtype, device=device)
+        sump = sum.data_ptr()
+    else:
+        sump = None
+    if y is None:
+        y = torch.empty(shape, dtype=_F8 if f8 else x.dtype, device=device)
+        yp = y.data_ptr()
+    else:
+        yp = _on(y, "y", device, _F8 if f8 else x.dtype, shape)
+    if f8:
+        scales = shape[:-1] + ((cols + 127) // 128,)
+        if y_scale is None:
+            y_scale = torch.empty(scales, dtype=torch.float32, device=device)
+            yscalep = y_scale.data_ptr()
+        else:
+            yscalep = _on(y_scale, "y_scale", device, torch.float32, scales)
+    elif y_scale is not None:
+        raise ValueError("rms_norm: y_scale goes with f8")
+    else:
+        yscalep = None
+    _ok(lib.cnn_rms_norm_fwd(xp, rp, code, rows, cols, wp, eps, sump, yp, CNN_F8 if f8 else code, yscalep, st))
+    if f8:
+        return (y, y_scale) if residual is None else (y, y_scale, sum)
+    return y if residual is None else (y, sum)
+
+
+def cnn_fc_f8_fwd(x, x_scale, w, w_scale, bias=None, fuse_relu=False, y_dtype=None, y=None, stream=None):
+    """x float8_e4m3fn [N][I] with x_scale [N][ceil(I/128)], w float8_e4m3fn [O][I] with w_scale
+    [ceil(O/128)][ceil(I/128)] -> y [N][O], of type y_dtype (y's, or float32, if not given)."""
+    device = _gpu(x, "x")
+    if stream is not None or device.index != _current_gpu():
+        with _there(device, stream):
+            return cnn_fc_f8_fwd(x, x_scale, w, w_scale, bias, fuse_relu, y_dtype, y)
+    if x.dim() != 2 or w.dim() != 2:
+        raise ValueError("fc_f8: x must be [N][I], w [O][I]")
+    (N, I), (O, cols) = x.shape, w.shape
+    if cols != I:
+        raise ValueError(f"fc_f8: x has {I} columns, w {cols}")
+    if max(N, I, O) > _INT_MAX:
+        _too_large("fc_f8")
+    blocks = (I + 127) // 128
+    xp = _on(x, "x", device, _F8)
+    xs = _on(x_scale, "x_scale", device, torch.float32, (N, blocks))
+    wp = _on(w, "w", device, _F8)
+    ws = _on(w_scale, "w_scale", device, torch.float32, ((O + 127) // 128, blocks))
+    bp = _on(bias, "bias", device, torch.float32, (O,))
+    st = _raw_stream(device.index)
+    if y is None:
+        y = torch.empty((N, O), dtype=y_dtype or torch.float32, device=device)
+        yp = y.data_ptr()
+    else:
+        yp = _on(y, "y", device, y_dtype, (N, O))
+    need = _fc_f8_workspace(N, I, O)
+    work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    _ok(lib.cnn_fc_f8_fwd(xp, xs, N, I, wp, ws, bp, O, 1 if fuse_relu else 0, yp, _WIDE.get(y.dtype, -1),
+                          work.data_ptr() if need else None, need, st))
+    return y
+
+
+def cnn_sample_fwd(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, stream=None):
+    """logits [N][V], u float32 [N] uniform in [0, 1) -> (token int32 [N], prob float32 [N]): a token for each row, and
+    its probability among those that the row's top_k (int32 [N]), top_p and min_p (float32 [N]) keep at its temperature
+    (float32 [N]); None for a parameter that no row has.  token is -1 where there is nothing to take.
+
+    The two are parts of one allocation: it lives as long as either of them."""
+    device = _gpu(logits, "logits")
+    if stream is not None or device.index != _current_gpu():
+        with _there(device, stream):
+            return cnn_sample_fwd(logits, u, temperature, top_k, top_p, min_p)
+    if logits.dim() != 2:
+        raise ValueError("sample: logits must be [N][V]")
+    N, V = logits.shape
+    if max(N, V) > _INT_MAX:
+        _too_large("sample")
+    code = _wide(logits.dtype, "logits")
+    if u is None:
+        raise TypeError(f"u must be a tensor on {device}")
+    row = (N,)
+    lp = _on(logits, "logits", device)
+    up = _on(u, "u", device, torch.float32, row)
+    tp = _on(temperature, "temperature", device, torch.float32, row)
+    kp = _on(top_k, "top_k", device, torch.int32, row)
+    pp = _on(top_p, "top_p", device, torch.float32, row)
+    mp = _on(min_p, "min_p", device, torch.float32, row)
+    st = _raw_stream(device.index)
+    parts = torch.empty((2, N), dtype=torch.int32, device=device)
+    base = parts.data_ptr()
+    need = _sample_workspace(code, N, V)
+    work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    _ok(lib.cnn_sample_fwd(lp, code, N, V, up, tp, kp, pp, mp, base, base + 4 * N,
+                           work.data_ptr() if need else None, need, st))
+    token, prob = parts.unbind(0)
+    return token, prob.view(torch.float32)
 
 
 # ---------------------------------------------------------------- NetFile

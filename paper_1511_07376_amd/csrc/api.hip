@@ -12,6 +12,7 @@
 
 #include "common.h"
 #include "experts.h"
+#include "f8.h"
 #include "wide_types.h"
 
 namespace cnn {
@@ -197,6 +198,58 @@ int check_route(int type, int T, int E, int k) {
     if (E > kMaxExperts || k > kMaxChoices)
         return fail(CNN_ERR_UNSUPPORTED, "route: %d experts, %d choices: at most %d and %d", E, k, kMaxExperts, kMaxChoices);
     if (too_big(T, E) || T > (1 << 26)) return fail(CNN_ERR_UNSUPPORTED, "route: %d tokens", T);
+    return CNN_OK;
+}
+
+// ------------------------------------------------------------------ norm, 8-bit floats, sampling
+int check_f8(const char* what, const void* wide_side, int type, int rows, int cols, int block_rows, const uint8_t* q,
+             const float* scale) {
+    if (!wide(type)) return fail(CNN_ERR_INVALID, "%s: type %d is not fp32, bf16 or fp16", what, type);
+    if (rows < 0 || cols <= 0) return fail(CNN_ERR_INVALID, "%s: %d rows of %d", what, rows, cols);
+    if (block_rows != 1 && block_rows != kF8Block)
+        return fail(CNN_ERR_INVALID, "%s: blocks of %d rows, not 1 or %d", what, block_rows, kF8Block);
+    if (rows != 0 && (!wide_side || !q || !scale)) return fail(CNN_ERR_INVALID, "%s: null pointer", what);
+    if (too_big(rows, cols)) return fail(CNN_ERR_UNSUPPORTED, "%s: more than 2^31-1 values", what);
+    if (!aligned(wide_side, type_bytes(type)) || !aligned(scale, 4))
+        return fail(CNN_ERR_UNSUPPORTED, "%s: values or scales not aligned to their type", what);
+    return CNN_OK;
+}
+
+int check_rms_norm(const RmsNorm& p) {
+    if (!wide(p.type)) return fail(CNN_ERR_INVALID, "rms_norm: type %d is not fp32, bf16 or fp16", p.type);
+    if (p.y_type != p.type && p.y_type != CNN_F8)
+        return fail(CNN_ERR_INVALID, "rms_norm: output type %d for inputs of type %d", p.y_type, p.type);
+    if ((p.y_type == CNN_F8) != (p.y_scale != nullptr) && p.rows != 0)
+        return fail(CNN_ERR_INVALID, "rms_norm: scales go with 8-bit results, and with those only");
+    if (p.rows < 0 || p.cols <= 0) return fail(CNN_ERR_INVALID, "rms_norm: %d rows of %d", p.rows, p.cols);
+    if (!(p.eps >= 0.0f) || p.eps > 3.4e38f) return fail(CNN_ERR_INVALID, "rms_norm: eps %g", (double)p.eps);
+    if (p.rows != 0 && (!p.x || !p.y)) return fail(CNN_ERR_INVALID, "rms_norm: null x or y");
+    if (p.sum && p.sum == p.y) return fail(CNN_ERR_INVALID, "rms_norm: y and sum are the same tensor");
+    if (p.y_type == CNN_F8 && p.y && (p.y == p.x || p.y == p.residual))
+        return fail(CNN_ERR_INVALID, "rms_norm: 8-bit results in an input's place");
+    if (too_big(p.rows, p.cols)) return fail(CNN_ERR_UNSUPPORTED, "rms_norm: more than 2^31-1 values");
+    const size_t to = type_bytes(p.type);
+    if (!aligned(p.x, to) || !aligned(p.residual, to) || !aligned(p.sum, to) || (p.y_type != CNN_F8 && !aligned(p.y, to)) ||
+        !aligned(p.weight, 4) || !aligned(p.y_scale, 4))
+        return fail(CNN_ERR_UNSUPPORTED, "rms_norm: a tensor is not aligned to its type");
+    return CNN_OK;
+}
+
+int check_fc_f8(const FcF8& p) {
+    if (p.N < 0 || p.I <= 0 || p.O <= 0) return fail(CNN_ERR_INVALID, "fc_f8: N=%d I=%d O=%d", p.N, p.I, p.O);
+    if (!wide(p.y_type)) return fail(CNN_ERR_INVALID, "fc_f8: output type %d", p.y_type);
+    if (!p.w || !p.ws || (p.N != 0 && (!p.x || !p.xs || !p.y))) return fail(CNN_ERR_INVALID, "fc_f8: null pointer");
+    if (too_big(p.N, p.I) || too_big(p.N, p.O) || too_big(p.O, p.I))
+        return fail(CNN_ERR_UNSUPPORTED, "fc_f8: x, y or w exceeds 2^31-1 elements");
+    if (!aligned(p.xs, 4) || !aligned(p.ws, 4) || !aligned(p.bias, 4) || !aligned(p.y, type_bytes(p.y_type)))
+        return fail(CNN_ERR_UNSUPPORTED, "fc_f8: scales, bias or y not aligned to their type");
+    return CNN_OK;
+}
+
+int check_sample(int type, int N, int V) {
+    if (!wide(type)) return fail(CNN_ERR_INVALID, "sample: type %d is not fp32, bf16 or fp16", type);
+    if (N < 0 || V <= 0) return fail(CNN_ERR_INVALID, "sample: N=%d V=%d", N, V);
+    if (too_big(N, V)) return fail(CNN_ERR_UNSUPPORTED, "sample: more than 2^31-1 logits");
     return CNN_OK;
 }
 
@@ -822,6 +875,72 @@ int cnn_combine_fwd(const void* x, int type, int M, int D, const int32_t* slot, 
     if (!aligned(x, type_bytes(type)) || !aligned(y, type_bytes(type)) || !aligned(slot, 4) || !aligned(weight, 4))
         return fail(CNN_ERR_UNSUPPORTED, "combine: a tensor is not aligned to its type");
     return launch_combine(x, type, M, D, slot, weight, N, k, y, as_stream(stream));
+}
+
+int cnn_f8_quantize(const void* x, int x_type, int rows, int cols, int block_rows, uint8_t* q, float* scale,
+                    cnn_stream_t stream) {
+    int rc = check_f8("f8_quantize", x, x_type, rows, cols, block_rows, q, scale);
+    if (rc) return rc;
+    return launch_f8_quantize(x, x_type, rows, cols, block_rows, q, scale, as_stream(stream));
+}
+
+int cnn_f8_dequantize(const uint8_t* q, const float* scale, int rows, int cols, int block_rows, void* y, int y_type,
+                      cnn_stream_t stream) {
+    int rc = check_f8("f8_dequantize", y, y_type, rows, cols, block_rows, q, scale);
+    if (rc) return rc;
+    return launch_f8_dequantize(q, scale, rows, cols, block_rows, y, y_type, as_stream(stream));
+}
+
+int cnn_rms_norm_fwd(const void* x, const void* residual, int type, int rows, int cols, const float* weight, float eps,
+                     void* sum, void* y, int y_type, float* y_scale, cnn_stream_t stream) {
+    const RmsNorm p{x, residual, weight, sum, y, y_scale, type, y_type, rows, cols, eps};
+    int rc = check_rms_norm(p);
+    if (rc) return rc;
+    return launch_rms_norm(p, as_stream(stream));
+}
+
+size_t cnn_fc_f8_workspace_bytes(int N, int I, int O) {
+    if (N <= 0 || I <= 0 || O <= 0 || too_big(N, I) || too_big(N, O) || too_big(O, I)) return 0;
+    FcF8 p{};
+    p.N = N;
+    p.I = I;
+    p.O = O;
+    return fc_f8_workspace(p);
+}
+
+int cnn_fc_f8_fwd(const uint8_t* x, const float* x_scale, int N, int I, const uint8_t* w, const float* w_scale,
+                  const float* bias, int O, int fuse_relu, void* y, int y_type, void* ws, size_t ws_bytes,
+                  cnn_stream_t stream) {
+    const FcF8 p{x, x_scale, w, w_scale, bias, y, y_type, N, I, O, fuse_relu != 0};
+    int rc = check_fc_f8(p);
+    if (rc || N == 0) return rc;
+    const size_t need = fc_f8_workspace(p);
+    if (need > 0 && (!ws || ws_bytes < need))
+        return fail(CNN_ERR_WORKSPACE, "fc_f8: workspace of %zu bytes, %zu needed", ws ? ws_bytes : 0, need);
+    if (!aligned(ws, 16)) return fail(CNN_ERR_UNSUPPORTED, "fc_f8: workspace not 16-byte aligned");
+    return launch_fc_f8(p, reinterpret_cast<float*>(ws), as_stream(stream));
+}
+
+size_t cnn_sample_workspace_bytes(int type, int N, int V) {
+    if (check_sample(type, N, V) || N == 0) return 0;
+    return sample_workspace(type, N, V);
+}
+
+int cnn_sample_fwd(const void* logits, int type, int N, int V, const float* u, const float* temperature,
+                   const int32_t* top_k, const float* top_p, const float* min_p, int32_t* token, float* prob, void* ws,
+                   size_t ws_bytes, cnn_stream_t stream) {
+    int rc = check_sample(type, N, V);
+    if (rc) return rc;
+    if (N != 0 && (!logits || !u || !token)) return fail(CNN_ERR_INVALID, "sample: null pointer");
+    if (!aligned(logits, type_bytes(type)) || !aligned(u, 4) || !aligned(temperature, 4) || !aligned(top_k, 4) ||
+        !aligned(top_p, 4) || !aligned(min_p, 4) || !aligned(token, 4) || !aligned(prob, 4) || !aligned(ws, 8))
+        return fail(CNN_ERR_UNSUPPORTED, "sample: a tensor is not aligned to its type");
+    if (N == 0) return CNN_OK;
+    const size_t need = sample_workspace(type, N, V);
+    if (need > 0 && (!ws || ws_bytes < need))
+        return fail(CNN_ERR_WORKSPACE, "sample: workspace of %zu bytes, %zu needed", ws ? ws_bytes : 0, need);
+    const Sample p{logits, u, temperature, top_k, top_p, min_p, token, prob, type, N, V};
+    return launch_sample(p, ws, as_stream(stream));
 }
 
 int cnn_net_out_shape(const cnn_layer_desc* layers, int n_layers, int N, int C, int H, int W,
