@@ -901,11 +901,7 @@ int cnn_rms_norm_fwd(const void* x, const void* residual, int type, int rows, in
 
 size_t cnn_fc_f8_workspace_bytes(int N, int I, int O) {
     if (N <= 0 || I <= 0 || O <= 0 || too_big(N, I) || too_big(N, O) || too_big(O, I)) return 0;
-    FcF8 p{};
-    p.N = N;
-    p.I = I;
-    p.O = O;
-    return fc_f8_workspace(p);
+    return fc_f8_workspace(N, I, O);
 }
 
 int cnn_fc_f8_fwd(const uint8_t* x, const float* x_scale, int N, int I, const uint8_t* w, const float* w_scale,
@@ -914,7 +910,7 @@ int cnn_fc_f8_fwd(const uint8_t* x, const float* x_scale, int N, int I, const ui
     const FcF8 p{x, x_scale, w, w_scale, bias, y, y_type, N, I, O, fuse_relu != 0};
     int rc = check_fc_f8(p);
     if (rc || N == 0) return rc;
-    const size_t need = fc_f8_workspace(p);
+    const size_t need = fc_f8_workspace(N, I, O);
     if (need > 0 && (!ws || ws_bytes < need))
         return fail(CNN_ERR_WORKSPACE, "fc_f8: workspace of %zu bytes, %zu needed", ws ? ws_bytes : 0, need);
     if (!aligned(ws, 16)) return fail(CNN_ERR_UNSUPPORTED, "fc_f8: workspace not 16-byte aligned");

@@ -39,7 +39,7 @@ struct FcF8 {
     void* y;
     int y_type, N, I, O, relu;
 };
-size_t fc_f8_workspace(const FcF8& p);
+size_t fc_f8_workspace(int N, int I, int O);
 int launch_fc_f8(const FcF8& p, float* ws, hipStream_t st);
 struct Sample {
     const void* logits;

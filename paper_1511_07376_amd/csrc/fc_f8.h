@@ -91,9 +91,10 @@ __device__ inline void store_value(int type, void* y, size_t at, float v) {
     else ((f16_t*)y)[at] = from_f32<f16_t>(v);
 }
 
-// A tile's size, and the parts its reduction is split into (over workgroups, joined by a second kernel).
+// A tile's size, and the parts its reduction is split into (over workgroups, joined by a second
+// kernel), of `run` blocks each, a multiple of 4.
 struct F8Tile {
-    int outs, tokens, parts;
+    int outs, tokens, parts, run;
 };
 void run_f8_tiles(const FcF8& p, const F8Tile& tile, bool vec, float* partial, hipStream_t st);
 

@@ -12,55 +12,68 @@ namespace {
 
 constexpr int kMostWaves = 16;
 
-// 16 outputs of 16 NT tokens a workgroup, whose waves share the blocks: the weights are read
+// 16 FO outputs of 16 NT tokens a workgroup, whose waves share the blocks: the weights are read
 // once for all of them, straight to registers.
-template <int NT>
+template <int NT, int FO>
 __global__ void __launch_bounds__(64 * kMostWaves) fc_f8_rows(FcF8 p, int blocks, int out_groups, int jobs) {
-    __shared__ float part[kMostWaves][16 * NT][17];
+    __shared__ float part[kMostWaves][16 * NT][16 * FO + 1];
     const int waves = blockDim.x >> 6, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, l16 = lane & 15, quarter = lane >> 4;
     const int each = (int)(((int64_t)blocks + waves - 1) / waves);
     const int first = (int)min((int64_t)wave * each, (int64_t)blocks), last = (int)min((int64_t)first + each, (int64_t)blocks);
     const int whole = min(last, p.I / kF8Block);
     for (int job = blockIdx.x; job < jobs; job += gridDim.x) {
-        const int o0 = job % out_groups * 16;
+        const int o0 = job % out_groups * (16 * FO);
         const int64_t n0 = (int64_t)(job / out_groups) * (16 * NT);
-        const uint8_t* w = p.w + (size_t)min((int64_t)o0 + l16, (int64_t)p.O - 1) * p.I + quarter * 32;
         const float* ws = p.ws + (size_t)(o0 >> 7) * blocks;
-        const uint8_t* x[NT];
-        const float* xs[NT];
-        f32x4 acc[NT];
+        // (offsets of 32 bits: a tensor has fewer than 2^31 bytes)
+        unsigned w[FO], x[NT], xs[NT];
+        f32x4 acc[FO][NT];
+#pragma unroll
+        for (int i = 0; i < FO; ++i) w[i] = (unsigned)min((int64_t)o0 + 16 * i + l16, (int64_t)p.O - 1) * (unsigned)p.I + quarter * 32;
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
-            const int64_t n = min(n0 + 16 * j + l16, (int64_t)p.N - 1);
-            x[j] = p.x + (size_t)n * p.I + quarter * 32;
-            xs[j] = p.xs + (size_t)n * blocks;
-            acc[j] = f32x4{0, 0, 0, 0};
+            const unsigned n = (unsigned)min(n0 + 16 * j + l16, (int64_t)p.N - 1);
+            x[j] = n * (unsigned)p.I + quarter * 32;
+            xs[j] = n * (unsigned)blocks;
+#pragma unroll
+            for (int i = 0; i < FO; ++i) acc[i][j] = f32x4{0, 0, 0, 0};
         }
-#pragma unroll 2
+        auto add = [&](int k, auto&& load) {
+            Halves a[FO];
+            Bytes raw[FO], b[NT];
+            float s[NT];
+#pragma unroll
+            for (int i = 0; i < FO; ++i) raw[i] = load(p.w, w[i]);
+#pragma unroll
+            for (int j = 0; j < NT; ++j) b[j] = load(p.x, x[j]), s[j] = (p.xs + k)[xs[j]] * ws[k];
+#pragma unroll
+            for (int i = 0; i < FO; ++i) a[i] = to_halves(raw[i]);
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                const Halves h = to_halves(b[j]);
+#pragma unroll
+                for (int i = 0; i < FO; ++i) add_scaled(acc[i][j], block_sums(a[i], h), s[j]);
+            }
+        };
         for (int k = first; k < whole; ++k) {
             const int64_t at = (int64_t)k * kF8Block;
-            const Halves a = to_halves(Bytes{load16(w + at), load16(w + at + 16)});
-            const float s = ws[k];
-#pragma unroll
-            for (int j = 0; j < NT; ++j)
-                add_scaled(acc[j], block_sums(a, to_halves(Bytes{load16(x[j] + at), load16(x[j] + at + 16)})), xs[j][k] * s);
+            add(k, [&](const uint8_t* base, unsigned row) { return Bytes{load16(base + at + row), load16(base + at + row + 16)}; });
         }
         if (whole < last) {
             const int64_t at = (int64_t)whole * kF8Block, in = at + quarter * 32, left = p.I - in;
-            auto edge = [&](const uint8_t* row) {
-                return to_halves(Bytes{load_bytes_edge(row + at, left, in), load_bytes_edge(row + at + 16, left - 16, in + 16)});
-            };
-            const Halves a = edge(w);
-#pragma unroll
-            for (int j = 0; j < NT; ++j) add_scaled(acc[j], block_sums(a, edge(x[j])), xs[j][whole] * ws[whole]);
+            add(whole, [&](const uint8_t* base, unsigned row) {
+                return Bytes{load_bytes_edge(base + at + row, left, in), load_bytes_edge(base + at + row + 16, left - 16, in + 16)};
+            });
         }
 #pragma unroll
         for (int j = 0; j < NT; ++j)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) part[wave][16 * j + l16][quarter * 4 + i] = acc[j][i];
+            for (int i = 0; i < FO; ++i)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) part[wave][16 * j + l16][16 * i + quarter * 4 + c] = acc[i][j][c];
         __syncthreads();
-        for (int e = threadIdx.x; e < 256 * NT; e += blockDim.x) {
-            const int t = e >> 4, c = e & 15;
+        for (int e = threadIdx.x; e < 256 * NT * FO; e += blockDim.x) {
+            const int t = e / (16 * FO), c = e % (16 * FO);
             if (n0 + t >= p.N || (int64_t)o0 + c >= p.O) continue;
             float v = 0.0f;
             for (int q = 0; q < waves; ++q) v += part[q][t][c];
@@ -70,39 +83,84 @@ __global__ void __launch_bounds__(64 * kMostWaves) fc_f8_rows(FcF8 p, int blocks
     }
 }
 
-template <int NT>
+template <int NT, int FO>
 void run_rows(const FcF8& p, hipStream_t st) {
-    const int blocks = f8_blocks(p.I), groups = ceil_div(p.O, 16);
+    const int blocks = f8_blocks(p.I), groups = ceil_div(p.O, 16 * FO);
     const int64_t jobs = (int64_t)groups * ceil_div(p.N, 16 * NT);
     const int waves = std::max(1, std::min(kMostWaves, blocks / 2));
-    enqueue(fc_f8_rows<NT>, dim3((unsigned)std::min<int64_t>(jobs, 1 << 20)), dim3(64 * waves), 0, st, p, blocks, groups, (int)jobs);
+    enqueue(fc_f8_rows<NT, FO>, dim3((unsigned)std::min<int64_t>(jobs, 1 << 20)), dim3(64 * waves), 0, st, p, blocks, groups, (int)jobs);
 }
 
-bool few_rows(const FcF8& p) { return p.N <= 64; }
+// Few tokens: the weights are streamed.  4096 x 4096 weights, 16 tokens: 8.0 us against 10.8 on tiles, 32 tokens 10.7 against 11.6;
+// 9216 x 8192, 16 tokens 18.1 against 19.3, 32 tokens 26 against 20.9: there every workgroup reads all inputs again.
+bool few_rows(int N, int I, int O) { return N <= 16 || (N <= 32 && (int64_t)I * O <= 24 << 20); }
 
-F8Tile choose_tile(const FcF8& p) {
-    const int64_t large = (int64_t)ceil_div(p.O, 256) * ceil_div(p.N, 256);
-    if (large >= 192) return {256, 256, 1};
-    return {128, 128, 1};
+// A tile's time is its blocks' times, which grow with the workgroups that share a compute unit, and some 3.5 us around
+// them; parts take a second kernel, and their way through memory.  As measured between 64 x 1024 and 4096 x
+// 8192 results of 2048 to 9216 values.
+struct TileCost {
+    int outs, tokens, slots;  // slots: workgroups that a compute unit holds
+    float half, one, two;     // us a block with 128 workgroups or fewer, with 256, with 512
+};
+constexpr TileCost kCosts16[] = {{128, 64, 3, 0.40f, 0.62f, 0.76f}, {128, 128, 2, 0.70f, 0.85f, 1.30f}, {256, 128, 1, 0.95f, 1.15f, 0}, {256, 256, 1, 1.57f, 2.1f, 0}};
+constexpr TileCost kCosts32[] = {{128, 64, 3, 0.77f, 0.86f, 1.32f}, {128, 128, 2, 1.27f, 1.56f, 2.23f}};
+constexpr int kMostParts = 16;
+constexpr size_t kMostWorkspace = 64 << 20;
+
+float block_time(const TileCost& c, int64_t jobs) {
+    const float at = (float)jobs / 256.0f;
+    return at <= 0.5f ? c.half : at <= 1 ? c.half + (c.one - c.half) * (2 * at - 1) : c.one + (c.two - c.one) * (at - 1);
+}
+
+// By sizes and the type alone (the workspace is sized before the call's pointers are known).
+F8Tile choose_tile(int N, int I, int O, bool wide32) {
+    const int blocks = f8_blocks(I);
+    F8Tile best{128, 64, 1, blocks};
+    float least = 3e38f;
+    const TileCost* costs = wide32 ? kCosts32 : kCosts16;
+    for (int c = 0; c < (wide32 ? 2 : 4); ++c) {
+        const TileCost& cost = costs[c];
+        if (cost.outs == 256 && I % kF8Block != 0) continue;
+        const int64_t tiles = (int64_t)ceil_div(O, cost.outs) * ceil_div(N, cost.tokens), round = 256 * cost.slots;
+        for (int parts = 1; parts <= kMostParts; ++parts) {
+            const int run = parts == 1 ? blocks : ceil_div(ceil_div(blocks, parts), 4) * 4;
+            const float bytes = (float)parts * N * O * 4.0f;
+            if (parts > 1 && (ceil_div(blocks, run) != parts || bytes > (float)kMostWorkspace || tiles * parts > round)) continue;
+            const int64_t jobs = tiles * parts, full = jobs / round, rest = jobs % round;
+            const float each = (float)full * block_time(cost, round) + (rest ? block_time(cost, rest) : 0.0f);
+            const float time = (float)run * each + (parts > 1 ? 2.5f + 0.75e-6f * bytes : 0.0f);
+            if (time < least) least = time, best = F8Tile{cost.outs, cost.tokens, parts, run};
+        }
+    }
+    return best;
 }
 
 }  // namespace
 
-size_t fc_f8_workspace(const FcF8& p) {
-    if (p.N == 0 || few_rows(p)) return 0;
-    const F8Tile t = choose_tile(p);
-    return t.parts > 1 ? (size_t)t.parts * p.N * p.O * sizeof(float) : 0;
+// The type decides too: the larger of the two needs.
+size_t fc_f8_workspace(int N, int I, int O) {
+    if (few_rows(N, I, O)) return 0;
+    size_t need = 0;
+    for (const bool wide32 : {false, true}) {
+        const F8Tile t = choose_tile(N, I, O, wide32);
+        if (t.parts > 1) need = std::max(need, (size_t)t.parts * N * O * sizeof(float));
+    }
+    return need;
 }
 
 int launch_fc_f8(const FcF8& p, float* ws, hipStream_t st) {
     if (p.N == 0) return CNN_OK;
-    if (few_rows(p)) {
-        if (p.N <= 16) run_rows<1>(p, st);
-        else if (p.N <= 32) run_rows<2>(p, st);
-        else run_rows<4>(p, st);
+    if (few_rows(p.N, p.I, p.O)) {
+        // 32 outputs a workgroup read the inputs half as often, where there are enough of them: 9216 x 8192, 1 token 16.8 to
+        // 14.4 us, 16 tokens 27 to 18; 4096 x 4096 5.9 and 8.0 against 7.5 and 9.7
+        if (p.N > 16) run_rows<2, 1>(p, st);
+        else if (p.O > 6144) run_rows<1, 2>(p, st);
+        else run_rows<1, 1>(p, st);
     } else {
-        const bool vec = (uintptr_t)p.x % 16 == 0 && (uintptr_t)p.w % 16 == 0 && p.I % 16 == 0;
-        run_f8_tiles(p, choose_tile(p), vec, ws, st);
+        const bool vec = (uintptr_t)p.x % 16 == 0 && (uintptr_t)p.w % 16 == 0 && p.I % kF8Block == 0;
+        F8Tile t = choose_tile(p.N, p.I, p.O, p.y_type == CNN_F32);
+        if (!vec && t.outs == 256) t.outs = t.tokens = 128;  // rows of whole vectors at an address that is none
+        run_f8_tiles(p, t, vec, ws, st);
     }
     return check_launch("fc_f8");
 }

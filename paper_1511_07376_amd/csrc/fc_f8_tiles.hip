@@ -17,15 +17,14 @@
 namespace cnn {
 namespace {
 
-static __device__ const u32x4 kZeroVector = {0, 0, 0, 0};
-
 // WO x WT waves of FO x FT fragments of 16.
 template <int WO, int WT, int FO, int FT>
 struct Shape {
     static constexpr int TO = WO * FO * 16, TT = WT * FT * 16, NT = 64 * WO * WT;
     static_assert(FO * 16 <= kF8Block, "a wave's outputs share their scale");
-    // exchange of a row's vectors
-    static __device__ int out_key(int row) { return (row & 3) | ((row / (FO * 4)) & 1) << 2; }
+    // Exchange of a row's vectors, by three bits in which 8 neighbouring lanes' rows differ.  A lane reads vectors q and
+    // q + 4 of its row (q: a quarter of the wave): 4.2 cycles a read of a wave; of 2 q and 2 q + 1 it would be 8.2.
+    static __device__ int out_key(int row) { return (row & 3) | (row / (FO * 4) & 1) << 2; }
     static __device__ int token_key(int row) { return row & 7; }
 };
 
@@ -33,13 +32,17 @@ struct TileParams {
     FcF8 fc;
     int blocks;           // of the reduction
     int out_tiles, tiles;
-    int parts, run;       // parts of the reduction, blocks of each
+    int parts, run;       // parts of the reduction, blocks of each (a multiple of 4)
+    bool whole_scales;    // a row's scales are whole 16-byte vectors
     float* partial;       // [parts][N][O] if parts > 1
 };
 
-__device__ inline void copy16(const uint8_t* src, char* dst) {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
-                                     (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
+// 64 lanes' 16 (4) bytes to consecutive places in LDS.
+__device__ inline void copy16(const void* src, char* dst) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
+}
+__device__ inline void copy4(const void* src, char* dst) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, (__attribute__((address_space(3))) void*)dst, 4, 0, 0);
 }
 
 // One operand's vectors of a block, of this work-item: ROWS rows, NT work-items.  Places are
@@ -59,16 +62,16 @@ struct Fetch {
 #pragma unroll
         for (int i = 0; i < N; ++i) at[i] = (unsigned)min(row0 + row_of(i), (int64_t)rows - 1) * (unsigned)cols + (unsigned)(vector_of(i) * 16);
     }
-    // Block k of rows of `cols` values.  FULL: all of it is in them.
-    template <bool FULL>
+    // Block k of rows of `cols` values.
     __device__ void load(const uint8_t* base, int k, int cols, char* lds) {
         base += (int64_t)k * kF8Block;
+        const int wave0 = __builtin_amdgcn_readfirstlane((int)threadIdx.x) & ~63;  // the wave's vectors are consecutive
         const int64_t left = cols - (int64_t)k * kF8Block;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int in = vector_of(i) * 16;
-            if constexpr (VEC) copy16(FULL || in < left ? base + at[i] : (const uint8_t*)&kZeroVector, lds + (i * NT + (int)(threadIdx.x & ~63u)) * 16);
-            else if (FULL || left >= kF8Block) reg[i] = load16(base + at[i]);
+            if constexpr (VEC) copy16(base + at[i], lds + (i * NT + wave0) * 16);
+            else if (left >= kF8Block) reg[i] = load16(base + at[i]);
             else reg[i] = load_bytes_edge(base + at[i], left - in, (int64_t)k * kF8Block + in);
         }
     }
@@ -88,13 +91,16 @@ struct TokenKey {
     static __device__ int of(int row) { return S::token_key(row); }
 };
 
-// All loads of the wave have landed, its LDS accesses are done; then all waves'.
+// All the wave's loads have landed, its LDS accesses are done; then all waves'.
 __device__ inline void block_barrier() {
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_waitcnt(0x70);  // vmcnt(0) lgkmcnt(0)
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 }
+
+template <int N>
+using Step = std::integral_constant<int, N>;
 
 // 4 FO neighbours of a token.
 template <int YT, int N>
@@ -128,9 +134,13 @@ __global__ void __launch_bounds__(64 * WO * WT, 2) fc_f8_tiles(TileParams tp) {
     constexpr int TO = S::TO, TT = S::TT, NT = S::NT;
     // arrays of their own: the compiler sees that a copy into one does not concern reads of another
     __shared__ __attribute__((aligned(16))) char sW0[TO * kF8Block], sW1[TO * kF8Block], sX0[TT * kF8Block], sX1[TT * kF8Block];
+    __shared__ __attribute__((aligned(16))) float sScale[2][4 * TT];
+    static_assert(NT >= TT, "a lane a token");
+    auto wbuf = [&](auto slot) -> char* { return decltype(slot)::value ? sW1 : sW0; };
+    auto xbuf = [&](auto slot) -> char* { return decltype(slot)::value ? sX1 : sX0; };
     const FcF8& p = tp.fc;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, quarter = lane >> 4;
-    const int wo = wave / WT, wt = wave % WT;
+    const int wo = wave / WT, wt = wave % WT, uwave = __builtin_amdgcn_readfirstlane(wave);
 
     const int jobs = tp.tiles * tp.parts;
     for (int turn = blockIdx.x; turn < jobs; turn += gridDim.x) {
@@ -151,16 +161,24 @@ __global__ void __launch_bounds__(64 * WO * WT, 2) fc_f8_tiles(TileParams tp) {
         Fetch<TT, NT, VEC, TokenKey<S>> fx;
         fw.begin(o0, p.O, p.I);
         fx.begin(n0, p.N, p.I);
-        const float* ws = p.ws + (size_t)min((o0 + wo * FO * 16) >> 7, (int64_t)(p.O - 1) >> 7) * tp.blocks;
-        unsigned xs[FT];
+        const float* ws = p.ws + (size_t)min((o0 + uwave / WT * FO * 16) >> 7, (int64_t)(p.O - 1) >> 7) * tp.blocks;
+        // The inputs' scales come in groups of 4 blocks, a lane a token: a row's are neighbours, and a line for
+        // every token and block would take as long as the operands (2048 x 9216 x 4096: 99 us against 109 with half as
+        // many of them, and 77 against 100 for the copies alone).
+        const float* xs = p.xs + (size_t)min(n0 + tid % TT, (int64_t)p.N - 1) * tp.blocks;
+        float wscale[2];
+        auto ask_scales = [&](int group) {
+            if (uwave >= TT / 64) return;
+            const int k = first + 4 * group;
+            char* dst = (char*)sScale[group & 1];
+            if (tp.whole_scales) {
+                copy16(xs + k, dst + uwave * 64 * 16);
+            } else {
 #pragma unroll
-        for (int j = 0; j < FT; ++j) xs[j] = (unsigned)min(n0 + (wt * FT + j) * 16 + l16, (int64_t)p.N - 1) * (unsigned)tp.blocks;
-        float wnext = 0, xnext[FT];
-        auto load_scales = [&](int k) {
-            wnext = ws[k];
-#pragma unroll
-            for (int j = 0; j < FT; ++j) xnext[j] = (p.xs + k)[xs[j]];
+                for (int i = 0; i < 4; ++i) copy4(xs + min(k + i, tp.blocks - 1), dst + (i * TT + uwave * 64) * 4);
+            }
         };
+        const int scale_token = tp.whole_scales ? 4 : 1, scale_block = tp.whole_scales ? 1 : TT;
 
         f32x4 acc[FO][FT];
 #pragma unroll
@@ -170,75 +188,100 @@ __global__ void __launch_bounds__(64 * WO * WT, 2) fc_f8_tiles(TileParams tp) {
 
         // Rows of fragment f: (l16 / 4) 4 FO + 4 f + l16 % 4 of the outputs, 16 f + l16 of the tokens.
         const int orow = wo * FO * 16 + (l16 >> 2) * (FO * 4) + (l16 & 3), trow = wt * FT * 16 + l16;
-        // a lane's first vector of a fragment, 2 quarter; the second is an XOR with 1 away
         auto read = [&](const char* base, int row, int key) {
-            const int v = (2 * quarter) ^ key;
+            const int v = quarter ^ key;
             return Bytes{*reinterpret_cast<const u32x4*>(base + row * kF8Block + v * 16),
-                         *reinterpret_cast<const u32x4*>(base + row * kF8Block + (v ^ 1) * 16)};
+                         *reinterpret_cast<const u32x4*>(base + row * kF8Block + (v ^ 4) * 16)};
         };
         auto as_operand = [&](const Bytes& b) {
             if constexpr (YT == CNN_F32) return to_halves(b);
             else return b;
         };
-        // The products of a fragment of outputs are at work while the sums of the one before are added.
-        auto multiply = [&](const char* W, const char* X, const float* s) {
-            Operand x[FT];
+        // Asks for block k, or, behind the last one, for that again (nothing comes of it).
+        auto ask = [&](int k, auto slot) {
+            k = min(k, last - 1);
+            wscale[decltype(slot)::value] = ws[k];
+            fw.load(p.w, k, p.I, wbuf(slot));
+            fx.load(p.x, k, p.I, xbuf(slot));
+        };
+        const int key = S::out_key(orow);
+        Operand x[FT];
+        Bytes next;                   // the outputs' next fragment
+        f32x4 d[2][FT];               // a fragment's sums, and those of the one before
+        float s[FT], before[FT];      // a block's scales, and those of the one before
+        auto read_scales = [&](int k, auto slot, float* to) {
+            const int at = k - first;
+            const float* group = sScale[(at >> 2) & 1] + (at & 3) * scale_block + trow * scale_token;
 #pragma unroll
-            for (int j = 0; j < FT; ++j) x[j] = as_operand(read(X, trow + 16 * j, S::token_key(l16)));
-            const int key = S::out_key(orow);
-            Bytes next = read(W, orow, key);
-            f32x4 d[2][FT];
-#pragma unroll
-            for (int i = 0; i <= FO; ++i) {
-                if (i < FO) {
-                    const Operand w = as_operand(next);
-                    if (i + 1 < FO) next = read(W, orow + 4 * (i + 1), key);
-#pragma unroll
-                    for (int j = 0; j < FT; ++j) d[i % 2][j] = block_sums(w, x[j]);
-                }
-                if (i > 0) {
-#pragma unroll
-                    for (int j = 0; j < FT; ++j) {
-                        add_scaled(acc[i - 1][j], d[(i - 1) % 2][j], s[j]);
-                        asm volatile("" : "+v"(acc[i - 1][j]));  // here, and not when the sum is next needed
-                    }
-                }
-                __builtin_amdgcn_sched_barrier(0);
+            for (int j = 0; j < FT; ++j) {
+                const float v = group[16 * j * scale_token] * wscale[decltype(slot)::value];
+                to[j] = k < last ? v : 0.0f;
             }
         };
-        // Block k, which is in (W, X) or on its way there; the next one goes to (NW, NX).
-        auto work = [&](int k, auto full, const char* W, const char* X, char* NW, char* NX) {
-            constexpr bool FULL = decltype(full)::value;  // there is a next one, a whole one
-            block_barrier();
-            float s[FT];
+        auto read_token = [&](auto slot, int j) { x[j] = as_operand(read(xbuf(slot), trow + 16 * j, S::token_key(l16))); };
+        // Block k, whose first fragments are in registers.  The products of a fragment of outputs are at work while the sums
+        // of the one before are added.  Before its last fragment's products the next block is made ready, a later one is
+        // asked for (this one's buffer is free: all waves have read what they need), and the next one's
+        // first fragments are read: those products cover that.  (Three buffers, which leave no more than one workgroup to
+        // a compute unit, were no faster: 256 x 128 tiles 91.6 us against 84.7, 2048 x 9216 x 4096.)
+        auto work = [&](int k, auto slot) {
+            using Here = decltype(slot);
+            using Next = Step<1 - Here::value>;
+            float after[FT];
 #pragma unroll
-            for (int j = 0; j < FT; ++j) s[j] = xnext[j] * wnext;
-            if (FULL || k + 1 < last) {
-                fw.template load<FULL>(p.w, k + 1, p.I, NW);
-                fx.template load<FULL>(p.x, k + 1, p.I, NX);
-                load_scales(k + 1);
+            for (int i = 0; i < FO; ++i) {
+                const Operand w = as_operand(next);
+                if (i + 1 < FO) {
+                    next = read(wbuf(Here{}), orow + 4 * (i + 1), key);
+                } else {
+                    fw.store(wbuf(Next{}));
+                    fx.store(xbuf(Next{}));
+                    block_barrier();
+                    // (scales are read before others are asked for: the compiler would wait for those first, and so for all)
+                    read_scales(k + 1, Next{}, after);
+                    next = read(wbuf(Next{}), orow, key);
+                    __builtin_amdgcn_sched_barrier(0);
+                    ask(k + 2, Here{});
+                    // the other group's places have been read by all waves; what is asked for now is used 3 blocks later
+                    if (((k - first) & 3) == 0 && k + 4 < last) ask_scales(((k - first) >> 2) + 1);
+                }
+#pragma unroll
+                for (int j = 0; j < FT; ++j) {
+                    d[i % 2][j] = block_sums(w, x[j]);
+                    if (i + 1 == FO) read_token(Next{}, j);
+                    const int done = (i + FO - 1) % FO;
+                    add_scaled(acc[done][j], d[(i + 1) % 2][j], i == 0 ? before[j] : s[j]);
+                    asm volatile("" : "+v"(acc[done][j]));  // here, and not when the sum is next needed
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             }
-            multiply(W, X, s);
-            if (FULL || k + 1 < last) {
-                fw.store(NW);
-                fx.store(NX);
-            }
+#pragma unroll
+            for (int j = 0; j < FT; ++j) before[j] = s[j], s[j] = after[j];
         };
+        static_assert(FO % 2 == 0, "a fragment's set of sums is the same in every block");
         if (first < last) {
-            fw.template load<false>(p.w, first, p.I, sW0);
-            fx.template load<false>(p.x, first, p.I, sX0);
-            load_scales(first);
+            ask_scales(0);
+            ask(first, Step<0>{});
             fw.store(sW0);
             fx.store(sX0);
-            int k = first;
-            for (; k + 3 < last; k += 2) {
-                work(k, std::true_type{}, sW0, sX0, sW1, sX1);
-                work(k + 1, std::true_type{}, sW1, sX1, sW0, sX0);
+            ask(first + 1, Step<1>{});
+            block_barrier();
+            next = read(sW0, orow, key);
+            read_scales(first, Step<0>{}, s);
+#pragma unroll
+            for (int j = 0; j < FT; ++j) {
+                read_token(Step<0>{}, j);
+                before[j] = 0.0f;
+                d[1][j] = f32x4{0, 0, 0, 0};
             }
-            for (; k < last; k += 2) {
-                work(k, std::false_type{}, sW0, sX0, sW1, sX1);
-                if (k + 1 < last) work(k + 1, std::false_type{}, sW1, sX1, sW0, sX0);
+            // whole turns: blocks behind the last one have a scale of 0
+#pragma unroll 1
+            for (int k = first; k < last; k += 2) {
+                work(k, Step<0>{});
+                work(k + 1, Step<1>{});
             }
+#pragma unroll
+            for (int j = 0; j < FT; ++j) add_scaled(acc[FO - 1][j], d[1][j], before[j]);
         }
 
         const int64_t o = o0 + wo * FO * 16 + quarter * (FO * 4), count = min((int64_t)p.O - o, (int64_t)FO * 4);
@@ -257,34 +300,88 @@ __global__ void __launch_bounds__(64 * WO * WT, 2) fc_f8_tiles(TileParams tp) {
                 else store_outputs<YT, FO * 4>(p.y, (size_t)n * p.O + o, v, count);
             }
         }
-        __syncthreads();  // the buffers are the next tile's
+        block_barrier();  // nothing is on its way to the buffers, which are the next tile's
     }
 }
 
-template <int WO, int WT, int FO, int FT, bool VEC, int YT, bool SPLIT>
-void start(const TileParams& tp, hipStream_t st) {
+// Adds the parts of a split reduction, in their order, then bias and ReLU: 4 neighbours a work-item.
+template <int YT>
+__global__ void __launch_bounds__(256) fc_f8_join(TileParams tp) {
+    const FcF8& p = tp.fc;
+    const int64_t all = (int64_t)p.N * p.O, step = (int64_t)gridDim.x * 1024;
+    for (int64_t e = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; e < all; e += step) {
+        const int count = (int)min(all - e, (int64_t)4);
+        float v[4] = {0, 0, 0, 0};
+#pragma unroll 4
+        for (int q = 0; q < tp.parts; ++q) {
+            const float* src = tp.partial + (size_t)q * all + e;
+            if (count == 4) {
+                f32x4 u;
+                __builtin_memcpy(&u, src, 16);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] += u[i];
+            } else {
+#pragma unroll
+                for (int i = 0; i < 3; ++i)
+                    if (i < count) v[i] += src[i];
+            }
+        }
+        int o = (int)(e % p.O);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[i] = finish(p, v[i], p.bias && i < count ? p.bias[o] : 0.0f);
+            o = o + 1 == p.O ? 0 : o + 1;
+        }
+        if constexpr (YT == CNN_F32) {
+            store_outputs<YT, 4>(p.y, (size_t)e, v, count);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i < count) store_value(YT, p.y, (size_t)e + i, v[i]);
+        }
+    }
+}
+
+template <int WO, int WT, int FO, int FT, bool VEC, int YT>
+void start(const FcF8& p, const F8Tile& t, float* partial, hipStream_t st) {
     using S = Shape<WO, WT, FO, FT>;
-    const int64_t jobs = (int64_t)tp.tiles * tp.parts;
-    enqueue(fc_f8_tiles<WO, WT, FO, FT, VEC, YT, SPLIT>, dim3((unsigned)std::min<int64_t>(jobs, 1 << 20)), dim3(S::NT), 0, st, tp);
+    const int blocks = f8_blocks(p.I);
+    TileParams tp{p, blocks, ceil_div(p.O, S::TO), 0, t.parts, t.run, (uintptr_t)p.xs % 16 == 0 && blocks % 4 == 0, partial};
+    tp.tiles = tp.out_tiles * ceil_div(p.N, S::TT);
+    const dim3 grid((unsigned)std::min<int64_t>((int64_t)tp.tiles * tp.parts, 1 << 20));
+    if (t.parts == 1) {
+        enqueue(fc_f8_tiles<WO, WT, FO, FT, VEC, YT, false>, grid, dim3(S::NT), 0, st, tp);
+    } else {
+        enqueue(fc_f8_tiles<WO, WT, FO, FT, VEC, YT, true>, grid, dim3(S::NT), 0, st, tp);
+        enqueue(fc_f8_join<YT>, dim3((unsigned)std::min<int64_t>(ceil_div64((int64_t)p.N * p.O, 1024), 1 << 16)), dim3(256), 0, st, tp);
+    }
 }
 
 template <int WO, int WT, int FO, int FT, bool VEC>
 void start_type(const FcF8& p, const F8Tile& t, float* partial, hipStream_t st) {
-    using S = Shape<WO, WT, FO, FT>;
-    const int blocks = f8_blocks(p.I);
-    TileParams tp{p, blocks, ceil_div(p.O, S::TO), 0, 1, blocks, partial};
-    tp.tiles = tp.out_tiles * ceil_div(p.N, S::TT);
-    if (p.y_type == CNN_F32) start<WO, WT, FO, FT, VEC, CNN_F32, false>(tp, st);
-    else if (p.y_type == CNN_BF16) start<WO, WT, FO, FT, VEC, CNN_BF16, false>(tp, st);
-    else start<WO, WT, FO, FT, VEC, CNN_F16, false>(tp, st);
+    if (p.y_type == CNN_F32) {
+        if constexpr (WO * WT == 4) start<WO, WT, FO, FT, VEC, CNN_F32>(p, t, partial, st);
+    } else if (p.y_type == CNN_BF16) {
+        start<WO, WT, FO, FT, VEC, CNN_BF16>(p, t, partial, st);
+    } else {
+        start<WO, WT, FO, FT, VEC, CNN_F16>(p, t, partial, st);
+    }
 }
 
 }  // namespace
 
 void run_f8_tiles(const FcF8& p, const F8Tile& t, bool vec, float* partial, hipStream_t st) {
-    if (t.outs == 256 && vec && p.y_type != CNN_F32) start_type<2, 4, 8, 4, true>(p, t, partial, st);
-    else if (vec) start_type<2, 2, 4, 4, true>(p, t, partial, st);
-    else start_type<2, 2, 4, 4, false>(p, t, partial, st);
+    if (t.tokens == 64) {
+        if (vec) start_type<2, 2, 4, 2, true>(p, t, partial, st);
+        else start_type<2, 2, 4, 2, false>(p, t, partial, st);
+    } else if (t.outs == 128) {
+        if (vec) start_type<2, 2, 4, 4, true>(p, t, partial, st);
+        else start_type<2, 2, 4, 4, false>(p, t, partial, st);
+    } else if (t.tokens == 128) {
+        start_type<4, 2, 4, 4, true>(p, t, partial, st);
+    } else {
+        start_type<2, 4, 8, 4, true>(p, t, partial, st);
+    }
 }
 
 }  // namespace cnn

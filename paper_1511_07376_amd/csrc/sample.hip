@@ -905,9 +905,9 @@ int tile_tokens(int V) { return 512 * (int)ceil_div64(V, 512 * kBins); }
 
 // Rows are split where there are too few for all compute units, and long.
 int chunks_of(int N, int V) {
-    if (N > 128 || V < 16384) return 0;
+    if (N > 128 || V < 40000) return 0;
     const int each = tile_tokens(V);
-    const int64_t most = std::min<int64_t>(1024 / N, V / 4096);
+    const int64_t most = std::min<int64_t>(512 / N, V / 4096);
     return most < 2 ? 0 : (int)ceil_div64(V, ceil_div64(ceil_div64(V, most), each) * each);
 }
 
