@@ -681,12 +681,12 @@ def cnn_f8_quantize(x, block_rows=1, q=None, scale=None, stream=None):
     xp = _on(x, "x", device)
     st = _raw_stream(device.index)
     if q is None:
-        q = torch.empty(x.shape, dtype=_F8, device=device)
+        q = torch.empty_like(x, dtype=_F8)  # of the ways to allocate the quickest: 1.5 us, torch.empty 2.6
         qp = q.data_ptr()
     else:
         qp = _on(q, "q", device, _F8, x.shape)
     if scale is None:
-        scale = torch.empty(scales, dtype=torch.float32, device=device)
+        scale = x.new_empty(scales, dtype=torch.float32)
         sp = scale.data_ptr()
     else:
         sp = _on(scale, "scale", device, torch.float32, scales)
@@ -710,7 +710,7 @@ def cnn_f8_dequantize(q, scale, block_rows=1, dtype=None, y=None, stream=None):
     sp = _on(scale, "scale", device, torch.float32, scales)
     st = _raw_stream(device.index)
     if y is None:
-        y = torch.empty(q.shape, dtype=dtype or torch.float32, device=device)
+        y = torch.empty_like(q, dtype=dtype or torch.float32)
         yp = y.data_ptr()
     else:
         yp = _on(y, "y", device, dtype, q.shape)
@@ -749,19 +749,19 @@ def cnn_rms_norm_fwd(x, weight=None, residual=None, eps=1e-6, f8=False, sum=None
             raise ValueError("rms_norm: sum goes with a residual")
         sump = _on(sum, "sum", device, x.dtype, shape)
     elif residual is not None:
-        sum = torch.empty(shape, dtype=x.dtype, device=device)
+        sum = torch.empty_like(x)
         sump = sum.data_ptr()
     else:
         sump = None
     if y is None:
-        y = torch.empty(shape, dtype=_F8 if f8 else x.dtype, device=device)
+        y = torch.empty_like(x, dtype=_F8) if f8 else torch.empty_like(x)
         yp = y.data_ptr()
     else:
         yp = _on(y, "y", device, _F8 if f8 else x.dtype, shape)
     if f8:
         scales = shape[:-1] + ((cols + 127) // 128,)
         if y_scale is None:
-            y_scale = torch.empty(scales, dtype=torch.float32, device=device)
+            y_scale = x.new_empty(scales, dtype=torch.float32)
             yscalep = y_scale.data_ptr()
         else:
             yscalep = _on(y_scale, "y_scale", device, torch.float32, scales)
@@ -797,12 +797,12 @@ def cnn_fc_f8_fwd(x, x_scale, w, w_scale, bias=None, fuse_relu=False, y_dtype=No
     bp = _on(bias, "bias", device, torch.float32, (O,))
     st = _raw_stream(device.index)
     if y is None:
-        y = torch.empty((N, O), dtype=y_dtype or torch.float32, device=device)
+        y = x.new_empty((N, O), dtype=y_dtype or torch.float32)
         yp = y.data_ptr()
     else:
         yp = _on(y, "y", device, y_dtype, (N, O))
     need = _fc_f8_workspace(N, I, O)
-    work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    work = x.new_empty(need, dtype=torch.uint8) if need else None
     _ok(lib.cnn_fc_f8_fwd(xp, xs, N, I, wp, ws, bp, O, 1 if fuse_relu else 0, yp, _WIDE.get(y.dtype, -1),
                           work.data_ptr() if need else None, need, st))
     return y
@@ -834,10 +834,10 @@ def cnn_sample_fwd(logits, u, temperature=None, top_k=None, top_p=None, min_p=No
     pp = _on(top_p, "top_p", device, torch.float32, row)
     mp = _on(min_p, "min_p", device, torch.float32, row)
     st = _raw_stream(device.index)
-    parts = torch.empty((2, N), dtype=torch.int32, device=device)
+    parts = logits.new_empty((2, N), dtype=torch.int32)
     base = parts.data_ptr()
     need = _sample_workspace(code, N, V)
-    work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    work = logits.new_empty(need, dtype=torch.uint8) if need else None
     _ok(lib.cnn_sample_fwd(lp, code, N, V, up, tp, kp, pp, mp, base, base + 4 * N,
                            work.data_ptr() if need else None, need, st))
     token, prob = parts.unbind(0)

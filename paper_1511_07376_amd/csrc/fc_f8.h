@@ -14,8 +14,8 @@
 //    what rounding it to bfloat16 takes, a fifteenth of fp16's.
 //  - in 16 bits: every 8-bit float is an fp16 number, the products are exact and are
 //    added in fp32, at half the rate and with conversions.
-// Results in fp32 take the second way, and so do those of few tokens, which are bound by
-// reading the weights; 16-bit results of more tokens the first.
+// Results in fp32 take the second way, and so do all that are computed by rows (few tokens, or little
+// work), which are bound by reading; 16-bit results on tiles the first.
 #pragma once
 
 #include "f8.h"
@@ -51,6 +51,25 @@ __device__ inline u32x4 load_bytes_edge(const uint8_t* p, int64_t count, int64_t
 struct Bytes {
     u32x4 v[2];
 };
+// Loads from addresses that are no multiples of 4 take twice as long (300 x 3001 x 1500: 62 us against 28 at 3008).  Such rows
+// are loaded by whole words, the first of which can hold bytes from before and the last from behind (the
+// same word, so the same page, as one that is wanted), and shifted.
+__device__ inline unsigned word_shift(const uint8_t* p) { return (unsigned)(uintptr_t)p & 3; }
+__device__ inline u32x4 shifted(u32x4 v, unsigned last, unsigned shift) {
+    return u32x4{__builtin_amdgcn_alignbyte(v[1], v[0], shift), __builtin_amdgcn_alignbyte(v[2], v[1], shift),
+                 __builtin_amdgcn_alignbyte(v[3], v[2], shift), __builtin_amdgcn_alignbyte(last, v[3], shift)};
+}
+// 32 bytes from p on.
+template <bool ODD>
+__device__ inline Bytes load32(const uint8_t* p) {
+    if constexpr (!ODD) return Bytes{load16(p), load16(p + 16)};
+    const unsigned shift = word_shift(p);
+    const uint8_t* words = p - shift;
+    const u32x4 a = load16(words), b = load16(words + 16);
+    unsigned last;
+    __builtin_memcpy(&last, words + (shift ? 32 : 28), 4);
+    return Bytes{shifted(a, b[0], shift), shifted(b, last, shift)};
+}
 struct Halves {
     f16x8 v[4];
 };
@@ -96,6 +115,7 @@ __device__ inline void store_value(int type, void* y, size_t at, float v) {
 struct F8Tile {
     int outs, tokens, parts, run;
 };
+// vec: rows of whole blocks at 16-byte addresses.
 void run_f8_tiles(const FcF8& p, const F8Tile& tile, bool vec, float* partial, hipStream_t st);
 
 }  // namespace cnn

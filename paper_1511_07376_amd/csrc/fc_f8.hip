@@ -14,7 +14,7 @@ constexpr int kMostWaves = 16;
 
 // 16 FO outputs of 16 NT tokens a workgroup, whose waves share the blocks: the weights are read
 // once for all of them, straight to registers.
-template <int NT, int FO>
+template <int NT, int FO, bool ODD>
 __global__ void __launch_bounds__(64 * kMostWaves) fc_f8_rows(FcF8 p, int blocks, int out_groups, int jobs) {
     __shared__ float part[kMostWaves][16 * NT][16 * FO + 1];
     const int waves = blockDim.x >> 6, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, l16 = lane & 15, quarter = lane >> 4;
@@ -57,7 +57,7 @@ __global__ void __launch_bounds__(64 * kMostWaves) fc_f8_rows(FcF8 p, int blocks
         };
         for (int k = first; k < whole; ++k) {
             const int64_t at = (int64_t)k * kF8Block;
-            add(k, [&](const uint8_t* base, unsigned row) { return Bytes{load16(base + at + row), load16(base + at + row + 16)}; });
+            add(k, [&](const uint8_t* base, unsigned row) { return load32<ODD>(base + at + row); });
         }
         if (whole < last) {
             const int64_t at = (int64_t)whole * kF8Block, in = at + quarter * 32, left = p.I - in;
@@ -84,26 +84,29 @@ __global__ void __launch_bounds__(64 * kMostWaves) fc_f8_rows(FcF8 p, int blocks
 }
 
 template <int NT, int FO>
-void run_rows(const FcF8& p, hipStream_t st) {
+void run_rows(const FcF8& p, bool odd, hipStream_t st) {
     const int blocks = f8_blocks(p.I), groups = ceil_div(p.O, 16 * FO);
     const int64_t jobs = (int64_t)groups * ceil_div(p.N, 16 * NT);
     const int waves = std::max(1, std::min(kMostWaves, blocks / 2));
-    enqueue(fc_f8_rows<NT, FO>, dim3((unsigned)std::min<int64_t>(jobs, 1 << 20)), dim3(64 * waves), 0, st, p, blocks, groups, (int)jobs);
+    const dim3 grid((unsigned)std::min<int64_t>(jobs, 1 << 20)), block(64 * waves);
+    if (odd) enqueue(fc_f8_rows<NT, FO, true>, grid, block, 0, st, p, blocks, groups, (int)jobs);
+    else enqueue(fc_f8_rows<NT, FO, false>, grid, block, 0, st, p, blocks, groups, (int)jobs);
 }
 
-// Few tokens: the weights are streamed.  4096 x 4096 weights, 16 tokens: 8.0 us against 10.8 on tiles, 32 tokens 10.7 against 11.6;
-// 9216 x 8192, 16 tokens 18.1 against 19.3, 32 tokens 26 against 20.9: there every workgroup reads all inputs again.
-bool few_rows(int N, int I, int O) { return N <= 16 || (N <= 32 && (int64_t)I * O <= 24 << 20); }
-
-// A tile's time is its blocks' times, which grow with the workgroups that share a compute unit, and some 3.5 us around
-// them; parts take a second kernel, and their way through memory.  As measured between 64 x 1024 and 4096 x
-// 8192 results of 2048 to 9216 values.
+// What a call costs one way or another, in us, as measured between 1 x 512 x 8192 and 4096 x 4096 x 8192.
+//
+// Rows: every workgroup reads its outputs' weights and its tokens' inputs, at some 6 TB/s from the L2s and behind them, and
+// half of that from odd addresses.
+//
+// Tiles: their blocks' times, which grow with the workgroups that share a compute unit, or the weights' time from memory, and
+// some 3.5 us around them; parts take a second kernel, and their way through memory.
 struct TileCost {
     int outs, tokens, slots;  // slots: workgroups that a compute unit holds
     float half, one, two;     // us a block with 128 workgroups or fewer, with 256, with 512
 };
 constexpr TileCost kCosts16[] = {{128, 64, 3, 0.40f, 0.62f, 0.76f}, {128, 128, 2, 0.70f, 0.85f, 1.30f}, {256, 128, 1, 0.95f, 1.15f, 0}, {256, 256, 1, 1.57f, 2.1f, 0}};
 constexpr TileCost kCosts32[] = {{128, 64, 3, 0.77f, 0.86f, 1.32f}, {128, 128, 2, 1.27f, 1.56f, 2.23f}};
+constexpr TileCost kCostsStaged[] = {{128, 64, 3, 1.2f, 1.4f, 1.8f}, {128, 128, 2, 1.5f, 1.75f, 2.2f}};  // through registers
 constexpr int kMostParts = 16;
 constexpr size_t kMostWorkspace = 64 << 20;
 
@@ -112,15 +115,30 @@ float block_time(const TileCost& c, int64_t jobs) {
     return at <= 0.5f ? c.half : at <= 1 ? c.half + (c.one - c.half) * (2 * at - 1) : c.one + (c.two - c.one) * (at - 1);
 }
 
+// Rows of 16 `tokens` and `outs` of 16, or a tile.
+struct Way {
+    bool rows;
+    int tokens, outs;
+    F8Tile tile;
+};
 // By sizes and the type alone (the workspace is sized before the call's pointers are known).
-F8Tile choose_tile(int N, int I, int O, bool wide32) {
+Way choose(int N, int I, int O, bool wide32) {
     const int blocks = f8_blocks(I);
-    F8Tile best{128, 64, 1, blocks};
+    Way best{};
     float least = 3e38f;
-    const TileCost* costs = wide32 ? kCosts32 : kCosts16;
-    for (int c = 0; c < (wide32 ? 2 : 4); ++c) {
+    constexpr int kRows[][2] = {{1, 1}, {1, 2}, {2, 1}, {4, 1}};
+    for (const auto& r : kRows) {
+        const int64_t jobs = (int64_t)ceil_div(O, 16 * r[1]) * ceil_div(N, 16 * r[0]);
+        // 256 of them at once take one's time, and 32 outputs a workgroup are slower where there are fewer
+        const float bytes = (float)std::max<int64_t>(jobs, r[1] == 2 ? 256 : 128) * (float)(16 * r[1] + std::min(N, 16 * r[0])) * (float)I;
+        const float time = 3.0f + bytes / 6.3e6f * (I % 4 ? 1.3f : 1.0f);
+        if (time < least) least = time, best = Way{true, r[0], r[1], {}};
+    }
+    const bool staged = I % kF8Block != 0;
+    const TileCost* costs = staged ? kCostsStaged : wide32 ? kCosts32 : kCosts16;
+    const float read = (float)O * (float)I / 5e6f;
+    for (int c = 0; c < (staged || wide32 ? 2 : 4); ++c) {
         const TileCost& cost = costs[c];
-        if (cost.outs == 256 && I % kF8Block != 0) continue;
         const int64_t tiles = (int64_t)ceil_div(O, cost.outs) * ceil_div(N, cost.tokens), round = 256 * cost.slots;
         for (int parts = 1; parts <= kMostParts; ++parts) {
             const int run = parts == 1 ? blocks : ceil_div(ceil_div(blocks, parts), 4) * 4;
@@ -128,8 +146,8 @@ F8Tile choose_tile(int N, int I, int O, bool wide32) {
             if (parts > 1 && (ceil_div(blocks, run) != parts || bytes > (float)kMostWorkspace || tiles * parts > round)) continue;
             const int64_t jobs = tiles * parts, full = jobs / round, rest = jobs % round;
             const float each = (float)full * block_time(cost, round) + (rest ? block_time(cost, rest) : 0.0f);
-            const float time = (float)run * each + (parts > 1 ? 2.5f + 0.75e-6f * bytes : 0.0f);
-            if (time < least) least = time, best = F8Tile{cost.outs, cost.tokens, parts, run};
+            const float time = 3.5f + std::max((float)run * each, read) + (parts > 1 ? 2.5f + 0.75e-6f * bytes : 0.0f);
+            if (time < least) least = time, best = Way{false, 0, 0, F8Tile{cost.outs, cost.tokens, parts, run}};
         }
     }
     return best;
@@ -139,28 +157,27 @@ F8Tile choose_tile(int N, int I, int O, bool wide32) {
 
 // The type decides too: the larger of the two needs.
 size_t fc_f8_workspace(int N, int I, int O) {
-    if (few_rows(N, I, O)) return 0;
     size_t need = 0;
     for (const bool wide32 : {false, true}) {
-        const F8Tile t = choose_tile(N, I, O, wide32);
-        if (t.parts > 1) need = std::max(need, (size_t)t.parts * N * O * sizeof(float));
+        const Way way = choose(N, I, O, wide32);
+        if (!way.rows && way.tile.parts > 1) need = std::max(need, (size_t)way.tile.parts * N * O * sizeof(float));
     }
     return need;
 }
 
 int launch_fc_f8(const FcF8& p, float* ws, hipStream_t st) {
     if (p.N == 0) return CNN_OK;
-    if (few_rows(p.N, p.I, p.O)) {
-        // 32 outputs a workgroup read the inputs half as often, where there are enough of them: 9216 x 8192, 1 token 16.8 to
-        // 14.4 us, 16 tokens 27 to 18; 4096 x 4096 5.9 and 8.0 against 7.5 and 9.7
-        if (p.N > 16) run_rows<2, 1>(p, st);
-        else if (p.O > 6144) run_rows<1, 2>(p, st);
-        else run_rows<1, 1>(p, st);
+    Way way = choose(p.N, p.I, p.O, p.y_type == CNN_F32);
+    auto whole = [&](int to) { return (uintptr_t)p.x % to == 0 && (uintptr_t)p.w % to == 0; };
+    const bool odd = !whole(4) || p.I % 4 != 0;
+    if (!way.rows) {
+        const bool vec = whole(16) && p.I % kF8Block == 0;
+        if (!vec && way.tile.outs == 256) way.tile.outs = way.tile.tokens = 128;  // whole blocks at addresses that are not
+        run_f8_tiles(p, way.tile, vec, ws, st);
+    } else if (way.tokens == 1) {
+        way.outs == 1 ? run_rows<1, 1>(p, odd, st) : run_rows<1, 2>(p, odd, st);
     } else {
-        const bool vec = (uintptr_t)p.x % 16 == 0 && (uintptr_t)p.w % 16 == 0 && p.I % kF8Block == 0;
-        F8Tile t = choose_tile(p.N, p.I, p.O, p.y_type == CNN_F32);
-        if (!vec && t.outs == 256) t.outs = t.tokens = 128;  // rows of whole vectors at an address that is none
-        run_f8_tiles(p, t, vec, ws, st);
+        way.tokens == 2 ? run_rows<2, 1>(p, odd, st) : run_rows<4, 1>(p, odd, st);
     }
     return check_launch("fc_f8");
 }

@@ -45,7 +45,8 @@ __device__ inline void copy4(const void* src, char* dst) {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, (__attribute__((address_space(3))) void*)dst, 4, 0, 0);
 }
 
-// One operand's vectors of a block, of this work-item: ROWS rows, NT work-items.  Places are
+// One operand's vectors of a block, of this work-item: ROWS rows, NT work-items.  VEC: rows of whole blocks at
+// 16-byte addresses, copied to LDS by the loads; others go through registers.  Places are
 // 32-bit offsets (a tensor has fewer than 2^31 bytes) from a base that moves on with the blocks.
 template <int ROWS, int NT, bool VEC, typename KEY>
 struct Fetch {
@@ -71,6 +72,7 @@ struct Fetch {
         for (int i = 0; i < N; ++i) {
             const int in = vector_of(i) * 16;
             if constexpr (VEC) copy16(base + at[i], lds + (i * NT + wave0) * 16);
+            // (at odd addresses too: loaded by words and shifted, as for few rows, 1500 x 4001 x 4001 was 75 us against 67)
             else if (left >= kF8Block) reg[i] = load16(base + at[i]);
             else reg[i] = load_bytes_edge(base + at[i], left - in, (int64_t)k * kF8Block + in);
         }
