@@ -903,18 +903,21 @@ int weight_bits(int V) {
 // A tile: as many tokens as a wave loads at a time, or more where that were more than kBins tiles.
 int tile_tokens(int V) { return 512 * (int)ceil_div64(V, 512 * kBins); }
 
-// Rows are split where there are too few for all compute units, and long.
-int chunks_of(int N, int V) {
-    if (N > 128 || V < 40000) return 0;
+// Rows are split where there are too few for all compute units, and long: six launches instead of one, or three where
+// there is no top-k or top-p.  Both ways took the same time, in fp32 with top-k and top-p, at
+// 1 x 32768 (29 us) and 64 x 50021 (54), without at 1 x 16384 (12.5) and 128 x 32768 (20.5); at 1 x 131072
+// it is 71 and 30 us, and 47 and 13.
+int chunks_of(int N, int V, bool cuts) {
+    if (N > 128 || V < (cuts ? 36000 + 300 * N : 16000 + 150 * N)) return 0;
     const int each = tile_tokens(V);
     const int64_t most = std::min<int64_t>(512 / N, V / 4096);
     return most < 2 ? 0 : (int)ceil_div64(V, ceil_div64(ceil_div64(V, most), each) * each);
 }
 
 // The workspace of a call that splits rows (base: or NULL, to know its size).
-size_t lay_out(Split& sp, int N, int V, char* base) {
+size_t lay_out(Split& sp, int N, int V, bool cuts, char* base) {
     const int each = tile_tokens(V);
-    sp.chunks = chunks_of(N, V);
+    sp.chunks = chunks_of(N, V, cuts);
     if (sp.chunks == 0) return 0;
     sp.chunk = (int)(ceil_div64(ceil_div64(V, sp.chunks), each) * each);
     size_t at = 0;
@@ -932,12 +935,20 @@ size_t lay_out(Split& sp, int N, int V, char* base) {
     return at;
 }
 
+template <typename T, int NT>
+void run_rows(const Args& a, const dim3& rows, hipStream_t st) {
+    enqueue(sample_rows<T, WHOLE, NT>, rows, dim3(NT), 0, st, a);
+}
 template <typename T>
-void run(const Args& a, hipStream_t st) {
+void run(const Args& a, bool cuts, hipStream_t st) {
     const dim3 rows((unsigned)std::min(a.p.N, 1 << 20));
     if (a.split.chunks == 0) {
-        if (a.p.V <= 8192) enqueue(sample_rows<T, WHOLE, 256>, rows, dim3(256), 0, st, a);
-        else enqueue(sample_rows<T, WHOLE, 512>, rows, dim3(512), 0, st, a);
+        // A workgroup's barriers cost more the larger it is, its passes less: 128 rows of 1000, 4096, 8000 with
+        // cuts took 17.6, 22.8, 30.5 us with 256 work-items and 16.1, 19.3, 24.0 with 512, one of 1000 11.7 and
+        // 12.1; 128 of 32768 46.9 with 512 and 42.0 with 1024, without cuts 20.5 and 20.9.
+        if (a.p.V <= 1024) run_rows<T, 256>(a, rows, st);
+        else if (a.p.V <= 20000 || !cuts) run_rows<T, 512>(a, rows, st);
+        else run_rows<T, 1024>(a, rows, st);
         return;
     }
     const dim3 parts((unsigned)(a.p.N * a.split.chunks)), threads(kChunkThreads);
@@ -956,17 +967,18 @@ void run(const Args& a, hipStream_t st) {
 
 size_t sample_workspace(int type, int N, int V) {
     Split sp{};
-    return lay_out(sp, N, V, nullptr);
+    return std::max(lay_out(sp, N, V, false, nullptr), lay_out(sp, N, V, true, nullptr));
 }
 
 int launch_sample(const Sample& p, void* ws, hipStream_t st) {
     if (p.N == 0) return CNN_OK;
     Args a{p, weight_bits(p.V), tile_tokens(p.V), {}};
-    lay_out(a.split, p.N, p.V, (char*)ws);
-    if (!p.top_k && !p.top_p) a.split.pending = nullptr;
-    if (p.type == CNN_F32) run<float>(a, st);
-    else if (p.type == CNN_BF16) run<bf16_t>(a, st);
-    else run<f16_t>(a, st);
+    const bool cuts = p.top_k || p.top_p;
+    lay_out(a.split, p.N, p.V, cuts, (char*)ws);
+    if (!cuts) a.split.pending = nullptr;
+    if (p.type == CNN_F32) run<float>(a, cuts, st);
+    else if (p.type == CNN_BF16) run<bf16_t>(a, cuts, st);
+    else run<f16_t>(a, cuts, st);
     return check_launch("sample");
 }
 
