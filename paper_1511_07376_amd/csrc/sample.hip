@@ -31,6 +31,7 @@ typedef unsigned long long u64;
 constexpr int kBins = 2048;
 constexpr float kBinsPerOctave = 38.0f;  // the last bin begins at 2^-53.8, which is no whole number's weight
 constexpr int kDigit = 8, kDigits = 1 << kDigit;
+constexpr int kFew = 64;                // tokens that a wave finishes a search among
 constexpr int kList = 2048;             // tokens that are worked on in LDS
 constexpr u64 kAll = ~0ull;
 
@@ -174,8 +175,10 @@ struct Shared {
     // digits of codes; all 0 between searches
     u64 digit_sum[kDigits];
     unsigned digit_count[kDigits];
+    u64 few_code[kFew], few_weight[kFew];
     u64 wave_sum[kWaves];
     unsigned wave_count[kWaves];
+    int few;
     u64 found_sum, found_code;
     unsigned found_count, found_many;
     int found;
@@ -354,7 +357,8 @@ struct Items {
 // The first code, of the items' in rising order, at which the border is reached: there is one.  Before
 // all of the items: (none, sum).  `weight`: the found one's.
 //
-// Digit by digit from the top one that differs; one wave looks through a digit's 256 sums.
+// Digit by digit from the top one that differs, one wave looking through a digit's 256 sums, until a few items
+// are left: those before each are added up.
 template <int NT, typename T>
 CNN_INLINE u64 find_code(Shared<NT>& s, const Items<T>& items, const Border& b, u64 none, u64 sum, u64& weight) {
     u64 low = kAll, high = 0;
@@ -397,15 +401,31 @@ CNN_INLINE u64 find_code(Shared<NT>& s, const Items<T>& items, const Border& b, 
         count = s.found_count;
         sum = s.found_sum;
         prefix |= (u64)max(bin, 0) << shift;
-        if (shift == 0 || many == 1 || bin < 0) break;
+        if (shift == 0 || many <= kFew || bin < 0) break;
         above = shift;
         shift = max(shift - kDigit, 0);
         __syncthreads();
     }
-    // the one item in the last bin
+    // the items in the last bin
+    if (threadIdx.x == 0) s.few = 0;
+    __syncthreads();
     items.go([&](u64 code, u64 w) {
-        if ((code - low) >> shift == prefix >> shift) s.found_code = code, s.found_sum = w;
+        if ((code - low) >> shift != prefix >> shift) return;
+        const int i = atomicAdd(&s.few, 1);
+        if (i < kFew) s.few_code[i] = code, s.few_weight[i] = w;
     });
+    __syncthreads();
+    const int few = min(s.few, kFew);
+    if ((int)threadIdx.x < few) {
+        const u64 code = s.few_code[threadIdx.x], w = s.few_weight[threadIdx.x];
+#pragma unroll 4
+        for (int i = 0; i < few; ++i) {
+            const bool before = s.few_code[i] < code;
+            count += before ? 1 : 0;
+            sum += before ? s.few_weight[i] : 0;
+        }
+        if (!(count > none && b.reached(count, sum)) && b.reached(count + 1, sum + w)) s.found_code = code, s.found_sum = w;
+    }
     __syncthreads();
     const u64 code = s.found_code;
     weight = s.found_sum;
