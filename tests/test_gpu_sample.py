@@ -222,3 +222,18 @@ def test_sample_refuses_and_empty(gpu):
     ]:
         with pytest.raises(error):
             call()
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("v", [20001, 45000, 70001])
+def test_sample_however_rows_are_shared_out(gpu, v, dtype):
+    """One row, few or many: its work goes to one workgroup or to several, its token and probability are the same."""
+    g = gen(v)
+    n = 140
+    x, u, kw = logits(n, v, g, dtype), rand(n, g), parameters(n, v, g, "tkpm")
+    for keys in ((), ("temperature", "min_p"), ("top_p",), tuple(kw)):
+        some = {k: kw[k] for k in keys}
+        token, prob = gpu.cnn_sample_fwd(x, u, **some)
+        for rows in (slice(0, 1), slice(3, 60)):
+            part = gpu.cnn_sample_fwd(x[rows], u[rows], **{k: t[rows] for k, t in some.items()})
+            assert torch.equal(part[0], token[rows]) and torch.equal(part[1], prob[rows])

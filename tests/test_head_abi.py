@@ -171,3 +171,24 @@ def test_reference_sample():
     assert int(ref.sample(torch.full((1, 3), -math.inf), one * 0.5)[0]) == -1
     x = torch.tensor([[1.0, math.inf, 2.0, math.inf]])
     assert int(ref.sample(x, 0.6 * one)[0]) == 3
+
+
+# ---------------------------------------------------------------- workspaces
+@pytest.mark.parametrize("n,i,o", [(130, 8192, 700), (13, 15616, 130), (768, 19968, 3018)])
+def test_fc_workspace(n, i, o):
+    need = L.cnn_fc_f8_workspace_bytes(n, i, o)
+    assert need >= 2 * 4 * n * o and need % (4 * n * o) == 0
+    for kw, status in [(dict(work=0, n=need), -4), (dict(work=FAKE, n=need - 1), -4), (dict(work=FAKE + 8, n=need), UNS)]:
+        assert _fc(N=n, I=i, O=o, **kw) == status
+        assert cnn.cnn_last_error().startswith("fc_f8: workspace")
+
+
+@pytest.mark.parametrize("n,v", [(1, 40000), (64, 131072), (128, 200000), (1, 2 ** 31 - 1)])
+def test_sample_workspace(n, v):
+    for t in (F32, BF16):
+        need = L.cnn_sample_workspace_bytes(t, n, v)
+        assert 0 < need <= n * 80000
+        # what a call without cuts needs is what any call needs
+        assert _sample(t=t, N=n, V=v, work=FAKE, n=need - 1) == -4
+        assert cnn.cnn_last_error().startswith("sample: workspace")
+        assert _sample(t=t, N=n, V=v, k=FAKE, work=0, n=need) == -4
