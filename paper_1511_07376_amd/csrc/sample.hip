@@ -976,7 +976,7 @@ void run(const Args& a, bool cuts, hipStream_t st) {
     if (a.split.pending) {
         enqueue(sample_bins<T>, parts, threads, 0, st, a);
         enqueue(sample_gather<T>, parts, threads, 0, st, a);
-        enqueue(sample_rows<T, CUTS, 256>, rows, dim3(256), 0, st, a);
+        enqueue(sample_rows<T, CUTS, 512>, rows, dim3(512), 0, st, a);
     }
     const int groups = ceil_div(ceil_div(a.p.V, a.each), kTileThreads / 64);
     enqueue(sample_tiles<T>, dim3((unsigned)(a.p.N * groups)), dim3(kTileThreads), 0, st, a, groups);
