@@ -351,15 +351,19 @@ int cnn_rms_norm_fwd(const void* x, const void* residual, int type, int rows, in
  *   w [O][I], w_scale [ceil(O/128)][ceil(I/128)]       bias fp32 [O] or NULL
  *   y [N][O], fp32, bf16 or fp16
  * Sums are fp32, the product of two scales is rounded to fp32 (and has to be in
- * its range), the result is rounded once.  fuse_relu = 1 applies y = y > 0 ? y : +0
- * (so NaN becomes 0). */
+ * its range), the result is rounded once.  With a 16-bit y, for all but few
+ * tokens, a block's sum is that of the matrix cores' 8-bit instruction, which
+ * adds products 8 by 8 to 2^-13 of the largest of the 8: some 1.5e-5 of a
+ * result of random values, where y's rounding is 2^-9 (bf16) or 2^-12 (fp16) on
+ * average.  With an fp32 y products are exact and their sums fp32.
+ * fuse_relu = 1 applies y = y > 0 ? y : +0 (so NaN becomes 0). */
 int cnn_fc_f8_fwd(const uint8_t* x, const float* x_scale, int N, int I,
                   const uint8_t* w, const float* w_scale, const float* bias, int O,
                   int fuse_relu, void* y, int y_type, void* ws, size_t ws_bytes,
                   cnn_stream_t stream);
 
-/* Device workspace of cnn_fc_f8_fwd (16-byte aligned, 64 MiB at most), as
- * cnn_fc_mx4_workspace_bytes. */
+/* Device workspace of cnn_fc_f8_fwd (16-byte aligned, 64 MiB at most; 0 if it
+ * needs none, and on error).  Calls that overlap need workspaces of their own. */
 size_t cnn_fc_f8_workspace_bytes(int N, int I, int O);
 
 /* A token for each row of logits, from a random number of the caller's.
@@ -388,8 +392,8 @@ int cnn_sample_fwd(const void* logits, int type, int N, int V, const float* u,
                    const float* min_p, int32_t* token, float* prob, void* ws,
                    size_t ws_bytes, cnn_stream_t stream);
 
-/* Device workspace of cnn_sample_fwd (8-byte aligned; 0 for many rows or few
- * logits, and on error).  Calls that overlap need workspaces of their own. */
+/* Device workspace of cnn_sample_fwd (8-byte aligned, some 50 KiB a row; 0 for
+ * many rows or few logits, and on error).  Calls that overlap need workspaces of their own. */
 size_t cnn_sample_workspace_bytes(int type, int N, int V);
 
 /* ---------------------------------------------------------------- networks

@@ -7,7 +7,9 @@
 // infinity and NaN above all of them: such a block gets NaN for its scale.
 //
 // Both directions move bytes and little else (HBM bound).  A work-item takes 8
-// values, so that 16 lanes are a block of a row.
+// values, so that 16 lanes are a block of a row, whose maximum four moves between lanes find.  4096 x 9216
+// fp32: rows 34 us (5.6 TB/s, above a copy's 5.05, as it mostly reads), squares 37 us (5.1), back 37 us
+// (5.1); bf16 23, 30 and 22 us; 64 x 4096 2.7 us, the least of a kernel.
 #include "f8.h"
 
 #include <algorithm>
@@ -38,7 +40,8 @@ f8_quantize_rows(const T* x, uint8_t* q, float* scale, int64_t items, int cols, 
     }
 }
 
-// A workgroup takes 128 rows of 128 values: 16 rows at a time, 8 times, held in registers.
+// A workgroup takes 128 rows of 128 values: 16 rows at a time, 8 times, held in registers.  (Weights are laid out
+// once: 16384 x 1013 bf16, whose rows begin at any element, takes 22 us against 12.5 by rows.)
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
 f8_quantize_squares(const T* x, uint8_t* q, float* scale, int rows, int cols, int blocks, int64_t squares) {

@@ -9,8 +9,10 @@
 // bits by the block as f8_quantize does from these fp32 values.
 //
 // Bound by HBM: every tensor is read or written once, a row held in registers
-// between the sum and the result.  A work-item takes vectors of 8 values, so
-// that 16 lanes hold a block of 128.
+// between the sum and the result (up to 16384 values).  A work-item takes vectors of 8 values, so
+// that 16 lanes hold a block of 128.  8192 x 4096 bf16 with residual and sum, to 8 bits: 49 to 51 us,
+// 4.7 TB/s (a copy reaches 5.05); 77 x 1013 fp32 3 us, which is a kernel's least and a chain of load,
+// sum and store.
 #include "f8.h"
 
 #include <algorithm>
@@ -86,18 +88,17 @@ __device__ inline double sum_of_squares(const float* s, double sum) {
     return sum;
 }
 
-// Rows of at most NV vectors a work-item.
+// Rows of at most NV vectors a work-item.  The weights stay in registers from row to row.
 template <typename T, bool F8, int NV>
 __global__ void __launch_bounds__(1024) rms_norm_rows(const T* x, const T* res, const float* w, Output<T, F8> out, int rows, int cols, float eps) {
     __shared__ double part[2][16];
     const int nt = blockDim.x, tid = threadIdx.x, blocks = (int)(((int64_t)cols + kF8Block - 1) / kF8Block);
-    constexpr bool KEEP = NV <= 2;  // the weights in registers from row to row
     int at[NV];
-    float wv[KEEP ? NV : 1][8];
+    float wv[NV][8];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         at[j] = min((tid + j * nt) * 8, cols);
-        if constexpr (KEEP) load_weight8(w, at[j], cols, wv[j]);
+        load_weight8(w, at[j], cols, wv[j]);
     }
     int turn = 0;
     for (int64_t row = blockIdx.x; row < rows; row += gridDim.x, turn ^= 1) {
@@ -109,15 +110,13 @@ __global__ void __launch_bounds__(1024) rms_norm_rows(const T* x, const T* res, 
         for (int j = 0; j < NV; ++j) sq = sum_of_squares(s[j], sq);
         const double r = 1.0 / sqrt(group_sum(sq, part[turn]) / cols + (double)eps);
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            if constexpr (!KEEP) load_weight8(w, at[j], cols, wv[0]);
-            out.put((int)row, at[j], cols, blocks, s[j], wv[KEEP ? j : 0], r);
-        }
+        for (int j = 0; j < NV; ++j) out.put((int)row, at[j], cols, blocks, s[j], wv[j], r);
     }
 }
 
-// Longer rows: read twice.  (Each value is read before it is written, by the same work-item:
-// y and sum may be x or residual.)
+// Longer rows: read twice, the second time mostly from the caches.  1024 x 32768 bf16 to 8 bits: 68 us, 3.5
+// TB/s.  (Four vectors a work-item held in registers spill: 75 us, in fp32 128 against 136.)
+// Each value is read before it is written, by the same work-item: y and sum may be x or residual.
 template <typename T, bool F8>
 __global__ void __launch_bounds__(1024) rms_norm_long(const T* x, const T* res, const float* w, Output<T, F8> out, int rows, int cols, float eps) {
     __shared__ double part[2][16];
@@ -132,7 +131,9 @@ __global__ void __launch_bounds__(1024) rms_norm_long(const T* x, const T* res, 
             sq = sum_of_squares(s, sq);
         }
         const double r = 1.0 / sqrt(group_sum(sq, part[turn]) / cols + (double)eps);
-        for (int64_t c = (int64_t)tid * 8; c < end; c += (int64_t)blockDim.x * 8) {
+        // from the end on, which the caches still hold
+        for (int64_t c = (end - 1) / ((int64_t)blockDim.x * 8) * (blockDim.x * 8) + tid * 8; c >= 0; c -= (int64_t)blockDim.x * 8) {
+            if (c >= end) continue;
             const int from = (int)min(c, (int64_t)cols);
             float s[8], wv[8];
             load_sum8(x, res, (size_t)row * cols, from, cols, s);
@@ -151,9 +152,11 @@ void run(const RmsNorm& p, hipStream_t st) {
         enqueue(kernel, grid, dim3(64 * waves), 0, st, (const T*)p.x, (const T*)p.residual, p.weight, out, p.rows, p.cols, p.eps);
     };
     const int64_t waves = ceil_div64(vectors, 64);
-    if (waves <= 16) go(rms_norm_rows<T, F8, 1>, (int)waves);
+    // One vector a work-item up to 1024 work-items, of fp32 up to 512: 4096 x 8192 took 55 us with one and 58 with two in
+    // bf16, 109 and 98 in fp32; 8192 x 4096 51 and 55, 97 and 101.  2048 x 16384 with two and read twice: 62 and 68
+    // in bf16, 115 and 125 in fp32.
+    if (waves <= (sizeof(T) == 4 ? 8 : 16)) go(rms_norm_rows<T, F8, 1>, (int)waves);
     else if (waves <= 32) go(rms_norm_rows<T, F8, 2>, (int)ceil_div64(waves, 2));
-    else if (waves <= 64) go(rms_norm_rows<T, F8, 4>, (int)ceil_div64(waves, 4));
     else go(rms_norm_long<T, F8>, 16);
 }
 

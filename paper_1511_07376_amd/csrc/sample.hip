@@ -18,6 +18,12 @@
 // One workgroup does a row, or, where there are few long rows, several do what passes over all
 // of it: the largest logit, the first histogram, the list, the tiles' sums.
 //
+// Not bound by memory.  256 rows of 50021 fp16, a temperature alone: 29 us, 0.9 TB/s, in which some 50 instructions a
+// logit are issued, half of them the 64-bit exponential (loading further ahead changed nothing).  64 rows of
+// 131072 bf16 with all the rules: 70 us, the six kernels taking 6 (largest), 15 (bins), 12 (list), 13
+// (cuts), 9 (tiles), 8 (draw), of which each one's start and end is about 3.  7 rows of 1000: 12 us, a chain of
+// barriers.
+//
 #include "f8.h"
 
 #include <algorithm>
@@ -524,7 +530,7 @@ CNN_INLINE u64 share_of(float u, u64 sum) {
     return min(t, sum - 1);
 }
 
-// As find_code, among a list's n <= blockDim.x codes.
+// As find_code, among a list's n <= blockDim.x codes, which are sorted.
 template <int NT>
 CNN_INLINE u64 find_sorted(Shared<NT>& s, List& list, const Row& r, int n, const Border& b, u64 count, u64 sum) {
     const u64 code = sorted(list, n);
