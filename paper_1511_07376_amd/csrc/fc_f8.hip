@@ -106,7 +106,7 @@ struct TileCost {
     int outs, tokens, slots;  // slots: workgroups that a compute unit holds
     float half, one, two;     // us a block with 128 workgroups or fewer, with 256, with 512
 };
-constexpr TileCost kCosts16[] = {{128, 64, 3, 0.40f, 0.62f, 0.76f}, {128, 128, 2, 0.70f, 0.85f, 1.30f}, {256, 128, 1, 0.95f, 1.15f, 0}, {256, 256, 1, 1.57f, 2.1f, 0}};
+constexpr TileCost kCosts16[] = {{128, 64, 2, 0.37f, 0.47f, 0.75f}, {128, 128, 2, 0.70f, 0.85f, 1.30f}, {256, 128, 1, 0.95f, 1.15f, 0}, {256, 256, 1, 1.57f, 2.1f, 0}};
 constexpr TileCost kCosts32[] = {{128, 64, 3, 0.77f, 0.86f, 1.32f}, {128, 128, 2, 1.27f, 1.56f, 2.23f}};
 constexpr TileCost kCostsStaged[] = {{128, 64, 3, 1.2f, 1.4f, 1.8f}, {128, 128, 2, 1.5f, 1.75f, 2.2f}};  // through registers
 constexpr int kMostParts = 16;
@@ -114,7 +114,8 @@ constexpr size_t kMostWorkspace = 64 << 20;
 
 float block_time(const TileCost& c, int64_t jobs) {
     const float at = (float)jobs / 256.0f;
-    return at <= 0.5f ? c.half : at <= 1 ? c.half + (c.one - c.half) * (2 * at - 1) : c.one + (c.two - c.one) * (at - 1);
+    // (the fullest compute unit counts: 288 workgroups take as long as 512)
+    return at <= 0.5f ? c.half : at <= 1 ? c.half + (c.one - c.half) * (2 * at - 1) : c.one + (c.two - c.one) * (float)((jobs - 1) / 256);
 }
 
 // Rows of 16 `tokens` and `outs` of 16, or a tile.
@@ -138,7 +139,7 @@ Way choose(int N, int I, int O, bool wide32) {
     }
     const bool staged = I % kF8Block != 0;
     const TileCost* costs = staged ? kCostsStaged : wide32 ? kCosts32 : kCosts16;
-    const float read = (float)O * (float)I / 5e6f;
+    const float read = (float)O * (float)I / 8e6f;
     for (int c = 0; c < (staged || wide32 ? 2 : 4); ++c) {
         const TileCost& cost = costs[c];
         const int64_t tiles = (int64_t)ceil_div(O, cost.outs) * ceil_div(N, cost.tokens), round = 256 * cost.slots;
@@ -148,7 +149,7 @@ Way choose(int N, int I, int O, bool wide32) {
             if (parts > 1 && (ceil_div(blocks, run) != parts || bytes > (float)kMostWorkspace || tiles * parts > round)) continue;
             const int64_t jobs = tiles * parts, full = jobs / round, rest = jobs % round;
             const float each = (float)full * block_time(cost, round) + (rest ? block_time(cost, rest) : 0.0f);
-            const float time = 3.5f + std::max((float)run * each, read) + (parts > 1 ? 2.5f + 0.75e-6f * bytes : 0.0f);
+            const float time = 3.5f + std::max((float)run * each, read) + (parts > 1 ? 3.2f + 0.75e-6f * bytes : 0.0f);
             if (time < least) least = time, best = Way{false, 0, 0, F8Tile{cost.outs, cost.tokens, parts, run}};
         }
     }

@@ -1,8 +1,8 @@
 // Products on 8-bit floats for many tokens: tiles of outputs x tokens, operands staged in LDS.
 //
 // A workgroup walks the reduction block by block.  While the matrix cores work on one, the
-// next one is on its way into the other LDS buffer: rows that are whole 16-byte vectors
-// are copied there by the load instruction itself, other rows go through registers.
+// next one (or two) are on their way into other LDS buffers: rows that are whole 16-byte
+// vectors are copied there by the load instruction itself, other rows go through registers.
 // LDS rows are a block's 128 bytes without padding (the copying loads write 64
 // consecutive vectors); the vectors of a row are exchanged by an XOR with three bits of
 // the row that differ between the lanes that read together.
@@ -41,12 +41,15 @@ struct TileParams {
     float* partial;       // [parts][N][O] if parts > 1
 };
 
-// 64 lanes' 16 (4) bytes to consecutive places in LDS.
-__device__ inline void copy16(const void* src, char* dst) {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
+// 64 lanes' 16 (4) bytes, at 32-bit offsets from a base, to consecutive places in LDS.  Not by the compiler's builtins: it
+// would wait for all such copies before reads of LDS that it cannot tell from their targets, and so for those that are
+// meant to be on their way over several blocks.  What is copied is read behind a wait and a barrier only (block_barrier).
+__device__ inline unsigned lds_address(const void* p) { return (unsigned)(uintptr_t)(const __attribute__((address_space(3))) char*)p; }
+__device__ inline void copy16(const void* base, unsigned at, unsigned lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(at), "s"(base) : "m0");
 }
-__device__ inline void copy4(const void* src, char* dst) {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, (__attribute__((address_space(3))) void*)dst, 4, 0, 0);
+__device__ inline void copy4(const void* base, unsigned at, unsigned lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(at), "s"(base) : "m0");
 }
 
 // One operand's vectors of a block, of this work-item: ROWS rows, NT work-items.  VEC: rows of whole blocks at
@@ -70,12 +73,12 @@ struct Fetch {
     // Block k of rows of `cols` values.
     __device__ void load(const uint8_t* base, int k, int cols, char* lds) {
         base += (int64_t)k * kF8Block;
-        const int wave0 = __builtin_amdgcn_readfirstlane((int)threadIdx.x) & ~63;  // the wave's vectors are consecutive
+        const unsigned to = lds_address(lds) + (__builtin_amdgcn_readfirstlane((int)threadIdx.x) & ~63) * 16;  // the wave's vectors are consecutive
         const int64_t left = cols - (int64_t)k * kF8Block;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int in = vector_of(i) * 16;
-            if constexpr (VEC) copy16(base + at[i], lds + (i * NT + wave0) * 16);
+            if constexpr (VEC) copy16(base, at[i], to + i * NT * 16);
             // (at odd addresses too: loaded by words and shifted, as for few rows, 1500 x 4001 x 4001 was 75 us against 67)
             else if (left >= kF8Block) reg[i] = load16(base + at[i]);
             else reg[i] = load_bytes_edge(base + at[i], left - in, (int64_t)k * kF8Block + in);
@@ -97,16 +100,15 @@ struct TokenKey {
     static __device__ int of(int row) { return S::token_key(row); }
 };
 
-// All the wave's loads have landed, its LDS accesses are done; then all waves'.
+// All the wave's loads but the last LEFT have landed, its LDS accesses are done; then all waves'.
+template <int LEFT>
 __device__ inline void block_barrier() {
+    static_assert(LEFT < 64, "what the counter of loads holds");
     asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt(0x70);  // vmcnt(0) lgkmcnt(0)
+    __builtin_amdgcn_s_waitcnt((LEFT & 15) | LEFT >> 4 << 14 | 0x70);  // vmcnt(LEFT) lgkmcnt(0)
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 }
-
-template <int N>
-using Step = std::integral_constant<int, N>;
 
 // 4 FO neighbours of a token.
 template <int YT, int N>
@@ -133,17 +135,19 @@ __device__ inline void store_outputs(void* y, size_t at, const float* v, int64_t
 
 // YT: the result's type; fp32 ones are summed in 16 bits, others on the 8-bit instruction.
 // SPLIT: sums go to the workspace, without bias.
-template <int WO, int WT, int FO, int FT, bool VEC, int YT, bool SPLIT>
+// DEPTH: LDS buffers, of which all but the one that is worked on are on their way.
+template <int WO, int WT, int FO, int FT, bool VEC, int DEPTH, int YT, bool SPLIT>
 __global__ void __launch_bounds__(64 * WO * WT, 2) fc_f8_tiles(TileParams tp) {
     using S = Shape<WO, WT, FO, FT>;
     using Operand = std::conditional_t<YT == CNN_F32, Halves, Bytes>;
     constexpr int TO = S::TO, TT = S::TT, NT = S::NT;
-    // arrays of their own: the compiler sees that a copy into one does not concern reads of another
-    __shared__ __attribute__((aligned(16))) char sW0[TO * kF8Block], sW1[TO * kF8Block], sX0[TT * kF8Block], sX1[TT * kF8Block];
+    static_assert(DEPTH == 2 || VEC, "what goes through registers is one block ahead");
+    static_assert(DEPTH >= 2 && DEPTH <= 4, "the scales have landed before they are read");
+    constexpr int kBuffer = (TO + TT) * kF8Block;
+    __shared__ __attribute__((aligned(16))) char buffers[DEPTH * kBuffer];  // outputs' rows, then tokens'
     __shared__ __attribute__((aligned(16))) float sScale[2][4 * TT];
-    static_assert(NT >= TT, "a lane a token");
-    auto wbuf = [&](auto slot) -> char* { return decltype(slot)::value ? sW1 : sW0; };
-    auto xbuf = [&](auto slot) -> char* { return decltype(slot)::value ? sX1 : sX0; };
+    __shared__ float sWeight[2][64];  // the weights' scales: 4 blocks of each 128 outputs
+    static_assert(NT > TT, "a lane a token, and a wave for the weights");
     const FcF8& p = tp.fc;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, quarter = lane >> 4;
     const int wo = wave / WT, wt = wave % WT, uwave = __builtin_amdgcn_readfirstlane(wave);
@@ -167,21 +171,25 @@ __global__ void __launch_bounds__(64 * WO * WT, 2) fc_f8_tiles(TileParams tp) {
         Fetch<TT, NT, VEC, TokenKey<S>> fx;
         fw.begin(o0, p.O, p.I);
         fx.begin(n0, p.N, p.I);
-        const float* ws = p.ws + (size_t)min((o0 + uwave / WT * FO * 16) >> 7, (int64_t)(p.O - 1) >> 7) * tp.blocks;
         // The inputs' scales come in groups of 4 blocks, a lane a token: a row's are neighbours, and a line for
         // every token and block would take as long as the operands (2048 x 9216 x 4096: 99 us against 109 with half as
-        // many of them, and 77 against 100 for the copies alone).
-        const float* xs = p.xs + (size_t)min(n0 + tid % TT, (int64_t)p.N - 1) * tp.blocks;
-        float wscale[2];
+        // many of them, and 77 against 100 for the copies alone).  So do the weights', a lane one of them.  (A scalar load of
+        // the block's would make the reads of LDS after it wait for all before.)
+        const unsigned xs = (unsigned)min(tid % TT, (int)min((int64_t)p.N - 1 - n0, (int64_t)TT)) * (unsigned)tp.blocks * 4;  // fewer than 2^31 bytes
         auto ask_scales = [&](int group) {
-            if (uwave >= TT / 64) return;
             const int k = first + 4 * group;
-            char* dst = (char*)sScale[group & 1];
+            if (uwave == TT / 64) {
+                const unsigned row = (unsigned)min((o0 >> 7) + (lane >> 2), (int64_t)(p.O - 1) >> 7);
+                copy4(p.ws, (row * (unsigned)tp.blocks + (unsigned)min(k + (lane & 3), tp.blocks - 1)) * 4, lds_address(sWeight[group & 1]));
+            }
+            if (uwave >= TT / 64) return;
+            const float* base = p.xs + (size_t)n0 * tp.blocks;
+            const unsigned dst = lds_address(sScale[group & 1]);
             if (tp.whole_scales) {
-                copy16(xs + k, dst + uwave * 64 * 16);
+                copy16(base + k, xs, dst + uwave * 64 * 16);
             } else {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) copy4(xs + min(k + i, tp.blocks - 1), dst + (i * TT + uwave * 64) * 4);
+                for (int i = 0; i < 4; ++i) copy4(base + min(k + i, tp.blocks - 1), xs, dst + (i * TT + uwave * 64) * 4);
             }
         };
         const int scale_token = tp.whole_scales ? 4 : 1, scale_block = tp.whole_scales ? 1 : TT;
@@ -204,57 +212,55 @@ __global__ void __launch_bounds__(64 * WO * WT, 2) fc_f8_tiles(TileParams tp) {
             else return b;
         };
         // Asks for block k, or, behind the last one, for that again (nothing comes of it).
-        auto ask = [&](int k, auto slot) {
+        auto ask = [&](int k, char* to) {
             k = min(k, last - 1);
-            wscale[decltype(slot)::value] = ws[k];
-            fw.load(p.w, k, p.I, wbuf(slot));
-            fx.load(p.x, k, p.I, xbuf(slot));
+            fw.load(p.w, k, p.I, to);
+            fx.load(p.x, k, p.I, to + TO * kF8Block);
         };
         const int key = S::out_key(orow);
         Operand x[FT];
         Bytes next;                   // the outputs' next fragment
         f32x4 d[2][FT];               // a fragment's sums, and those of the one before
         float s[FT], before[FT];      // a block's scales, and those of the one before
-        auto read_scales = [&](int k, auto slot, float* to) {
+        auto read_scales = [&](int k, float* to) {
             const int at = k - first;
+            const float w = sWeight[(at >> 2) & 1][(wo * FO * 16 >> 7) * 4 + (at & 3)];
             const float* group = sScale[(at >> 2) & 1] + (at & 3) * scale_block + trow * scale_token;
 #pragma unroll
             for (int j = 0; j < FT; ++j) {
-                const float v = group[16 * j * scale_token] * wscale[decltype(slot)::value];
+                const float v = group[16 * j * scale_token] * w;
                 to[j] = k < last ? v : 0.0f;
             }
         };
-        auto read_token = [&](auto slot, int j) { x[j] = as_operand(read(xbuf(slot), trow + 16 * j, S::token_key(l16))); };
+        auto read_token = [&](const char* buffer, int j) { x[j] = as_operand(read(buffer + TO * kF8Block, trow + 16 * j, S::token_key(l16))); };
         // Block k, whose first fragments are in registers.  The products of a fragment of outputs are at work while the sums
         // of the one before are added.  Before its last fragment's products the next block is made ready, a later one is
         // asked for (this one's buffer is free: all waves have read what they need), and the next one's
-        // first fragments are read: those products cover that.  (Three buffers, which leave no more than one workgroup to
-        // a compute unit, were no faster: 256 x 128 tiles 91.6 us against 84.7, 2048 x 9216 x 4096.)
-        auto work = [&](int k, auto slot) {
-            using Here = decltype(slot);
-            using Next = Step<1 - Here::value>;
-            float after[FT];
+        // first fragments are read: those products cover that.
+        constexpr int OPS = decltype(fw)::N + decltype(fx)::N;  // a wave's loads for a block
+        auto work = [&](int k, char* here, char* after) {
+            float s_after[FT];
 #pragma unroll
             for (int i = 0; i < FO; ++i) {
                 const Operand w = as_operand(next);
                 if (i + 1 < FO) {
-                    next = read(wbuf(Here{}), orow + 4 * (i + 1), key);
+                    next = read(here, orow + 4 * (i + 1), key);
                 } else {
-                    fw.store(wbuf(Next{}));
-                    fx.store(xbuf(Next{}));
-                    block_barrier();
-                    // (scales are read before others are asked for: the compiler would wait for those first, and so for all)
-                    read_scales(k + 1, Next{}, after);
-                    next = read(wbuf(Next{}), orow, key);
+                    fw.store(after);
+                    fx.store(after + TO * kF8Block);
+                    block_barrier<(DEPTH - 2) * OPS>();
+                    read_scales(k + 1, s_after);
+                    next = read(after, orow, key);
                     __builtin_amdgcn_sched_barrier(0);
-                    ask(k + 2, Here{});
-                    // the other group's places have been read by all waves; what is asked for now is used 3 blocks later
+                    ask(k + DEPTH, here);
+                    // the other group's places have been read by all waves; what is asked for now is used 3 blocks later, and
+                    // two blocks' loads are asked for before that: the barriers wait for it
                     if (((k - first) & 3) == 0 && k + 4 < last) ask_scales(((k - first) >> 2) + 1);
                 }
 #pragma unroll
                 for (int j = 0; j < FT; ++j) {
                     d[i % 2][j] = block_sums(w, x[j]);
-                    if (i + 1 == FO) read_token(Next{}, j);
+                    if (i + 1 == FO) read_token(after, j);
                     const int done = (i + FO - 1) % FO;
                     add_scaled(acc[done][j], d[(i + 1) % 2][j], i == 0 ? before[j] : s[j]);
                     asm volatile("" : "+v"(acc[done][j]));  // here, and not when the sum is next needed
@@ -262,29 +268,30 @@ __global__ void __launch_bounds__(64 * WO * WT, 2) fc_f8_tiles(TileParams tp) {
                 }
             }
 #pragma unroll
-            for (int j = 0; j < FT; ++j) before[j] = s[j], s[j] = after[j];
+            for (int j = 0; j < FT; ++j) before[j] = s[j], s[j] = s_after[j];
         };
         static_assert(FO % 2 == 0, "a fragment's set of sums is the same in every block");
         if (first < last) {
             ask_scales(0);
-            ask(first, Step<0>{});
-            fw.store(sW0);
-            fx.store(sX0);
-            ask(first + 1, Step<1>{});
-            block_barrier();
-            next = read(sW0, orow, key);
-            read_scales(first, Step<0>{}, s);
+            ask(first, buffers);
+            fw.store(buffers);
+            fx.store(buffers + TO * kF8Block);
+#pragma unroll
+            for (int i = 1; i < DEPTH; ++i) ask(first + i, buffers + i * kBuffer);
+            block_barrier<VEC ? (DEPTH - 1) * OPS : 0>();
+            next = read(buffers, orow, key);
+            read_scales(first, s);
 #pragma unroll
             for (int j = 0; j < FT; ++j) {
-                read_token(Step<0>{}, j);
+                read_token(buffers, j);
                 before[j] = 0.0f;
                 d[1][j] = f32x4{0, 0, 0, 0};
             }
-            // whole turns: blocks behind the last one have a scale of 0
+            // whole turns of the buffers: blocks behind the last one have a scale of 0
 #pragma unroll 1
-            for (int k = first; k < last; k += 2) {
-                work(k, Step<0>{});
-                work(k + 1, Step<1>{});
+            for (int k = first; k < last; k += DEPTH) {
+#pragma unroll
+                for (int i = 0; i < DEPTH; ++i) work(k + i, buffers + i * kBuffer, buffers + (i + 1) % DEPTH * kBuffer);
             }
 #pragma unroll
             for (int j = 0; j < FT; ++j) add_scaled(acc[FO - 1][j], d[1][j], before[j]);
@@ -306,7 +313,7 @@ __global__ void __launch_bounds__(64 * WO * WT, 2) fc_f8_tiles(TileParams tp) {
                 else store_outputs<YT, FO * 4>(p.y, (size_t)n * p.O + o, v, count);
             }
         }
-        block_barrier();  // nothing is on its way to the buffers, which are the next tile's
+        block_barrier<0>();  // nothing is on its way to the buffers, which are the next tile's
     }
 }
 
@@ -351,14 +358,18 @@ __global__ void __launch_bounds__(256) fc_f8_join(TileParams tp) {
 template <int WO, int WT, int FO, int FT, bool VEC, int YT>
 void start(const FcF8& p, const F8Tile& t, float* partial, hipStream_t st) {
     using S = Shape<WO, WT, FO, FT>;
+    // Three buffers for the smallest tiles of 16-bit results: 64 x 9216 x 4096, 32 of them, 42.5 to 30.7 us, in 6 parts 17.8 to
+    // 16.0; 512 x 4096 x 4096 22.9 to 18.4.  No faster are four, or three for fp32 results (53.1 and 52.7), or for
+    // larger tiles (2048 x 9216 x 4096 on 256 x 128: 77 and 84): they have enough to do for a block's time.
+    constexpr int DEPTH = VEC && S::TT == 64 && YT != CNN_F32 ? 3 : 2;
     const int blocks = f8_blocks(p.I);
     TileParams tp{p, blocks, ceil_div(p.O, S::TO), 0, t.parts, t.run, (uintptr_t)p.xs % 16 == 0 && blocks % 4 == 0, partial};
     tp.tiles = tp.out_tiles * ceil_div(p.N, S::TT);
     const dim3 grid((unsigned)std::min<int64_t>((int64_t)tp.tiles * tp.parts, 1 << 20));
     if (t.parts == 1) {
-        enqueue(fc_f8_tiles<WO, WT, FO, FT, VEC, YT, false>, grid, dim3(S::NT), 0, st, tp);
+        enqueue(fc_f8_tiles<WO, WT, FO, FT, VEC, DEPTH, YT, false>, grid, dim3(S::NT), 0, st, tp);
     } else {
-        enqueue(fc_f8_tiles<WO, WT, FO, FT, VEC, YT, true>, grid, dim3(S::NT), 0, st, tp);
+        enqueue(fc_f8_tiles<WO, WT, FO, FT, VEC, DEPTH, YT, true>, grid, dim3(S::NT), 0, st, tp);
         enqueue(fc_f8_join<YT>, dim3((unsigned)std::min<int64_t>(ceil_div64((int64_t)p.N * p.O, 1024), 1 << 16)), dim3(256), 0, st, tp);
     }
 }

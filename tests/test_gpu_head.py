@@ -152,7 +152,7 @@ def test_head_on_another_stream(gpu, t):
 # outputs, whole and with the reduction split, from vectors and through registers.
 WAYS = [(3, 130, 9000), (651, 128, 1166), (13, 15616, 130), (5499, 128, 1040), (3161, 15744, 3), (3536, 128, 1676),
         (2114, 20736, 422), (6535, 128, 1797), (768, 19968, 3018), (1214, 58752, 1774), (759, 246, 1054), (15, 16253, 130),
-        (3992, 47, 777), (459, 2171, 1467)]
+        (3992, 47, 777), (459, 2171, 1467), (4171, 128, 386), (64, 9216, 4096), (12, 24543, 1), (20, 16145, 2)]
 
 
 def operands(n, i, o, seed):
@@ -186,3 +186,16 @@ def test_product_every_way_at_odd_addresses(gpu, n, i, o):
     y = torch.empty((n * o + 1,), dtype=torch.float16, device="cuda")[1:].view(n, o)
     gpu.cnn_fc_f8_fwd(moved(x, 3), xs, moved(w, 17), ws, b, y=y)
     ref.assert_product(y, want, s, i, f"{n}x{i}x{o}")
+
+
+@pytest.mark.parametrize("n,o", [(600, 1200), (2305, 776), (4000, 1100), (3400, 2440)])
+def test_product_numbers_of_blocks(gpu, n, o):
+    """Reductions of one block, of as many as there are buffers, of a few more."""
+    for blocks in (*range(1, 10), 13):
+        x, xs, w, ws, b = operands(n, 128 * blocks, o, n + blocks)
+        want, s = ref.product(x, xs, w, ws, b, False)
+        for dtype in (torch.float32, torch.float16):
+            y = gpu.cnn_fc_f8_fwd(x, xs, w, ws, b, y_dtype=dtype)
+            ref.assert_product(y, want, s, 128 * blocks, f"{n}x{128 * blocks}x{o} {dtype}")
+            for _ in range(3):
+                assert torch.equal(y, gpu.cnn_fc_f8_fwd(x, xs, w, ws, b, y_dtype=dtype))
