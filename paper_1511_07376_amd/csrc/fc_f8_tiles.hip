@@ -12,7 +12,7 @@
 //
 // 2048 x 9216 x 4096 to bf16 (256 x 128 tiles): 77 us, 2.0 PFLOP/s; the matrix cores are at work for 40% of it,
 // and waves wait for a block's barrier, LDS and each other's turn for the rest.  64 x 9216 x 4096 to fp32 (128 x 64
-// tiles in 8 parts): 16 us and 4 for the join, of which reading the weights would take 7.5.
+// tiles in 6 parts): 16 us and 4 for the join, of which reading the weights would take 7.5.
 #include "fc_f8.h"
 
 #include <algorithm>
