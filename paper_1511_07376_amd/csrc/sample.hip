@@ -74,8 +74,8 @@ struct Scale {
         if (infinite) return l == INFINITY ? 0.0f : -INFINITY;
         return l > -INFINITY ? l + 0.0f : -INFINITY;
     }
-    // Not falling as the logit falls, in the same way wherever it is called.  (Halves: the
-    // difference of the largest and the least float is more than a float.)
+    // Not falling as the logit falls, in the same way wherever it is called; the last one for minus infinity and NaN.
+    // (Halves: the difference of the largest and the least float is more than a float.)
     CNN_INLINE int bin(float v) const { return (int)fminf((0.5f * top - 0.5f * v) * bins, (float)(kBins - 1)); }
     // 2^bits exp((v - top) / T), rounded to a whole number: 2^f by a polynomial that
     // interpolates it at the Chebyshev nodes of [-1/2, 1/2] (to 3e-16), 1 at f = 0.
@@ -155,20 +155,31 @@ struct Row {
     CNN_INLINE bool keeps(u64 code, u64 w, u64 last) const { return code <= last && (w >= least || code == first_code); }
 };
 
-// f(token, logit) for the tokens from `from` to `to` of a row of V, 8 neighbours a work-item (`from` is a
+// f(token, 8 logits from it on) for the tokens from `from` to `to` of a row of V, 8 neighbours a work-item (`from` is a
 // multiple of 8).  Logits of no token are minus infinity.
+template <typename T>
+CNN_INLINE void load_logits(const T* row, int64_t c, int64_t to, int V, float* v) {
+    load_values8(row, (int)c, V, v);
+    if (to - c < 8) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = c + i < to ? v[i] : -INFINITY;
+    }
+}
 template <typename T, typename F>
-CNN_INLINE void each_logit(const T* row, int64_t from, int64_t to, int V, F&& f) {
+CNN_INLINE void each_eight(const T* row, int64_t from, int64_t to, int V, F&& f) {
     for (int64_t c = from + threadIdx.x * 8; c < to; c += (int64_t)blockDim.x * 8) {
         float v[8];
-        load_values8(row, (int)c, V, v);
-        if (to - c < 8) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = c + i < to ? v[i] : -INFINITY;
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f((int)c + i, v[i]);
+        load_logits(row, c, to, V, v);
+        f((int)c, v);
     }
+}
+// f(token, logit) for each.
+template <typename T, typename F>
+CNN_INLINE void each_logit(const T* row, int64_t from, int64_t to, int V, F&& f) {
+    each_eight(row, from, to, V, [&](int c, const float* v) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f(c + i, v[i]);
+    });
 }
 
 // ---------------------------------------------------------------- within a workgroup
@@ -578,11 +589,17 @@ CNN_INLINE Drawn draw_sorted(Shared<NT>& s, List& list, const Row& r, int n, u64
 // The largest logit and its first token, as one number (0: there is none).
 template <int NT, typename T>
 CNN_INLINE u64 largest(Shared<NT>& s, const T* x, int64_t from, int64_t to, int V) {
-    float most = -INFINITY;
-    int first = 0;
-    each_logit(x, from, to, V, [&](int i, float l) {
-        if (l > most) most = l, first = i;
+    float most = -INFINITY, v[8];
+    int at = 0, first = 0;
+    each_eight(x, from, to, V, [&](int c, const float* l) {  // (fmaxf leaves NaN out)
+        const float m = fmaxf(fmaxf(fmaxf(l[0], l[1]), fmaxf(l[2], l[3])), fmaxf(fmaxf(l[4], l[5]), fmaxf(l[6], l[7])));
+        if (m > most) most = m, at = c;
     });
+    if (most > -INFINITY) {
+        load_logits(x, at, to, V, v);
+#pragma unroll
+        for (int i = 7; i >= 0; --i) first = v[i] == most ? at + i : first;
+    }
     return group_max(s, most > -INFINITY ? (u64)key_of(most + 0.0f) << 32 | (unsigned)~first : 0);
 }
 
@@ -598,9 +615,13 @@ CNN_INLINE void add_by_weight(Shared<NT>& s, const T* x, int64_t from, int64_t t
             atomicAdd(&s.sum[b], r.scale.weight(v));
             atomicAdd(&s.count[b], 1u);
         });
+    } else if (r.scale.infinite) {
+        each_logit(x, from, to, V, [&](int, float l) {
+            if (l == INFINITY) atomicAdd(&s.count[0], 1u);
+        });
     } else {
         each_logit(x, from, to, V, [&](int, float l) {
-            const int b = r.scale.bin(r.scale.value(l));
+            const int b = r.scale.bin(l);
             if (b < kBins - 1) atomicAdd(&s.count[b], 1u);
         });
     }
@@ -610,11 +631,7 @@ CNN_INLINE void add_by_weight(Shared<NT>& s, const T* x, int64_t from, int64_t t
 template <typename T>
 CNN_INLINE u64 kept_weights(const T* x, int64_t c, int V, const Row& r, u64 last, u64* w) {
     float l[8];
-    load_values8(x, (int)c, V, l);
-    if (V - c < 8) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) l[i] = c + i < V ? l[i] : -INFINITY;
-    }
+    load_logits(x, c, V, V, l);
     u64 sum = 0;
     if (last == kAll && r.least == 0 && !r.scale.infinite) {  // minus infinity and NaN weigh nothing
 #pragma unroll
@@ -666,13 +683,14 @@ CNN_INLINE void draw_in_tile(Shared<NT>& s, const T* x, int64_t from, int64_t to
 // put(code) for the tokens kept by code of the bins first..end, between two places of the row.
 template <typename T, typename F>
 CNN_INLINE void each_in_bins(const T* x, int64_t from, int64_t to, int V, const Row& r, int first, int end, u64 last, F&& put) {
-    each_logit(x, from, to, V, [&](int i, float l) {
-        const float v = r.scale.value(l);
+    auto in = [&](int i, float v) {
         const int b = r.scale.bin(v);
         if (b < first || b > end) return;
-        const u64 code = code_of(v, i);
+        const u64 code = code_of(v + 0.0f, i);
         if (code <= last) put(code);
-    });
+    };
+    if (r.scale.infinite) each_logit(x, from, to, V, [&](int i, float l) { in(i, r.scale.value(l)); });
+    else each_logit(x, from, to, V, in);
 }
 // The weights of the list's codes.
 CNN_INLINE void weigh_list(List& list, const Row& r, int n) {
@@ -971,9 +989,9 @@ void run(const Args& a, bool cuts, hipStream_t st) {
     if (a.split.chunks == 0) {
         // A workgroup's barriers cost more the larger it is, its passes less: 128 rows of 1000, 4096, 8000 with
         // cuts took 17.6, 22.8, 30.5 us with 256 work-items and 16.1, 19.3, 24.0 with 512, one of 1000 11.7 and
-        // 12.1; 128 of 32768 46.9 with 512 and 42.0 with 1024, without cuts 20.5 and 20.9.
+        // 12.1; 128 of 32768 46.9 with 512 and 42.0 with 1024, without cuts 20.5 and 20.9, of 50021 28.7 and 26.7.
         if (a.p.V <= 1024) run_rows<T, 256>(a, rows, st);
-        else if (a.p.V <= 20000 || !cuts) run_rows<T, 512>(a, rows, st);
+        else if (a.p.V <= (cuts ? 20000 : 40000)) run_rows<T, 512>(a, rows, st);
         else run_rows<T, 1024>(a, rows, st);
         return;
     }
