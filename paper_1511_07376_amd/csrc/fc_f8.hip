@@ -98,7 +98,7 @@ void run_rows(const FcF8& p, bool odd, hipStream_t st) {
 // What a call costs one way or another, in us, as measured between 1 x 512 x 8192 and 4096 x 4096 x 8192.
 //
 // Rows: every workgroup reads its outputs' weights and its tokens' inputs, at some 6 TB/s from the L2s and behind them, and
-// half of that from odd addresses.
+// three quarters to a half of that from odd addresses.
 //
 // Tiles: their blocks' times, which grow with the workgroups that share a compute unit, or the weights' time from memory, and
 // some 3.5 us around them; parts take a second kernel, and their way through memory.
@@ -108,7 +108,9 @@ struct TileCost {
 };
 constexpr TileCost kCosts16[] = {{128, 64, 2, 0.37f, 0.47f, 0.75f}, {128, 128, 2, 0.70f, 0.85f, 1.30f}, {256, 128, 1, 0.95f, 1.15f, 0}, {256, 256, 1, 1.57f, 2.1f, 0}};
 constexpr TileCost kCosts32[] = {{128, 64, 3, 0.77f, 0.86f, 1.32f}, {128, 128, 2, 1.27f, 1.56f, 2.23f}};
-constexpr TileCost kCostsStaged[] = {{128, 64, 3, 1.2f, 1.4f, 1.8f}, {128, 128, 2, 1.5f, 1.75f, 2.2f}};  // through registers
+// through registers
+constexpr TileCost kCostsStaged16[] = {{128, 64, 3, 1.15f, 1.25f, 2.1f}, {128, 128, 2, 1.6f, 1.65f, 2.2f}};
+constexpr TileCost kCostsStaged32[] = {{128, 64, 2, 1.45f, 1.68f, 2.3f}, {128, 128, 2, 2.2f, 2.5f, 3.2f}};
 constexpr int kMostParts = 16;
 constexpr size_t kMostWorkspace = 64 << 20;
 
@@ -134,11 +136,11 @@ Way choose(int N, int I, int O, bool wide32) {
         const int64_t jobs = (int64_t)ceil_div(O, 16 * r[1]) * ceil_div(N, 16 * r[0]);
         // 256 of them at once take one's time, and 32 outputs a workgroup are slower where there are fewer
         const float bytes = (float)std::max<int64_t>(jobs, r[1] == 2 ? 256 : 128) * (float)(16 * r[1] + std::min(N, 16 * r[0])) * (float)I;
-        const float time = 3.0f + bytes / 6.3e6f * (I % 4 ? 1.3f : 1.0f);
+        const float time = 3.0f + bytes / 6.3e6f * (I % 4 == 0 ? 1.0f : r[0] == 4 ? 2.1f : 1.3f);
         if (time < least) least = time, best = Way{true, r[0], r[1], {}};
     }
     const bool staged = I % kF8Block != 0;
-    const TileCost* costs = staged ? kCostsStaged : wide32 ? kCosts32 : kCosts16;
+    const TileCost* costs = staged ? (wide32 ? kCostsStaged32 : kCostsStaged16) : wide32 ? kCosts32 : kCosts16;
     const float read = (float)O * (float)I / 8e6f;
     for (int c = 0; c < (staged || wide32 ? 2 : 4); ++c) {
         const TileCost& cost = costs[c];
