@@ -61,7 +61,7 @@ __global__ void __launch_bounds__(64 * kMostWaves) fc_f8_rows(FcF8 p, int blocks
             const int64_t at = (int64_t)k * kF8Block;
             add(k, [&](const uint8_t* base, unsigned row) { return load32<ODD>(base + at + row); });
         }
-        if (whole < last) {
+        if (first < last && whole < last) {  // (waves behind the last block have none)
             const int64_t at = (int64_t)whole * kF8Block, in = at + quarter * 32, left = p.I - in;
             add(whole, [&](const uint8_t* base, unsigned row) {
                 return Bytes{load_bytes_edge(base + at + row, left, in), load_bytes_edge(base + at + row + 16, left - 16, in + 16)};

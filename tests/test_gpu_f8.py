@@ -224,6 +224,14 @@ def test_product_nan_and_its_rows(gpu):
         assert float(y[n // 2].abs().max()) == 0
 
 
+@pytest.mark.parametrize("n,o", [(3, 50), (20, 33), (70, 300), (2, 8300), (90, 900)])
+def test_product_ends_inside_a_block(gpu, n, o):
+    """Few tokens: a workgroup's waves share the blocks, the last of which is not whole; waves may have none."""
+    for blocks in (*range(1, 35), 63, 70):
+        for dtype, i in ((torch.float32, 128 * blocks - 7), (torch.bfloat16, 128 * blocks - 120)):
+            check(gpu, n, i, o, dtype, bias=True, relu=False)
+
+
 @pytest.mark.parametrize("shift", [1, 4, 8])
 def test_product_at_any_byte(gpu, shift):
     for n, i, o in ((2, 256, 64), (40, 512, 130), (260, 384, 257)):

@@ -152,7 +152,9 @@ def test_head_on_another_stream(gpu, t):
 # outputs, whole and with the reduction split, from vectors and through registers.
 WAYS = [(3, 130, 9000), (651, 128, 1166), (13, 15616, 130), (5499, 128, 1040), (3161, 15744, 3), (3536, 128, 1676),
         (2114, 20736, 422), (6535, 128, 1797), (768, 19968, 3018), (1214, 58752, 1774), (759, 246, 1054), (15, 16253, 130),
-        (3992, 47, 777), (459, 2171, 1467), (4171, 128, 386), (64, 9216, 4096), (12, 24543, 1), (20, 16145, 2)]
+        (3992, 47, 777), (459, 2171, 1467), (4171, 128, 386), (64, 9216, 4096), (12, 24543, 1), (20, 16145, 2), (335, 1905, 1355),
+        (807, 2211, 423), (491, 2226, 958), (1688, 1362, 2688), (16, 32631, 5), (1631, 8704, 1159), (1805, 20352, 2259),
+        (587, 5760, 3442), (885, 250, 646), (768, 119, 1090)]
 
 
 def operands(n, i, o, seed):
