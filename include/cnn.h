@@ -335,8 +335,8 @@ int cnn_f8_dequantize(const uint8_t* q, const float* scale, int rows, int cols,
  *   weight fp32 [cols] or NULL (ones)      eps finite, 0 or more
  *   sum [rows][cols], s rounded to x's type, or NULL
  *   y [rows][cols]; y_type that of x (then y_scale is NULL), or CNN_F8: brought
- *     to 8 bits from the fp32 results as by cnn_f8_quantize with block_rows 1,
- *     y_scale fp32 [rows][ceil(cols/128)]
+ *     to 8 bits as by cnn_f8_quantize with block_rows 1, but from results that
+ *     are not rounded before (in 64 bits), y_scale fp32 [rows][ceil(cols/128)]
  * The norm is of s as it is before it is rounded.  Squares are summed in 64
  * bits.  y (if not CNN_F8) and sum may each be x or residual, but not both the
  * same one. */

@@ -120,20 +120,26 @@ struct F8Scale {
     }
 };
 
-// 8 values in 8 bits: times the factor, rounded to fp32, then to the nearest, ties to even.
-// The largest becomes 448 or a rounding more, which 448 is the nearest to.
-__device__ inline u32x2 to_f8(const float* v, const F8Scale& s) {
-    u32x2 out = {0, 0};
-    if (!s.bad) {
+// 8 values in 8 bits: to the nearest, ties to even.  (A block's largest times its factor is 448 or a rounding more,
+// which 448 is the nearest to.)
+__device__ inline u32x2 to_f8(const float* v) {
+    u32x2 out;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            int w = 0;
-            w = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * h] * s.factor, v[4 * h + 1] * s.factor, w, false);
-            w = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * h + 2] * s.factor, v[4 * h + 3] * s.factor, w, true);
-            out[h] = (unsigned)w;
-        }
+    for (int h = 0; h < 2; ++h) {
+        int w = 0;
+        w = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * h], v[4 * h + 1], w, false);
+        w = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * h + 2], v[4 * h + 3], w, true);
+        out[h] = (unsigned)w;
     }
     return out;
+}
+// ... times the factor, rounded to fp32.
+__device__ inline u32x2 to_f8(const float* v, const F8Scale& s) {
+    if (s.bad) return u32x2{0, 0};
+    float scaled[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) scaled[i] = v[i] * s.factor;
+    return to_f8(scaled);
 }
 __device__ inline void store_f8(uint8_t* row, int c, int cols, u32x2 q) {
     if (c <= cols - 8) {

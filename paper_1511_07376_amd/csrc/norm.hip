@@ -5,13 +5,15 @@
 //
 // s is fp32 (it is rounded where it is stored, not where it is used), its squares
 // are summed in 64 bits, which no value over- or underflows and which cost
-// nothing beside the memory's time, y is rounded once to its type, or brought to 8
-// bits by the block as f8_quantize does from these fp32 values.
+// nothing beside the memory's time, y is rounded to fp32 after each product and then to its type.  8-bit
+// results are made in 64 bits: a value near the middle between two 8-bit floats goes to the one
+// that the definition gives, where fp32's roundings would now and then (a few of 10^7) take the other.
 //
 // Bound by HBM: every tensor is read or written once, a row held in registers
 // between the sum and the result (up to 16384 values).  A work-item takes vectors of 8 values, so
-// that 16 lanes hold a block of 128.  8192 x 4096 bf16 with residual and sum, to 8 bits: 49 to 51 us,
-// 4.7 TB/s (a copy reaches 5.05); 77 x 1013 fp32 3 us, which is a kernel's least and a chain of load,
+// that 16 lanes hold a block of 128.  8192 x 4096 bf16 with residual and sum, to 8 bits: 61 to 63
+// us, 3.8 TB/s, of which the 64 bits take 11 (made from fp32 values it was 50, 4.7 TB/s; a copy reaches
+// 5.05); 77 x 1013 fp32 3 us, which is a kernel's least and a chain of load,
 // sum and store.
 #include "f8.h"
 
@@ -39,6 +41,20 @@ __device__ inline double group_sum(double v, double* part) {
     return v;
 }
 
+// The largest of 16 neighbouring lanes, in all of them: rotations within a row of 16.
+template <int CTRL>
+__device__ inline double rotated(double v) {
+    const uint64_t u = (uint64_t)__double_as_longlong(v);
+    const unsigned lo = (unsigned)__builtin_amdgcn_mov_dpp((int)u, CTRL, 0xf, 0xf, true), hi = (unsigned)__builtin_amdgcn_mov_dpp((int)(u >> 32), CTRL, 0xf, 0xf, true);
+    return __longlong_as_double((long long)((uint64_t)hi << 32 | lo));
+}
+__device__ inline double max_of_16_lanes(double v) {
+    v = fmax(v, rotated<0x128>(v));
+    v = fmax(v, rotated<0x124>(v));
+    v = fmax(v, rotated<0x122>(v));
+    return fmax(v, rotated<0x121>(v));
+}
+
 template <typename T, bool F8>
 struct Output {
     T* y;
@@ -48,17 +64,27 @@ struct Output {
     // 8 results of a row from column c on (c: cols or more for lanes with none; all
     // 16 lanes of a block are here)
     __device__ void put(int row, int c, int cols, int blocks, const float* s, const float* w, double r) const {
-        float v[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = (float)((double)s[i] * r) * w[i];
         if (sum) store_values8(sum + (size_t)row * cols, c, cols, s);
+        float v[8];
         if constexpr (F8) {
+            // s w and its maximum are exact in 64 bits
+            double p[8], top = 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = c < cols - i ? v[i] : 0.0f;  // what is behind the row: 0 / 0, say
-            const F8Scale f(max_of_16_lanes(top_bits8(v)));
-            store_f8(q + (size_t)row * cols, c, cols, to_f8(v, f));
-            if ((threadIdx.x & 15) == 0 && c < cols) scale[(size_t)row * blocks + c / kF8Block] = f.scale;
+            for (int i = 0; i < 8; ++i) {
+                p[i] = (double)s[i] * (double)w[i];  // 0 behind the row
+                top = fmax(top, fabs(p[i]));
+            }
+            const double a = fmax(max_of_16_lanes(top) * r, (double)kF8LeastTop), factor = r * (double)(float)((double)kF8Most / a);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = c < cols - i ? (float)(p[i] * factor) : 0.0f;  // 0 over 0 too
+            // (a value that is none makes its scaled one NaN: infinity is scaled by 0)
+            const float of = (float)(a * (1 / (double)kF8Most));
+            const bool bad = max_of_16_lanes(top_bits8(v)) >= 0x7f800000u || of == INFINITY;
+            store_f8(q + (size_t)row * cols, c, cols, bad ? u32x2{0, 0} : to_f8(v));
+            if ((threadIdx.x & 15) == 0 && c < cols) scale[(size_t)row * blocks + c / kF8Block] = bad ? __uint_as_float(0x7fc00000u) : of;
         } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = (float)((double)s[i] * r) * w[i];
             store_values8(y + (size_t)row * cols, c, cols, v);
         }
     }
@@ -114,8 +140,8 @@ __global__ void __launch_bounds__(1024) rms_norm_rows(const T* x, const T* res, 
     }
 }
 
-// Longer rows: read twice, the second time mostly from the caches.  1024 x 32768 bf16 to 8 bits: 68 us, 3.5
-// TB/s.  (Four vectors a work-item held in registers spill: 75 us, in fp32 128 against 136.)
+// Longer rows: read twice, the second time mostly from the caches.  1024 x 32768 bf16 to 8 bits: 71 us, 3.3
+// TB/s.  (Four vectors a work-item held in registers spill.)
 // Each value is read before it is written, by the same work-item: y and sum may be x or residual.
 template <typename T, bool F8>
 __global__ void __launch_bounds__(1024) rms_norm_long(const T* x, const T* res, const float* w, Output<T, F8> out, int rows, int cols, float eps) {
@@ -152,10 +178,10 @@ void run(const RmsNorm& p, hipStream_t st) {
         enqueue(kernel, grid, dim3(64 * waves), 0, st, (const T*)p.x, (const T*)p.residual, p.weight, out, p.rows, p.cols, p.eps);
     };
     const int64_t waves = ceil_div64(vectors, 64);
-    // One vector a work-item up to 1024 work-items, of fp32 up to 512: 4096 x 8192 took 55 us with one and 58 with two in
-    // bf16, 109 and 98 in fp32; 8192 x 4096 51 and 55, 97 and 101.  2048 x 16384 with two and read twice: 62 and 68
-    // in bf16, 115 and 125 in fp32.
-    if (waves <= (sizeof(T) == 4 ? 8 : 16)) go(rms_norm_rows<T, F8, 1>, (int)waves);
+    // One vector a work-item up to 1024 work-items, of fp32 or to 8 bits up to 512: 4096 x 8192 took 77 us with one and 66 with
+    // two in bf16 to 8 bits, 109 and 98 in fp32; 8192 x 4096 63 and 65, 97 and 101.  2048 x 16384 with two and read
+    // twice: 72 and 74 in bf16 to 8 bits, 115 and 125 in fp32.
+    if (waves <= (F8 || sizeof(T) == 4 ? 8 : 16)) go(rms_norm_rows<T, F8, 1>, (int)waves);
     else if (waves <= 32) go(rms_norm_rows<T, F8, 2>, (int)ceil_div64(waves, 2));
     else go(rms_norm_long<T, F8>, 16);
 }

@@ -156,3 +156,18 @@ def test_norm_writes_its_own_rows_only(gpu):
                              y_scale=sroom[32:32 + rows * nb].view(rows, nb))
         assert bool((qroom[:33] == 7).all()) and bool((qroom[33 + rows * cols:] == 7).all())
         assert bool((sroom[:32] == 7).all()) and bool((sroom[32 + rows * nb:] == 7).all())
+
+
+@pytest.mark.parametrize("residual", [False, True])
+@pytest.mark.parametrize("rows,cols", [(1024, 4096), (3000, 1000), (100, 33000)])
+def test_norm_in_8_bits_is_that_of_unrounded_values(gpu, rows, cols, residual):
+    """Among 10^6 values some are so near to the middle between two 8-bit floats that fp32's roundings would decide: codes are
+    those of the definition in 64 bits, but for values within 2^-50 of a middle (of 10^6 none)."""
+    g = gen(rows)
+    x = torch.randn((rows, cols), generator=g, device="cuda")
+    r = torch.randn((rows, cols), generator=g, device="cuda") if residual else None
+    w = 1 + 0.2 * torch.randn((cols,), generator=g, device="cuda")
+    q, scale = gpu.cnn_rms_norm_fwd(x, w, r, 1e-5, f8=True)[:2]
+    want, want_scale = ref.quantize(ref.norm(x, r, w, 1e-5)[1])
+    assert torch.equal(q.double(), want)
+    assert bool(((scale.double() / want_scale.double() - 1).abs() <= 4 * 2.0 ** -24).all())
