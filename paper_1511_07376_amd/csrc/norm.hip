@@ -11,8 +11,8 @@
 //
 // Bound by HBM: every tensor is read or written once, a row held in registers
 // between the sum and the result (up to 16384 values).  A work-item takes vectors of 8 values, so
-// that 16 lanes hold a block of 128.  8192 x 4096 bf16 with residual and sum, to 8 bits: 61 to 63
-// us, 3.8 TB/s, of which the 64 bits take 11 (made from fp32 values it was 50, 4.7 TB/s; a copy reaches
+// that 16 lanes hold a block of 128.  8192 x 4096 bf16 with residual and sum, to 8 bits: 59 to 63
+// us, 3.9 TB/s, of which the 64 bits take 10 (made from fp32 values it was 50, 4.7 TB/s; a copy reaches
 // 5.05); 77 x 1013 fp32 3 us, which is a kernel's least and a chain of load,
 // sum and store.
 #include "f8.h"
