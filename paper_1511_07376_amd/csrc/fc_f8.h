@@ -5,17 +5,13 @@
 // weights are the instructions' first operand and the inputs their second, so that
 // a lane's four sums are outputs of one token and share their scale.
 //
-// Two ways to sum a block:
-//  - on the 8-bit instruction (16 x 16 x 128, 5 PFLOP/s).  It adds the products of 8
-//    consecutive values as fixed-point numbers whose last place is 2^-13 of the power
-//    of two at or below the largest of them (found by trying: beside 2^16, 2^3 counts
-//    and 2^2 does not), and these sums in fp32.  So a product is off by 2^-13 of
-//    its group's largest at most: 1.5e-5 of a result of random values, a hundredth of
-//    what rounding it to bfloat16 takes, a fifteenth of fp16's.
-//  - in 16 bits: every 8-bit float is an fp16 number, the products are exact and are
-//    added in fp32, at half the rate and with conversions.
-// Results in fp32 take the second way, and so do all that are computed by rows (few tokens, or little
-// work), which are bound by reading; 16-bit results on tiles the first.
+// A block is summed in 16 bits: every 8-bit float is an fp16 number, the products are exact and are added in
+// fp32, at half the 8-bit rate and with conversions.  The 8-bit instructions are no way to do it: they add
+// the products of 8 values as fixed-point numbers whose last place is 2^-13 of the power of two at or below the
+// largest of them (found by trying, for 16 x 16 x 32, 32 x 32 x 16 and 16 x 16 x 128: random values of all
+// exponents come out off by up to 2^-10.3 of the largest product, in 16 bits by 2^-20.9), so that a product
+// beside a large one that cancels is lost whole.  What exactness costs: 2048 x 9216 x 4096 to bf16 takes 138 to 146 us
+// where it took 77, 512 x 4096 x 4096 28 where it took 18.
 #pragma once
 
 #include "f8.h"
@@ -23,7 +19,6 @@
 namespace cnn {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
@@ -81,14 +76,8 @@ __device__ inline f16x8 to_halves(unsigned a, unsigned b) {
 __device__ inline Halves to_halves(const Bytes& b) {
     return Halves{to_halves(b.v[0][0], b.v[0][1]), to_halves(b.v[0][2], b.v[0][3]), to_halves(b.v[1][0], b.v[1][1]), to_halves(b.v[1][2], b.v[1][3])};
 }
-__device__ inline i32x8 operand(const Bytes& b) {
-    return i32x8{(int)b.v[0][0], (int)b.v[0][1], (int)b.v[0][2], (int)b.v[0][3], (int)b.v[1][0], (int)b.v[1][1], (int)b.v[1][2], (int)b.v[1][3]};
-}
 
 // A block's sums: output 4 (lane / 16) + i of token lane % 16.
-__device__ inline f32x4 block_sums(const Bytes& w, const Bytes& x) {
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(w), operand(x), f32x4{0, 0, 0, 0}, 0, 0, 0, 0, 0, 0);
-}
 __device__ inline f32x4 block_sums(const Halves& w, const Halves& x) {
     f32x4 d = {0, 0, 0, 0};
 #pragma unroll
@@ -115,6 +104,12 @@ __device__ inline void store_value(int type, void* y, size_t at, float v) {
 struct F8Tile {
     int outs, tokens, parts, run;
 };
+// Which kernel a product takes: by rows, 16 times `tokens` of them and 16 times `outs` outputs a workgroup, or on a tile.
+struct F8Way {
+    int rows, tokens, outs;
+    F8Tile tile;
+};
+F8Way fc_f8_way(int N, int I, int O);
 // vec: rows of whole blocks at 16-byte addresses.
 void run_f8_tiles(const FcF8& p, const F8Tile& tile, bool vec, float* partial, hipStream_t st);
 

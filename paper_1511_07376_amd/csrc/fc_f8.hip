@@ -95,10 +95,14 @@ void run_rows(const FcF8& p, bool odd, hipStream_t st) {
     else enqueue(fc_f8_rows<NT, FO, false>, grid, block, 0, st, p, blocks, groups, (int)jobs);
 }
 
-// What a call costs one way or another, in us, as measured between 1 x 512 x 8192 and 4096 x 4096 x 8192.
+// What a call costs one way or another, in us, as measured between 1 x 512 x 8192, 1 x 4096 x 128256, 1 x 28672 x 8192 and
+// 4096 x 4096 x 8192.  Of 45 sizes measured on tiles and, few tokens, by rows, to fp32 and bf16, the way that the rule takes is
+// the quickest or within 7% of it but for two: 459 x 2171 x 1467 (27.8 us in 5 parts, 24.8 in 2) and 13 x 15616 x 130 (20.0, by rows 16.3).
 //
 // Rows: every workgroup reads its outputs' weights and its tokens' inputs, at some 6 TB/s from the L2s and behind them, and
-// three quarters to a half of that from odd addresses.
+// three quarters to a half of that from odd addresses; more workgroups than run at once read the weights at 4.7 TB/s
+// (1 x 8192 x 28672: 55 us, 46 on tiles; 1 x 4096 x 128256: 118, 115 on tiles), and a wave waits some 1.6 us for each block of
+// a long row (16 x 16384 x 128: 20.7 us, 14.9 on tiles in 16 parts; 8 x 28672 x 1024: 28.1 and 21.5).
 //
 // Tiles: their blocks' times, which grow with the workgroups that share a compute unit, or the weights' time from memory, and
 // some 3.5 us around them; parts take a second kernel, and their way through memory.
@@ -106,11 +110,9 @@ struct TileCost {
     int outs, tokens, slots;  // slots: workgroups that a compute unit holds
     float half, one, two;     // us a block with 128 workgroups or fewer, with 256, with 512
 };
-constexpr TileCost kCosts16[] = {{128, 64, 2, 0.37f, 0.47f, 0.75f}, {128, 128, 2, 0.70f, 0.85f, 1.30f}, {256, 128, 1, 0.95f, 1.15f, 0}, {256, 256, 1, 1.57f, 2.1f, 0}};
-constexpr TileCost kCosts32[] = {{128, 64, 3, 0.77f, 0.86f, 1.32f}, {128, 128, 2, 1.27f, 1.56f, 2.23f}};
+constexpr TileCost kCosts[] = {{128, 64, 3, 0.74f, 0.86f, 1.32f}, {128, 128, 2, 1.2f, 1.45f, 2.2f}, {256, 128, 1, 1.75f, 2.0f, 0}};
 // through registers
-constexpr TileCost kCostsStaged16[] = {{128, 64, 3, 1.15f, 1.25f, 2.1f}, {128, 128, 2, 1.6f, 1.65f, 2.2f}};
-constexpr TileCost kCostsStaged32[] = {{128, 64, 2, 1.45f, 1.68f, 2.3f}, {128, 128, 2, 2.2f, 2.5f, 3.2f}};
+constexpr TileCost kCostsStaged[] = {{128, 64, 2, 1.45f, 1.68f, 2.3f}, {128, 128, 2, 2.2f, 2.5f, 3.2f}};
 constexpr int kMostParts = 16;
 constexpr size_t kMostWorkspace = 64 << 20;
 
@@ -120,30 +122,26 @@ float block_time(const TileCost& c, int64_t jobs) {
     return at <= 0.5f ? c.half : at <= 1 ? c.half + (c.one - c.half) * (2 * at - 1) : c.one + (c.two - c.one) * (float)((jobs - 1) / 256);
 }
 
-// Rows of 16 `tokens` and `outs` of 16, or a tile.
-struct Way {
-    bool rows;
-    int tokens, outs;
-    F8Tile tile;
-};
-// By sizes and the type alone (the workspace is sized before the call's pointers are known).
-Way choose(int N, int I, int O, bool wide32) {
+}  // namespace
+
+// By sizes alone: the workspace is sized before the call's pointers are known, and results of every type are the same sums.
+F8Way fc_f8_way(int N, int I, int O) {
     const int blocks = f8_blocks(I);
-    Way best{};
+    F8Way best{};
     float least = 3e38f;
     constexpr int kRows[][2] = {{1, 1}, {1, 2}, {2, 1}, {4, 1}};
     for (const auto& r : kRows) {
         const int64_t jobs = (int64_t)ceil_div(O, 16 * r[1]) * ceil_div(N, 16 * r[0]);
         // 256 of them at once take one's time, and 32 outputs a workgroup are slower where there are fewer
         const float bytes = (float)std::max<int64_t>(jobs, r[1] == 2 ? 256 : 128) * (float)(16 * r[1] + std::min(N, 16 * r[0])) * (float)I;
-        const float time = 3.0f + bytes / 6.3e6f * (I % 4 == 0 ? 1.0f : r[0] == 4 ? 2.1f : 1.3f);
-        if (time < least) least = time, best = Way{true, r[0], r[1], {}};
+        const float most = std::max({bytes / 6.3e6f, jobs > 512 ? (float)O * (float)I / 4.7e6f : 0.0f, (float)(blocks / kMostWaves) * 1.6f});
+        const float time = 3.0f + most * (I % 4 == 0 ? 1.0f : r[0] == 4 ? 2.1f : 1.3f);
+        if (time < least) least = time, best = F8Way{1, r[0], r[1], {}};
     }
     const bool staged = I % kF8Block != 0;
-    const TileCost* costs = staged ? (wide32 ? kCostsStaged32 : kCostsStaged16) : wide32 ? kCosts32 : kCosts16;
     const float read = (float)O * (float)I / 8e6f;
-    for (int c = 0; c < (staged || wide32 ? 2 : 4); ++c) {
-        const TileCost& cost = costs[c];
+    for (int c = 0; c < (staged ? 2 : 3); ++c) {
+        const TileCost& cost = staged ? kCostsStaged[c] : kCosts[c];
         const int64_t tiles = (int64_t)ceil_div(O, cost.outs) * ceil_div(N, cost.tokens), round = 256 * cost.slots;
         for (int parts = 1; parts <= kMostParts; ++parts) {
             const int run = parts == 1 ? blocks : ceil_div(ceil_div(blocks, parts), 4) * 4;
@@ -152,32 +150,25 @@ Way choose(int N, int I, int O, bool wide32) {
             const int64_t jobs = tiles * parts, full = jobs / round, rest = jobs % round;
             const float each = (float)full * block_time(cost, round) + (rest ? block_time(cost, rest) : 0.0f);
             const float time = 3.5f + std::max((float)run * each, read) + (parts > 1 ? 3.2f + 0.75e-6f * bytes : 0.0f);
-            if (time < least) least = time, best = Way{false, 0, 0, F8Tile{cost.outs, cost.tokens, parts, run}};
+            if (time < least) least = time, best = F8Way{0, 0, 0, F8Tile{cost.outs, cost.tokens, parts, run}};
         }
     }
     return best;
 }
 
-}  // namespace
-
-// The type decides too: the larger of the two needs.
 size_t fc_f8_workspace(int N, int I, int O) {
-    size_t need = 0;
-    for (const bool wide32 : {false, true}) {
-        const Way way = choose(N, I, O, wide32);
-        if (!way.rows && way.tile.parts > 1) need = std::max(need, (size_t)way.tile.parts * N * O * sizeof(float));
-    }
-    return need;
+    const F8Way way = fc_f8_way(N, I, O);
+    return way.rows || way.tile.parts == 1 ? 0 : (size_t)way.tile.parts * N * O * sizeof(float);
 }
 
 int launch_fc_f8(const FcF8& p, float* ws, hipStream_t st) {
     if (p.N == 0) return CNN_OK;
-    Way way = choose(p.N, p.I, p.O, p.y_type == CNN_F32);
+    F8Way way = fc_f8_way(p.N, p.I, p.O);
     auto whole = [&](int to) { return (uintptr_t)p.x % to == 0 && (uintptr_t)p.w % to == 0; };
     const bool odd = !whole(4) || p.I % 4 != 0;
     if (!way.rows) {
         const bool vec = whole(16) && p.I % kF8Block == 0;
-        if (!vec && way.tile.outs == 256) way.tile.outs = way.tile.tokens = 128;  // whole blocks at addresses that are not
+        if (!vec && way.tile.outs == 256) way.tile.outs = 128;  // whole blocks at addresses that are not
         run_f8_tiles(p, way.tile, vec, ws, st);
     } else if (way.tokens == 1) {
         way.outs == 1 ? run_rows<1, 1>(p, odd, st) : run_rows<1, 2>(p, odd, st);

@@ -1,7 +1,7 @@
 // Products on 8-bit floats for many tokens: tiles of outputs x tokens, operands staged in LDS.
 //
 // A workgroup walks the reduction block by block.  While the matrix cores work on one, the
-// next one (or two) are on their way into other LDS buffers: rows that are whole 16-byte
+// next one is on its way into another LDS buffer: rows that are whole 16-byte
 // vectors are copied there by the load instruction itself, other rows go through registers.
 // LDS rows are a block's 128 bytes without padding (the copying loads write 64
 // consecutive vectors); the vectors of a row are exchanged by an XOR with three bits of
@@ -10,9 +10,10 @@
 // A wave's outputs are dealt to the instruction's rows so that a lane ends with 4 FO
 // neighbouring outputs of a token, which it stores as they are.
 //
-// 2048 x 9216 x 4096 to bf16 (256 x 128 tiles): 77 us, 2.0 PFLOP/s; the matrix cores are at work for 40% of it,
-// and waves wait for a block's barrier, LDS and each other's turn for the rest.  64 x 9216 x 4096 to fp32 (128 x 64
-// tiles in 6 parts): 16 us and 4 for the join, of which reading the weights would take 7.5.
+// 2048 x 9216 x 4096 to bf16 (256 x 128 tiles): 138 to 146 us, 1.1 PFLOP/s (a large product of bf16 matrices runs
+// at 1.4): what is not the products' time is the conversions of both operands, which every wave makes of what it reads, and a
+// block's barrier.  64 x 9216 x 4096 to fp32 (128 x 64 tiles in 6 parts): 16 us and 4 for the join, of which reading
+// the weights would take 7.5.
 #include "fc_f8.h"
 
 #include <algorithm>
@@ -43,7 +44,7 @@ struct TileParams {
 
 // 64 lanes' 16 (4) bytes, at 32-bit offsets from a base, to consecutive places in LDS.  Not by the compiler's builtins: it
 // would wait for all such copies before reads of LDS that it cannot tell from their targets, and so for those that are
-// meant to be on their way over several blocks.  What is copied is read behind a wait and a barrier only (block_barrier).
+// meant to be on their way while a block is worked on.  What is copied is read behind a wait and a barrier only (block_barrier).
 __device__ inline unsigned lds_address(const void* p) { return (unsigned)(uintptr_t)(const __attribute__((address_space(3))) char*)p; }
 __device__ inline void copy16(const void* base, unsigned at, unsigned lds) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(at), "s"(base) : "m0");
@@ -101,7 +102,7 @@ struct TokenKey {
 };
 
 // All the wave's loads but the last LEFT have landed, its LDS accesses are done; then all waves'.
-template <int LEFT>
+template <int LEFT = 0>
 __device__ inline void block_barrier() {
     static_assert(LEFT < 64, "what the counter of loads holds");
     asm volatile("" ::: "memory");
@@ -133,18 +134,13 @@ __device__ inline void store_outputs(void* y, size_t at, const float* v, int64_t
     }
 }
 
-// YT: the result's type; fp32 ones are summed in 16 bits, others on the 8-bit instruction.
-// SPLIT: sums go to the workspace, without bias.
-// DEPTH: LDS buffers, of which all but the one that is worked on are on their way.
-template <int WO, int WT, int FO, int FT, bool VEC, int DEPTH, int YT, bool SPLIT>
+// YT: the result's type.  SPLIT: sums go to the workspace, without bias.
+template <int WO, int WT, int FO, int FT, bool VEC, int YT, bool SPLIT>
 __global__ void __launch_bounds__(64 * WO * WT, 2) fc_f8_tiles(TileParams tp) {
     using S = Shape<WO, WT, FO, FT>;
-    using Operand = std::conditional_t<YT == CNN_F32, Halves, Bytes>;
     constexpr int TO = S::TO, TT = S::TT, NT = S::NT;
-    static_assert(DEPTH == 2 || VEC, "what goes through registers is one block ahead");
-    static_assert(DEPTH >= 2 && DEPTH <= 4, "the scales have landed before they are read");
     constexpr int kBuffer = (TO + TT) * kF8Block;
-    __shared__ __attribute__((aligned(16))) char buffers[DEPTH * kBuffer];  // outputs' rows, then tokens'
+    __shared__ __attribute__((aligned(16))) char buffers[2 * kBuffer];  // outputs' rows, then tokens'
     __shared__ __attribute__((aligned(16))) float sScale[2][4 * TT];
     __shared__ float sWeight[2][64];  // the weights' scales: 4 blocks of each 128 outputs
     static_assert(NT > TT, "a lane a token, and a wave for the weights");
@@ -207,10 +203,6 @@ __global__ void __launch_bounds__(64 * WO * WT, 2) fc_f8_tiles(TileParams tp) {
             return Bytes{*reinterpret_cast<const u32x4*>(base + row * kF8Block + v * 16),
                          *reinterpret_cast<const u32x4*>(base + row * kF8Block + (v ^ 4) * 16)};
         };
-        auto as_operand = [&](const Bytes& b) {
-            if constexpr (YT == CNN_F32) return to_halves(b);
-            else return b;
-        };
         // Asks for block k, or, behind the last one, for that again (nothing comes of it).
         auto ask = [&](int k, char* to) {
             k = min(k, last - 1);
@@ -218,7 +210,7 @@ __global__ void __launch_bounds__(64 * WO * WT, 2) fc_f8_tiles(TileParams tp) {
             fx.load(p.x, k, p.I, to + TO * kF8Block);
         };
         const int key = S::out_key(orow);
-        Operand x[FT];
+        Halves x[FT];
         Bytes next;                   // the outputs' next fragment
         f32x4 d[2][FT];               // a fragment's sums, and those of the one before
         float s[FT], before[FT];      // a block's scales, and those of the one before
@@ -232,29 +224,28 @@ __global__ void __launch_bounds__(64 * WO * WT, 2) fc_f8_tiles(TileParams tp) {
                 to[j] = k < last ? v : 0.0f;
             }
         };
-        auto read_token = [&](const char* buffer, int j) { x[j] = as_operand(read(buffer + TO * kF8Block, trow + 16 * j, S::token_key(l16))); };
+        auto read_token = [&](const char* buffer, int j) { x[j] = to_halves(read(buffer + TO * kF8Block, trow + 16 * j, S::token_key(l16))); };
         // Block k, whose first fragments are in registers.  The products of a fragment of outputs are at work while the sums
-        // of the one before are added.  Before its last fragment's products the next block is made ready, a later one is
+        // of the one before are added.  Before its last fragment's products the next block is made ready, the one after it is
         // asked for (this one's buffer is free: all waves have read what they need), and the next one's
         // first fragments are read: those products cover that.
-        constexpr int OPS = decltype(fw)::N + decltype(fx)::N;  // a wave's loads for a block
         auto work = [&](int k, char* here, char* after) {
             float s_after[FT];
 #pragma unroll
             for (int i = 0; i < FO; ++i) {
-                const Operand w = as_operand(next);
+                const Halves w = to_halves(next);
                 if (i + 1 < FO) {
                     next = read(here, orow + 4 * (i + 1), key);
                 } else {
                     fw.store(after);
                     fx.store(after + TO * kF8Block);
-                    block_barrier<(DEPTH - 2) * OPS>();
+                    block_barrier();
                     read_scales(k + 1, s_after);
                     next = read(after, orow, key);
                     __builtin_amdgcn_sched_barrier(0);
-                    ask(k + DEPTH, here);
-                    // the other group's places have been read by all waves; what is asked for now is used 3 blocks later, and
-                    // two blocks' loads are asked for before that: the barriers wait for it
+                    ask(k + 2, here);
+                    // the other group's places have been read by all waves; what is asked for now is used 3 blocks later,
+                    // behind the barriers between, which wait for it
                     if (((k - first) & 3) == 0 && k + 4 < last) ask_scales(((k - first) >> 2) + 1);
                 }
 #pragma unroll
@@ -276,9 +267,8 @@ __global__ void __launch_bounds__(64 * WO * WT, 2) fc_f8_tiles(TileParams tp) {
             ask(first, buffers);
             fw.store(buffers);
             fx.store(buffers + TO * kF8Block);
-#pragma unroll
-            for (int i = 1; i < DEPTH; ++i) ask(first + i, buffers + i * kBuffer);
-            block_barrier<VEC ? (DEPTH - 1) * OPS : 0>();
+            ask(first + 1, buffers + kBuffer);
+            block_barrier<VEC ? decltype(fw)::N + decltype(fx)::N : 0>();  // that block's loads may be on their way
             next = read(buffers, orow, key);
             read_scales(first, s);
 #pragma unroll
@@ -287,11 +277,11 @@ __global__ void __launch_bounds__(64 * WO * WT, 2) fc_f8_tiles(TileParams tp) {
                 before[j] = 0.0f;
                 d[1][j] = f32x4{0, 0, 0, 0};
             }
-            // whole turns of the buffers: blocks behind the last one have a scale of 0
+            // whole turns of the buffers: a block behind the last one has a scale of 0
 #pragma unroll 1
-            for (int k = first; k < last; k += DEPTH) {
-#pragma unroll
-                for (int i = 0; i < DEPTH; ++i) work(k + i, buffers + i * kBuffer, buffers + (i + 1) % DEPTH * kBuffer);
+            for (int k = first; k < last; k += 2) {
+                work(k, buffers, buffers + kBuffer);
+                work(k + 1, buffers + kBuffer, buffers);
             }
 #pragma unroll
             for (int j = 0; j < FT; ++j) add_scaled(acc[FO - 1][j], d[1][j], before[j]);
@@ -313,7 +303,7 @@ __global__ void __launch_bounds__(64 * WO * WT, 2) fc_f8_tiles(TileParams tp) {
                 else store_outputs<YT, FO * 4>(p.y, (size_t)n * p.O + o, v, count);
             }
         }
-        block_barrier<0>();  // nothing is on its way to the buffers, which are the next tile's
+        block_barrier();  // nothing is on its way to the buffers, which are the next tile's
     }
 }
 
@@ -358,18 +348,14 @@ __global__ void __launch_bounds__(256) fc_f8_join(TileParams tp) {
 template <int WO, int WT, int FO, int FT, bool VEC, int YT>
 void start(const FcF8& p, const F8Tile& t, float* partial, hipStream_t st) {
     using S = Shape<WO, WT, FO, FT>;
-    // Three buffers for the smallest tiles of 16-bit results: 64 x 9216 x 4096, 32 of them, 42.5 to 30.7 us, in 6 parts 17.8 to
-    // 16.0; 512 x 4096 x 4096 22.9 to 18.4.  No faster are four, or three for fp32 results (53.1 and 52.7), or for
-    // larger tiles (2048 x 9216 x 4096 on 256 x 128: 77 and 84): they have enough to do for a block's time.
-    constexpr int DEPTH = VEC && S::TT == 64 && YT != CNN_F32 ? 3 : 2;
     const int blocks = f8_blocks(p.I);
     TileParams tp{p, blocks, ceil_div(p.O, S::TO), 0, t.parts, t.run, (uintptr_t)p.xs % 16 == 0 && blocks % 4 == 0, partial};
     tp.tiles = tp.out_tiles * ceil_div(p.N, S::TT);
     const dim3 grid((unsigned)std::min<int64_t>((int64_t)tp.tiles * tp.parts, 1 << 20));
     if (t.parts == 1) {
-        enqueue(fc_f8_tiles<WO, WT, FO, FT, VEC, DEPTH, YT, false>, grid, dim3(S::NT), 0, st, tp);
+        enqueue(fc_f8_tiles<WO, WT, FO, FT, VEC, YT, false>, grid, dim3(S::NT), 0, st, tp);
     } else {
-        enqueue(fc_f8_tiles<WO, WT, FO, FT, VEC, DEPTH, YT, true>, grid, dim3(S::NT), 0, st, tp);
+        enqueue(fc_f8_tiles<WO, WT, FO, FT, VEC, YT, true>, grid, dim3(S::NT), 0, st, tp);
         enqueue(fc_f8_join<YT>, dim3((unsigned)std::min<int64_t>(ceil_div64((int64_t)p.N * p.O, 1024), 1 << 16)), dim3(256), 0, st, tp);
     }
 }
@@ -377,7 +363,7 @@ void start(const FcF8& p, const F8Tile& t, float* partial, hipStream_t st) {
 template <int WO, int WT, int FO, int FT, bool VEC>
 void start_type(const FcF8& p, const F8Tile& t, float* partial, hipStream_t st) {
     if (p.y_type == CNN_F32) {
-        if constexpr (WO * WT == 4) start<WO, WT, FO, FT, VEC, CNN_F32>(p, t, partial, st);
+        start<WO, WT, FO, FT, VEC, CNN_F32>(p, t, partial, st);
     } else if (p.y_type == CNN_BF16) {
         start<WO, WT, FO, FT, VEC, CNN_BF16>(p, t, partial, st);
     } else {
@@ -394,10 +380,8 @@ void run_f8_tiles(const FcF8& p, const F8Tile& t, bool vec, float* partial, hipS
     } else if (t.outs == 128) {
         if (vec) start_type<2, 2, 4, 4, true>(p, t, partial, st);
         else start_type<2, 2, 4, 4, false>(p, t, partial, st);
-    } else if (t.tokens == 128) {
-        start_type<4, 2, 4, 4, true>(p, t, partial, st);
     } else {
-        start_type<2, 4, 8, 4, true>(p, t, partial, st);
+        start_type<4, 2, 4, 4, true>(p, t, partial, st);
     }
 }
 

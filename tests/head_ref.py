@@ -113,11 +113,11 @@ def assert_product(got, want, s, i, what):
     """A product's results against the float64 ones.
 
     fp32 results: every product is exact and added in fp32, so that experts_ref's bound holds, a step of 2^-23 of the sum
-    of magnitudes S for every addition and rounding.  16-bit results may be of the matrix cores' 8-bit instruction,
-    which adds the products of 8 consecutive values in steps of 2^-13 of the power of two at or below the largest of
-    them: 8 steps a group, no more than 2^-10 of the group's S, and of all S in sum.  The groups' errors are
-    independent, so that their 2-norm is within 2^-10 S / sqrt(groups) for S spread over them; twice that is
-    allowed."""
+    of magnitudes S for every addition and rounding.  16-bit results are those rounded, which test_gpu_f8_ways holds
+    them to by equality; the bounds here are wider: they would allow for products added by eights in steps of 2^-13 of
+    the power of two at or below the largest of them: 8 steps a group, no more than 2^-10 of the group's S, and of all
+    S in sum.  The groups' errors would be independent, so that their 2-norm is within 2^-10 S / sqrt(groups) for S
+    spread over them; twice that is allowed."""
     if got.dtype is torch.float32:
         experts_ref.assert_product(got, want, s, steps(i), what)
         return
