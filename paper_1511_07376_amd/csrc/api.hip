@@ -2,6 +2,7 @@
 // executor (a layer list run in order over two ping-pong activation buffers
 // in a caller-provided workspace).
 #include <algorithm>
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
@@ -222,7 +223,7 @@ int check_rms_norm(const RmsNorm& p) {
     if ((p.y_type == CNN_F8) != (p.y_scale != nullptr) && p.rows != 0)
         return fail(CNN_ERR_INVALID, "rms_norm: scales go with 8-bit results, and with those only");
     if (p.rows < 0 || p.cols <= 0) return fail(CNN_ERR_INVALID, "rms_norm: %d rows of %d", p.rows, p.cols);
-    if (!(p.eps >= 0.0f) || p.eps > 3.4e38f) return fail(CNN_ERR_INVALID, "rms_norm: eps %g", (double)p.eps);
+    if (!(p.eps >= 0.0f && p.eps < INFINITY)) return fail(CNN_ERR_INVALID, "rms_norm: eps %g", (double)p.eps);
     if (p.rows != 0 && (!p.x || !p.y)) return fail(CNN_ERR_INVALID, "rms_norm: null x or y");
     if (p.sum && p.sum == p.y) return fail(CNN_ERR_INVALID, "rms_norm: y and sum are the same tensor");
     if (p.y_type == CNN_F8 && p.y && (p.y == p.x || p.y == p.residual))

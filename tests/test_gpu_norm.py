@@ -171,3 +171,12 @@ def test_norm_in_8_bits_is_that_of_unrounded_values(gpu, rows, cols, residual):
     want, want_scale = ref.quantize(ref.norm(x, r, w, 1e-5)[1])
     assert torch.equal(q.double(), want)
     assert bool(((scale.double() / want_scale.double() - 1).abs() <= 4 * 2.0 ** -24).all())
+
+
+def test_norm_of_the_largest_eps(gpu):
+    """eps of fp32's largest number, beside squares of 2^100 and of 2^130."""
+    x, _, w = inputs(2, 200, torch.float32, 5)
+    x[0] *= 2.0 ** 50
+    x[1] *= 2.0 ** 65
+    eps = float(torch.finfo(torch.float32).max)
+    ref.assert_norm(gpu.cnn_rms_norm_fwd(x, w, eps=eps), ref.norm(x, None, w, eps)[1], "largest eps")

@@ -61,6 +61,12 @@ def test_norm_refuses(kw, status):
         assert cnn.cnn_last_error().startswith("rms_norm")
 
 
+@pytest.mark.parametrize("eps", [0.0, 2.0 ** -149, 3.4e38, 3.4028234663852886e38])
+def test_norm_takes_every_finite_eps(eps):
+    """Up to fp32's largest number."""
+    assert _norm(eps=eps, rows=0, x=0, y=0) == OK
+
+
 def _fc(**kw):
     a = dict(x=FAKE, xs=FAKE, N=4, I=64, w=FAKE, ws=FAKE, bias=0, O=8, relu=0, y=FAKE, yt=BF16, work=0, n=0, st=0)
     a.update(kw)
