@@ -61,6 +61,13 @@ def norm(x, residual, weight, eps):
     return s, y * weight.double() if weight is not None else y
 
 
+def norm_inputs(rows, cols, dtype):
+    """x, a residual of its size and weights, whose sums are not numbers of the type: on the CPU, the same ones each time."""
+    g = torch.Generator().manual_seed(rows + cols)
+    x, r = (torch.randn((rows, cols), generator=g).to(dtype) for _ in range(2))
+    return x, r, 1 + 0.2 * torch.randn((cols,), generator=g)
+
+
 #: y is rounded after the product with 1 / rms (held in 64 bits) and after the weight: two roundings, and a little
 NORM_REL = 2.02 * 2.0 ** -24
 

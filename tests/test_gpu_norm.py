@@ -180,3 +180,16 @@ def test_norm_of_the_largest_eps(gpu):
     x[1] *= 2.0 ** 65
     eps = float(torch.finfo(torch.float32).max)
     ref.assert_norm(gpu.cnn_rms_norm_fwd(x, w, eps=eps), ref.norm(x, None, w, eps)[1], "largest eps")
+
+
+@pytest.mark.parametrize("dtype", TYPES[1:], ids=IDS[1:])
+@pytest.mark.parametrize("rows,cols", [(4, 1000), (3, 20000), (2, 40000)])
+def test_norm_is_not_that_of_the_rounded_sum(gpu, rows, cols, dtype):
+    """Values at which the bounds tell the two apart: here, and for 4 x 1000 without a GPU (``test_head_abi``)."""
+    x, r, w = (t.cuda() for t in ref.norm_inputs(rows, cols, dtype))
+    s, want = ref.norm(x, r, w, 1e-6)
+    other = ref.norm(s.to(dtype), None, w, 1e-6)[1]
+    with pytest.raises(AssertionError):
+        ref.assert_norm(other.to(dtype), want, "rounded")
+    ref.assert_norm(gpu.cnn_rms_norm_fwd(x, w, r)[0], want, "unrounded")
+    ref.assert_norm_f8(*gpu.cnn_rms_norm_fwd(x, w, r, f8=True)[:2], want, "unrounded, 8 bits")

@@ -145,6 +145,21 @@ def test_reference_norm():
     assert torch.allclose(y, want, rtol=1e-15, atol=0) and torch.equal(s, x)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16], ids=["bf16", "f16"])
+def test_norm_bounds_see_a_sum_that_is_rounded_first(dtype):
+    """The norm is of x + residual as it is before it is rounded to x's type: results of the rounded sum are outside the bounds,
+    in the wide type and in 8 bits, results of the unrounded one are within."""
+    x, r, w = ref.norm_inputs(4, 1000, dtype)
+    s, want = ref.norm(x, r, w, 1e-6)
+    other = ref.norm(s.to(dtype), None, w, 1e-6)[1]
+    ref.assert_norm(want.to(dtype), want, "unrounded")
+    ref.assert_norm_f8(*ref.quantize(want), want, "unrounded")
+    with pytest.raises(AssertionError):
+        ref.assert_norm(other.to(dtype), want, "rounded")
+    with pytest.raises(AssertionError):
+        ref.assert_norm_f8(*ref.quantize(other), want, "rounded")
+
+
 def test_reference_product():
     g = torch.Generator().manual_seed(3)
     x, w = ref.random_f8((3, 150), g), ref.random_f8((130, 150), g)
