@@ -10,9 +10,9 @@
 // A wave's outputs are dealt to the instruction's rows so that a lane ends with 4 FO
 // neighbouring outputs of a token, which it stores as they are.
 //
-// 2048 x 9216 x 4096 to bf16 (256 x 128 tiles): 138 to 146 us, 1.1 PFLOP/s (a large product of bf16 matrices runs
-// at 1.4): what is not the products' time is the conversions of both operands, which every wave makes of what it reads, and a
-// block's barrier.  64 x 9216 x 4096 to fp32 (128 x 64 tiles in 6 parts): 16 us and 4 for the join, of which reading
+// 2048 x 9216 x 4096 to bf16 (256 x 128 tiles): 133 to 146 us, 1.1 PFLOP/s (a large product of bf16 matrices runs
+// at 1.4); the matrix cores are at work for 52% of it and the vector units, which convert both operands in every wave
+// that reads them, for 57%.  64 x 9216 x 4096 to fp32 (128 x 64 tiles in 6 parts): 16 us and 4 for the join, of which reading
 // the weights would take 7.5.
 #include "fc_f8.h"
 
@@ -80,7 +80,8 @@ struct Fetch {
         for (int i = 0; i < N; ++i) {
             const int in = vector_of(i) * 16;
             if constexpr (VEC) copy16(base, at[i], to + i * NT * 16);
-            // (at odd addresses too: loaded by words and shifted, as for few rows, 1500 x 4001 x 4001 was 75 us against 67)
+            // (at odd addresses too: 1500 x 4001 x 4001 takes 99 to 103 us; loaded by words and shifted, as for few rows, it was a
+            // tenth slower on products of half the time)
             else if (left >= kF8Block) reg[i] = load16(base + at[i]);
             else reg[i] = load_bytes_edge(base + at[i], left - in, (int64_t)k * kF8Block + in);
         }
@@ -168,8 +169,8 @@ __global__ void __launch_bounds__(64 * WO * WT, 2) fc_f8_tiles(TileParams tp) {
         fw.begin(o0, p.O, p.I);
         fx.begin(n0, p.N, p.I);
         // The inputs' scales come in groups of 4 blocks, a lane a token: a row's are neighbours, and a line for
-        // every token and block would take as long as the operands (2048 x 9216 x 4096: 99 us against 109 with half as
-        // many of them, and 77 against 100 for the copies alone).  So do the weights', a lane one of them.  (A scalar load of
+        // every token and block would take as long as the operands (2048 x 9216 x 4096 on products of half the time:
+        // 99 us against 109 with half as many of them, and 77 against 100 for the copies alone).  So do the weights', a lane one of them.  (A scalar load of
         // the block's would make the reads of LDS after it wait for all before.)
         const unsigned xs = (unsigned)min(tid % TT, (int)min((int64_t)p.N - 1 - n0, (int64_t)TT)) * (unsigned)tp.blocks * 4;  // fewer than 2^31 bytes
         auto ask_scales = [&](int group) {
